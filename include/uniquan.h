@@ -732,6 +732,123 @@ uq_status uniquan_bcq_matmul(int T, int64_t R, int64_t C, int k, int g,
                              void* stream);
 
 /*
+ * Serving the deployed block: a paged key/value cache and the attention of
+ * one new token over it.  Between the deployed products of one decoding step
+ * (uniquan_bcq_matmul) a serving loop calls uniquan_kv_append on the rows of
+ * the query, key and value products and uniquan_attn_decode on the rotated
+ * queries; its O rows are the output product's activations.  For a prompt,
+ * uniquan_kv_read gives keys and values back in uniquan_attn_fwd's layout.
+ *
+ * Cache.  Positions 0, 1, ... of a sequence lie in pages of page_len
+ * positions: position p of sequence s is place p % page_len of page
+ * pages[s max_pages + p / page_len] (int32 page table, [n_seq x max_pages]).
+ * Keys and values have one array each, [n_pages][H_kv][page_len][row], and
+ * for codes one array of statistics each, [n_pages][H_kv][d / group]
+ * [page_len][2] bf16: (scale, lo) of every group of `group` channels.
+ *   UQ_KV_BF16  row: d bf16 values in channel order; group 0, no statistics.
+ *   UQ_KV_U8    row: d bytes; codes 0..255.
+ *   UQ_KV_U4    row: d / 2 bytes; codes 0..15, two a byte, the lower first.
+ * A code c stands for lo + scale c.  Order of the codes in a row: channel ch
+ * of a key at (ch / 8 % 4)(d / 4) + 8 (ch / 32) + j, where j is ch % 8 for
+ * UQ_KV_U8 and (ch % 8) / 2 + 4 (ch % 2) for UQ_KV_U4; channel ch of a value
+ * at (ch % 16)(d / 16) + ch / 16 (so that a lane of the attention finds its
+ * channels side by side).
+ * Quantiser of a group x, top = 255 or 15 (fp32, no contraction):
+ *   lo    = min x rounded down to bf16
+ *   scale = (max x - lo) fl(1 / top) rounded up to bf16; 0 if below 2^-126
+ *   c     = rint((x - lo) fl(1 / scale)), at most top; 0 where scale is 0
+ * so every value comes back to within half a scale.  A group with a
+ * non-finite value, or whose max x - lo overflows, gets NaN for scale and lo
+ * and comes back as NaN.
+ * A page id outside [0, n_pages) is no page (-1: not allocated, or evicted):
+ * nothing is written there and its positions take no part in an attention.
+ * Sequences may share pages that are only read.  Two rows of one append must
+ * not name the same place: which of them it then holds is not defined.
+ *
+ * Rules shared by the three calls.  d is 64 or 128 (UQ_EUNSUPPORTED
+ * otherwise); group is 0 for UQ_KV_BF16, else 32 or d; page_len a power of
+ * two in [16, 1024]; H a multiple of H_kv <= 4096, head h reading key/value
+ * head h / (H / H_kv); max_pages page_len < 2^31.  Cache arrays and fp32/bf16
+ * rows 16-byte, int32 arrays 4-byte aligned.  k_stat and v_stat are NULL for
+ * UQ_KV_BF16.
+ */
+typedef enum { UQ_KV_BF16 = 0, UQ_KV_U8 = 1, UQ_KV_U4 = 2 } uq_kv_format;
+
+/*
+ * uniquan_kv_append -- T new rows into the cache.  Row t belongs to sequence
+ * seq[t] (seq NULL: t) at position pos[t].  With cs given (n_cs rows of
+ * uniquan_rope_table's layout [n_cs, d/2] (cos, sin); that table's fp32 angles
+ * are off by up to p 2^-23 at position p, so far positions want one computed
+ * in 64 bits), the heads of q and k are rotated at pos[t]:
+ *   y_i = x_i cos - x_{i+d/2} sin,  y_{i+d/2} = x_{i+d/2} cos + x_i sin (fp32);
+ * then q rows are rounded to bf16 in q_out and k, v rows are stored in the
+ * cache's format.  A row whose position is negative, not below n_cs (with cs)
+ * or not below max_pages page_len, or whose sequence is not in [0, n_seq), is
+ * padding: nothing is written for it, its q_out row is left as it was.  A row
+ * whose page is none gets its q_out row only.
+ *
+ * q [T] rows of H d, k, v [T] rows of H_kv d, in_dtype (UQ_F32 or UQ_BF16),
+ * rows ld_q, ld_k, ld_v elements apart (multiples of 8; 0: no gap); q may be
+ * NULL (with q_out).  q_out [T x H d] bf16, row-major.  H is H_kv where q is
+ * NULL.  T >= 0 (0: nothing to do), T (H + 2 H_kv) <= 2^28.
+ */
+uq_status uniquan_kv_append(int64_t T, int H, int H_kv, int d,
+                            const void* q, int64_t ld_q, const void* k, int64_t ld_k,
+                            const void* v, int64_t ld_v, int in_dtype,
+                            const int32_t* seq, const int32_t* pos,
+                            const float* cs, int64_t n_cs,
+                            const int32_t* pages, int64_t n_seq, int64_t max_pages,
+                            int format, int group, int64_t n_pages, int page_len,
+                            void* k_cache, void* v_cache, uint16_t* k_stat, uint16_t* v_stat,
+                            uint16_t* q_out, void* stream);
+
+/*
+ * uniquan_kv_read -- positions [start[s], start[s] + L) of every sequence
+ * (start NULL: 0) back from the cache: K and V [H_kv][n_seq][L][d], the
+ * key/value layout of uniquan_attn_fwd (batch h n_seq + s), out_dtype UQ_F32
+ * or UQ_BF16 (nearest even); values of codes are lo + scale c in fp32 before
+ * that.  Positions outside [0, lens[s]) and positions on no page are 0.  K or
+ * V may be NULL.  n_seq H_kv L <= 2^28.
+ */
+uq_status uniquan_kv_read(int64_t n_seq, int H_kv, int d, int64_t L,
+                          const int32_t* start, const int32_t* lens,
+                          const int32_t* pages, int64_t max_pages,
+                          int format, int group, int64_t n_pages, int page_len,
+                          const void* k_cache, const void* v_cache,
+                          const uint16_t* k_stat, const uint16_t* v_stat,
+                          void* K, void* V, int out_dtype, void* stream);
+
+/*
+ * uniquan_attn_decode -- attention of one query row per sequence over its
+ * cached positions t < lens[s] (capped at max_pages page_len; <= 0: none)
+ * that lie on a page: per head h, with x_t = scale q . k_t,
+ *   row_lse = log2 sum_t 2^(x_t log2 e)   (the base-2 log-sum-exp of
+ *                                          uniquan_attn_fwd; may be NULL)
+ *   O = sum_t 2^(x_t log2 e - row_lse) v_t
+ * in fp32 from the stored values, O rounded to bf16.  Where no position
+ * takes part O is 0 and row_lse -infinity.  What the cache holds at other
+ * positions has no influence, whatever it is.  Long sequences are split over
+ * workgroups and joined in a fixed order, so results do not change from run
+ * to run; how they are split depends on lens alone.
+ *
+ * Q [n_seq] rows of H d bf16, ld_q elements apart (a multiple of 8; 0: H d);
+ * O [n_seq] rows of H d bf16, ld_o elements apart (a multiple of 4; 0: H d);
+ * row_lse [n_seq x H] fp32.  ws [ws_len] fp32 workspace of at least
+ * uniquan_attn_decode_ws(n_seq, H, H_kv, d, max_pages, page_len) floats
+ * (16-byte aligned; 0: may be NULL), free to be reused once the call is done;
+ * calls that overlap need one each.  n_seq H <= 2^24.
+ */
+size_t uniquan_attn_decode_ws(int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len);
+uq_status uniquan_attn_decode(int64_t n_seq, int H, int H_kv, int d,
+                              const uint16_t* Q, int64_t ld_q, const int32_t* lens,
+                              const int32_t* pages, int64_t max_pages,
+                              int format, int group, int64_t n_pages, int page_len,
+                              const void* k_cache, const void* v_cache,
+                              const uint16_t* k_stat, const uint16_t* v_stat,
+                              float scale, uint16_t* O, int64_t ld_o, float* row_lse,
+                              float* ws, size_t ws_len, void* stream);
+
+/*
  * uniquan_init_greedy -- greedy binary-coding start of the appendix
  * algorithm "General alternating update" (its first step): per group,
  * r = wbar - z_B with wbar = T_F(w) as in uniquan_fq_fwd; then for

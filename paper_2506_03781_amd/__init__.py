@@ -5,4 +5,4 @@ and ``layer`` drives one optimisation step of one linear layer through it.
 Importing the package does not load the library; the first call does, and
 fails loudly if it has not been built.
 """
-__all__ = ["uniquan", "layer", "synth", "build"]
+__all__ = ["uniquan", "layer", "cache", "synth", "build"]

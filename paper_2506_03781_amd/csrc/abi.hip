@@ -759,6 +759,129 @@ uq_status uniquan_attn_bwd(int64_t batch, int64_t kv_batch, int L, int d, const 
   return hip_status(fn, uq::launch_attn_bwd(q, static_cast<hipStream_t>(stream)));
 }
 
+// Shape rules shared by the paged cache's entry points; fills *c.
+static uq_status check_cache(const char* fn, uq::KvCache* c, int H_kv, int d, const int32_t* pages, int64_t n_seq,
+                             int64_t max_pages, int format, int group, int64_t n_pages, int page_len,
+                             const void* k_cache, const void* v_cache, const uint16_t* k_stat,
+                             const uint16_t* v_stat) {
+  if (H_kv < 1 || H_kv > 4096) return fail(UQ_EINVAL, "%s: H_kv=%d must be in [1, 4096]", fn, H_kv);
+  if (d < 1) return fail(UQ_EINVAL, "%s: d=%d must be >= 1", fn, d);
+  if (d != 64 && d != 128) return fail(UQ_EUNSUPPORTED, "%s: d=%d, supported 64 and 128", fn, d);
+  if (format < UQ_KV_BF16 || format > UQ_KV_U4) return fail(UQ_EINVAL, "%s: bad format %d", fn, format);
+  if (format == UQ_KV_BF16 ? group != 0 : (group != 32 && group != d))
+    return fail(UQ_EINVAL, "%s: group=%d must be 0 for bf16 and 32 or d=%d for codes", fn, group, d);
+  if (page_len < 16 || page_len > 1024 || (page_len & (page_len - 1)) != 0)
+    return fail(UQ_EINVAL, "%s: page_len=%d must be a power of two in [16, 1024]", fn, page_len);
+  const int64_t lim = int64_t(1) << 31;
+  if (n_pages < 1 || n_pages >= lim) return fail(UQ_EINVAL, "%s: n_pages=%lld must be in [1, 2^31)", fn, (long long)n_pages);
+  if (n_seq < 1 || n_seq >= lim) return fail(UQ_EINVAL, "%s: n_seq=%lld must be in [1, 2^31)", fn, (long long)n_seq);
+  if (max_pages < 1 || max_pages > (lim - 1) / page_len)
+    return fail(UQ_EINVAL, "%s: max_pages=%lld must be >= 1 and max_pages * page_len < 2^31", fn, (long long)max_pages);
+  REQ_PTR(pages, 4); REQ_PTR(k_cache, 16); REQ_PTR(v_cache, 16);
+  if (format != UQ_KV_BF16) {
+    REQ_PTR(k_stat, 16); REQ_PTR(v_stat, 16);
+  } else if (k_stat != nullptr || v_stat != nullptr) {
+    return fail(UQ_EINVAL, "%s: k_stat and v_stat must be NULL for bf16", fn);
+  }
+  *c = uq::KvCache{format, group, n_pages, page_len, __builtin_ctz(unsigned(page_len)), H_kv, d,
+                   const_cast<void*>(k_cache), const_cast<void*>(v_cache), const_cast<uint16_t*>(k_stat),
+                   const_cast<uint16_t*>(v_stat), pages, n_seq, max_pages};
+  return UQ_OK;
+}
+
+// Row distance ld (0: cols) of rows of cols elements, a multiple of step.
+static uq_status check_ld(const char* fn, const char* name, int64_t* ld, int64_t cols, int step) {
+  if (*ld == 0) *ld = cols;
+  if (*ld < cols || *ld % step != 0 || *ld >= int64_t(1) << 31)
+    return fail(UQ_EINVAL, "%s: %s=%lld must be 0 or a multiple of %d in [%lld, 2^31)", fn, name, (long long)*ld, step,
+                (long long)cols);
+  return UQ_OK;
+}
+
+static uq_status check_heads(const char* fn, int H, int H_kv) {
+  if (H < 1 || H > 65535 || H % H_kv != 0)
+    return fail(UQ_EINVAL, "%s: H=%d must be a positive multiple of H_kv=%d, at most 65535", fn, H, H_kv);
+  return UQ_OK;
+}
+
+uq_status uniquan_kv_append(int64_t T, int H, int H_kv, int d, const void* q, int64_t ld_q, const void* k, int64_t ld_k,
+                            const void* v, int64_t ld_v, int in_dtype, const int32_t* seq, const int32_t* pos,
+                            const float* cs, int64_t n_cs, const int32_t* pages, int64_t n_seq, int64_t max_pages,
+                            int format, int group, int64_t n_pages, int page_len, void* k_cache, void* v_cache,
+                            uint16_t* k_stat, uint16_t* v_stat, uint16_t* q_out, void* stream) {
+  const char* fn = "uniquan_kv_append";
+  uq::KvAppendLaunch p{};
+  if (uq_status st = check_cache(fn, &p.c, H_kv, d, pages, n_seq, max_pages, format, group, n_pages, page_len, k_cache,
+                                 v_cache, k_stat, v_stat))
+    return st;
+  if (uq_status st = check_heads(fn, H, H_kv)) return st;
+  if (T < 0 || T >= int64_t(1) << 31) return fail(UQ_EINVAL, "%s: T=%lld must be in [0, 2^31)", fn, (long long)T);
+  if (!is_dtype(in_dtype)) return fail(UQ_EINVAL, "%s: bad dtype", fn);
+  if ((q == nullptr) != (q_out == nullptr)) return fail(UQ_EINVAL, "%s: q and q_out must be given together", fn);
+  if (q == nullptr && H != H_kv) return fail(UQ_EINVAL, "%s: H=%d must be H_kv=%d without q", fn, H, H_kv);
+  if (cs != nullptr && n_cs < 1) return fail(UQ_EINVAL, "%s: n_cs=%lld must be >= 1", fn, (long long)n_cs);
+  if (uq_status st = check_ld(fn, "ld_q", &ld_q, int64_t(H) * d, 8)) return st;
+  if (uq_status st = check_ld(fn, "ld_k", &ld_k, int64_t(H_kv) * d, 8)) return st;
+  if (uq_status st = check_ld(fn, "ld_v", &ld_v, int64_t(H_kv) * d, 8)) return st;
+  if (T > (int64_t(1) << 28) / (int64_t(H) + 2 * H_kv)) return fail(UQ_EUNSUPPORTED, "%s: T (H + 2 H_kv) > 2^28", fn);
+  if (T == 0) return UQ_OK;
+  OPT_PTR(q, 16); REQ_PTR(k, 16); REQ_PTR(v, 16); OPT_PTR(seq, 4); REQ_PTR(pos, 4); OPT_PTR(cs, 16); OPT_PTR(q_out, 16);
+  p.T = T; p.H = H;
+  p.q = q; p.k = k; p.v = v;
+  p.ld_q = ld_q; p.ld_k = ld_k; p.ld_v = ld_v;
+  p.in_dtype = in_dtype;
+  p.seq = seq; p.pos = pos; p.cs = cs; p.n_cs = n_cs;
+  p.q_out = q_out;
+  return hip_status(fn, uq::launch_kv_append(p, static_cast<hipStream_t>(stream)));
+}
+
+uq_status uniquan_kv_read(int64_t n_seq, int H_kv, int d, int64_t L, const int32_t* start, const int32_t* lens,
+                          const int32_t* pages, int64_t max_pages, int format, int group, int64_t n_pages, int page_len,
+                          const void* k_cache, const void* v_cache, const uint16_t* k_stat, const uint16_t* v_stat,
+                          void* K, void* V, int out_dtype, void* stream) {
+  const char* fn = "uniquan_kv_read";
+  uq::KvReadLaunch p{};
+  if (uq_status st = check_cache(fn, &p.c, H_kv, d, pages, n_seq, max_pages, format, group, n_pages, page_len, k_cache,
+                                 v_cache, k_stat, v_stat))
+    return st;
+  if (L < 1 || L >= int64_t(1) << 31) return fail(UQ_EINVAL, "%s: L=%lld must be in [1, 2^31)", fn, (long long)L);
+  if (n_seq > (int64_t(1) << 28) / L / H_kv) return fail(UQ_EUNSUPPORTED, "%s: n_seq H_kv L > 2^28", fn);
+  if (!is_dtype(out_dtype)) return fail(UQ_EINVAL, "%s: bad dtype", fn);
+  REQ_PTR(lens, 4); OPT_PTR(start, 4); OPT_PTR(K, 16); OPT_PTR(V, 16);
+  p.L = L; p.start = start; p.lens = lens;
+  p.K = K; p.V = V; p.out_dtype = out_dtype;
+  if (K == nullptr && V == nullptr) return UQ_OK;
+  return hip_status(fn, uq::launch_kv_read(p, static_cast<hipStream_t>(stream)));
+}
+
+size_t uniquan_attn_decode_ws(int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len) {
+  if (n_seq < 1 || H_kv < 1 || H < H_kv || d < 1 || max_pages < 1 || page_len < 1) return 0;
+  return uq::attn_decode_ws(n_seq, H, H_kv, d, max_pages, page_len);
+}
+
+uq_status uniquan_attn_decode(int64_t n_seq, int H, int H_kv, int d, const uint16_t* Q, int64_t ld_q,
+                              const int32_t* lens, const int32_t* pages, int64_t max_pages, int format, int group,
+                              int64_t n_pages, int page_len, const void* k_cache, const void* v_cache,
+                              const uint16_t* k_stat, const uint16_t* v_stat, float scale, uint16_t* O, int64_t ld_o,
+                              float* row_lse, float* ws, size_t ws_len, void* stream) {
+  const char* fn = "uniquan_attn_decode";
+  uq::AttnDecodeLaunch p{};
+  if (uq_status st = check_cache(fn, &p.c, H_kv, d, pages, n_seq, max_pages, format, group, n_pages, page_len, k_cache,
+                                 v_cache, k_stat, v_stat))
+    return st;
+  if (uq_status st = check_heads(fn, H, H_kv)) return st;
+  if (n_seq > (int64_t(1) << 24) / H) return fail(UQ_EUNSUPPORTED, "%s: n_seq * H > 2^24", fn);
+  if (uq_status st = check_ld(fn, "ld_q", &ld_q, int64_t(H) * d, 8)) return st;
+  if (uq_status st = check_ld(fn, "ld_o", &ld_o, int64_t(H) * d, 4)) return st;
+  REQ_PTR(Q, 16); REQ_PTR(lens, 4); REQ_PTR(O, 8); OPT_PTR(row_lse, 4);
+  const size_t need = uniquan_attn_decode_ws(n_seq, H, H_kv, d, max_pages, page_len);
+  if (ws_len < need) return fail(UQ_EINVAL, "%s: ws_len=%zu < %zu", fn, ws_len, need);
+  if (need > 0) REQ_PTR(ws, 16);
+  p.H = H; p.Q = Q; p.ld_q = ld_q; p.lens = lens; p.scale = scale;
+  p.O = O; p.ld_o = ld_o; p.lse = row_lse; p.ws = ws;
+  return hip_status(fn, uq::launch_attn_decode(p, static_cast<hipStream_t>(stream)));
+}
+
 double uniquan_probe_mfma_flops(int iters) {
   return 2.0 * 32 * 32 * 16 * double(uq::PROBE_MFMA_CHAINS) * double(iters) * (4.0 * uq::PROBE_MFMA_BLOCKS);
 }

@@ -194,6 +194,51 @@ struct AttnLaunch {
 hipError_t launch_attn_fwd(const AttnLaunch& p, hipStream_t st);
 hipError_t launch_attn_bwd(const AttnLaunch& p, hipStream_t st);
 
+// Paged key/value cache (kv_cache.hip) and the attention of one new token
+// over it (attn_decode.hip); layout in uniquan.h.
+enum KvFormat : int { KV_BF16 = 0, KV_U8 = 1, KV_U4 = 2 };
+struct KvCache {
+  int format, group;
+  int64_t n_pages;
+  int page_len, log_page, H_kv, d;
+  void* k; void* v;
+  uint16_t* k_stat; uint16_t* v_stat;
+  const int32_t* pages;  // [n_seq, max_pages]
+  int64_t n_seq, max_pages;
+};
+struct KvAppendLaunch {
+  KvCache c;
+  int64_t T;
+  int H;
+  const void* q; const void* k; const void* v;
+  int64_t ld_q, ld_k, ld_v;
+  int in_dtype;
+  const int32_t* seq; const int32_t* pos;
+  const float* cs; int64_t n_cs;
+  uint16_t* q_out;
+};
+struct KvReadLaunch {
+  KvCache c;
+  int64_t L;
+  const int32_t* start; const int32_t* lens;
+  void* K; void* V;
+  int out_dtype;
+};
+struct AttnDecodeLaunch {
+  KvCache c;
+  int H;
+  const uint16_t* Q; int64_t ld_q;
+  const int32_t* lens;
+  float scale;
+  uint16_t* O; int64_t ld_o;
+  float* lse;
+  float* ws;
+};
+hipError_t launch_kv_append(const KvAppendLaunch& p, hipStream_t st);
+hipError_t launch_kv_read(const KvReadLaunch& p, hipStream_t st);
+hipError_t launch_attn_decode(const AttnDecodeLaunch& p, hipStream_t st);
+size_t attn_decode_ws(int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len);
+
 // Deployment form (bit-planes + binary16 Theta*_B) and its product.
 struct BcqPackLaunch {
   int64_t R, C;

@@ -22,6 +22,7 @@ HEADER = os.path.join(os.path.dirname(HERE), "include", "uniquan.h")
 UQ_OK, UQ_EINVAL, UQ_EUNSUPPORTED, UQ_EHIP = 0, 1, 2, 3
 UQ_F32, UQ_BF16 = 0, 1
 MAP_FULL, MAP_LOCAL, MAP_FROZEN = 0, 1, 2
+KV_BF16, KV_U8, KV_U4 = 0, 1, 2
 
 _STATUS = {UQ_EINVAL: "EINVAL", UQ_EUNSUPPORTED: "EUNSUPPORTED", UQ_EHIP: "EHIP"}
 
@@ -86,6 +87,13 @@ _SIGS = {
     "uniquan_attn_fwd": ([_i64, _i64, _i32, _i32, _vp, _vp, _vp, _f32, _vp, _vp, _i32, _i32, _vp], _i32),
     "uniquan_attn_bwd": ([_i64, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _f32, _vp, _vp, _vp, _vp, _i32, _i32,
                           _vp, _vp], _i32),
+    "uniquan_kv_append": ([_i64, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _vp, _vp, _i64, _vp, _i64,
+                           _i64, _i32, _i32, _i64, _i32, _vp, _vp, _vp, _vp, _vp, _vp], _i32),
+    "uniquan_kv_read": ([_i64, _i32, _i32, _i64, _vp, _vp, _vp, _i64, _i32, _i32, _i64, _i32, _vp, _vp, _vp, _vp, _vp,
+                         _vp, _i32, _vp], _i32),
+    "uniquan_attn_decode_ws": ([_i64, _i32, _i32, _i32, _i64, _i32], ctypes.c_size_t),
+    "uniquan_attn_decode": ([_i64, _i32, _i32, _i32, _vp, _i64, _vp, _vp, _i64, _i32, _i32, _i64, _i32, _vp, _vp, _vp,
+                             _vp, _f32, _vp, _i64, _vp, _vp, ctypes.c_size_t, _vp], _i32),
     "uniquan_probe_mfma_flops": ([_i32], ctypes.c_double),
     "uniquan_probe_stream": ([_i32, _i64, _vp, _vp, _vp, _i32, _vp], _i32),
     "uniquan_probe_mfma": ([_i32, _vp, _vp], _i32),
@@ -271,6 +279,7 @@ _B = (torch.bfloat16,)
 _U8 = (torch.uint8,)
 _H = (torch.float16,)
 _U32 = (torch.int32, torch.uint32)  # bit-plane words (bits only)
+_I32 = (torch.int32,)
 
 
 def uniquan_fq_fwd(R, C, k, g, W, s, s_r, delta, z_u, alpha, z_b, mode, codes, W_hat, stream=None):
@@ -608,6 +617,111 @@ def uniquan_attn_bwd(batch, kv_batch, L, d, Q, K, V, O, dO, row_lse, scale, delt
                                   _p(delta, nr, _F, "delta"), _p(dQ, nq, tq, "dQ"), _p(dK, nq, tkv, "dK"),
                                   _p(dV, nq, tkv, "dV"), int(tok_seqs), int(group),
                                   _p(cs, L * d, _F, "cs") if tok_seqs else None, _stream(stream)))
+
+
+def _one_device(*tensors):
+    """Raise unless every tensor given lies on the current device (whose streams the calls run on)."""
+    here = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != here:
+            raise ValueError(f"tensor on {t.device}, the current device is cuda:{here}")
+
+
+def _ld(t, rows, cols, dtypes, name):
+    """Device pointer and row distance of [rows, cols] values: a contiguous tensor of that many, or a
+    [rows, cols] view whose rows lie apart (a column slice)."""
+    if t is None:
+        return None, 0
+    if isinstance(t, torch.Tensor) and tuple(t.shape) == (rows, cols) and t.stride(1) == 1 and rows > 1:
+        if not t.is_cuda:
+            raise ValueError(f"{name} must be a device tensor")
+        if t.dtype not in dtypes:
+            raise TypeError(f"{name} has dtype {t.dtype}, expected one of {dtypes}")
+        if t.stride(0) < cols:
+            raise ValueError(f"{name} has rows {t.stride(0)} elements apart, needs {cols}")
+        return t.data_ptr(), t.stride(0)
+    if isinstance(t, torch.Tensor) and rows == 1 and tuple(t.shape) == (1, cols):
+        t = t[0]
+    return _p(t, rows * cols, dtypes, name), 0
+
+
+def _kv(Hkv, d, page_len, table, k_cache, v_cache, k_stat, v_stat, fmt, group):
+    """The cache's pointers and sizes, checked: (pages, n_seq, max_pages), (format, group, n_pages, page_len),
+    (k_cache, v_cache, k_stat, v_stat)."""
+    if fmt not in (KV_BF16, KV_U8, KV_U4):
+        raise ValueError(f"fmt must be KV_BF16, KV_U8 or KV_U4, not {fmt!r}")
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise ValueError("table must be a [n_seq, max_pages] tensor")
+    row = d // 2 if fmt == KV_U4 else d
+    if min(Hkv, d, page_len) < 1 or row < 1:
+        raise ValueError(f"bad cache sizes Hkv={Hkv}, d={d}, page_len={page_len}")
+    page = Hkv * page_len * row
+    n_pages = k_cache.numel() // page if isinstance(k_cache, torch.Tensor) else 0
+    dt = _B if fmt == KV_BF16 else _U8
+    stats = None
+    if fmt != KV_BF16 and group > 0:
+        stats = n_pages * Hkv * page_len * 2 * (d // group)
+        if k_stat is None or v_stat is None:
+            raise ValueError("k_stat and v_stat must be given for a cache of codes")
+    return ((_p(table, None, _I32, "table"), table.shape[0], table.shape[1]),
+            (int(fmt), int(group), n_pages, int(page_len)),
+            (_p(k_cache, max(1, n_pages) * page, dt, "k_cache"), _p(v_cache, max(1, n_pages) * page, dt, "v_cache"),
+             _p(k_stat, stats, _B, "k_stat"), _p(v_stat, stats, _B, "v_stat")))
+
+
+def uniquan_kv_append(T, H, Hkv, d, q, k, v, pos, table, k_cache, v_cache, q_out=None, seq=None, cs=None, fmt=KV_BF16,
+                      group=0, page_len=64, k_stat=None, v_stat=None, stream=None):
+    """Rows q [T, H d], k, v [T, Hkv d] (fp32 or bf16; column slices allowed) at positions pos [T] of sequences
+    seq [T] (None: row t of sequence t): q and k rotated by cs [n, d/2, 2] (None: not), q to q_out bf16, k and v
+    into the paged cache (see the header).  q may be None (H = Hkv then)."""
+    if not isinstance(k, torch.Tensor) or not isinstance(v, torch.Tensor):
+        raise TypeError("k and v must be torch.Tensors")
+    _one_device(q, k, v, pos, table, k_cache, v_cache, q_out, seq, cs, k_stat, v_stat)
+    (pg, n_seq, mp), f, m = _kv(Hkv, d, page_len, table, k_cache, v_cache, k_stat, v_stat, fmt, group)
+    pk, ld_k = _ld(k, T, Hkv * d, _W, "k")
+    pv, ld_v = _ld(v, T, Hkv * d, (k.dtype,), "v")
+    pq, ld_q = _ld(q, T, H * d, (k.dtype,), "q")
+    _check(lib().uniquan_kv_append(
+        T, H, Hkv, d, pq, ld_q, pk, ld_k, pv, ld_v, _dt(k), _p(seq, T, _I32, "seq"), _p(pos, T, _I32, "pos"),
+        _p(cs, None, _F, "cs"), 0 if cs is None else cs.numel() // d, pg, n_seq, mp, *f, *m,
+        _p(q_out, T * H * d, _B, "q_out"), _stream(stream)))
+
+
+def uniquan_kv_read(n_seq, Hkv, d, L, lens, table, k_cache, v_cache, K, V, start=None, fmt=KV_BF16, group=0,
+                    page_len=64, k_stat=None, v_stat=None, stream=None):
+    """K, V [Hkv, n_seq, L, d] (fp32 or bf16; either may be None): positions start[s] .. + L of every sequence,
+    0 where they hold nothing."""
+    _one_device(lens, table, k_cache, v_cache, K, V, start, k_stat, v_stat)
+    (pg, ns, mp), f, m = _kv(Hkv, d, page_len, table, k_cache, v_cache, k_stat, v_stat, fmt, group)
+    if ns != n_seq:
+        raise ValueError(f"table has {ns} rows, n_seq is {n_seq}")
+    n = Hkv * n_seq * L * d
+    one = K if K is not None else V
+    dt = _W if one is None else (one.dtype,)
+    _check(lib().uniquan_kv_read(
+        n_seq, Hkv, d, L, _p(start, n_seq, _I32, "start"), _p(lens, n_seq, _I32, "lens"), pg, mp, *f, *m,
+        _p(K, n, dt, "K"), _p(V, n, dt, "V"), UQ_BF16 if one is None else _dt(one), _stream(stream)))
+
+
+def uniquan_attn_decode_ws(n_seq, H, Hkv, d, max_pages, page_len) -> int:
+    return int(lib().uniquan_attn_decode_ws(n_seq, H, Hkv, d, max_pages, page_len))
+
+
+def uniquan_attn_decode(n_seq, H, Hkv, d, Q, lens, table, k_cache, v_cache, scale, O, row_lse=None, ws=None,
+                        fmt=KV_BF16, group=0, page_len=64, k_stat=None, v_stat=None, stream=None):
+    """O [n_seq, H d] (bf16; a column slice allowed) and row_lse [n_seq, H]: attention of the query rows
+    Q [n_seq, H d] (bf16; a column slice allowed) over positions [0, lens[s]) of the paged cache.  ws: fp32
+    workspace of uniquan_attn_decode_ws floats."""
+    _one_device(Q, lens, table, k_cache, v_cache, O, row_lse, ws, k_stat, v_stat)
+    (pg, ns, mp), f, m = _kv(Hkv, d, page_len, table, k_cache, v_cache, k_stat, v_stat, fmt, group)
+    if ns != n_seq:
+        raise ValueError(f"table has {ns} rows, n_seq is {n_seq}")
+    pq, ld_q = _ld(Q, n_seq, H * d, _B, "Q")
+    po, ld_o = _ld(O, n_seq, H * d, _B, "O")
+    _check(lib().uniquan_attn_decode(
+        n_seq, H, Hkv, d, pq, ld_q, _p(lens, n_seq, _I32, "lens"), pg, mp, *f, *m, float(scale), po, ld_o,
+        _p(row_lse, n_seq * H, _F, "row_lse"), _p(ws, None, _F, "ws"), 0 if ws is None else ws.numel(),
+        _stream(stream)))
 
 
 def uniquan_transpose_bf16_batched(batch, R, C, x, out, stream=None):
