@@ -836,7 +836,8 @@ uq_status uniquan_kv_read(int64_t n_seq, int H_kv, int d, int64_t L,
  * row_lse [n_seq x H] fp32.  ws [ws_len] fp32 workspace of at least
  * uniquan_attn_decode_ws(n_seq, H, H_kv, d, max_pages, page_len) floats
  * (16-byte aligned; 0: may be NULL), free to be reused once the call is done;
- * calls that overlap need one each.  n_seq H <= 2^24.
+ * calls that overlap need one each.  n_seq H <= 2^24, n_seq (max_pages page_len
+ * + 256) <= 2^37.
  */
 size_t uniquan_attn_decode_ws(int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len);
 uq_status uniquan_attn_decode(int64_t n_seq, int H, int H_kv, int d,

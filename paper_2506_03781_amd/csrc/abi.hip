@@ -871,6 +871,8 @@ uq_status uniquan_attn_decode(int64_t n_seq, int H, int H_kv, int d, const uint1
     return st;
   if (uq_status st = check_heads(fn, H, H_kv)) return st;
   if (n_seq > (int64_t(1) << 24) / H) return fail(UQ_EUNSUPPORTED, "%s: n_seq * H > 2^24", fn);
+  if (n_seq > (int64_t(1) << 37) / (max_pages * page_len + 256))
+    return fail(UQ_EUNSUPPORTED, "%s: n_seq max_pages page_len > 2^37", fn);
   if (uq_status st = check_ld(fn, "ld_q", &ld_q, int64_t(H) * d, 8)) return st;
   if (uq_status st = check_ld(fn, "ld_o", &ld_o, int64_t(H) * d, 4)) return st;
   REQ_PTR(Q, 16); REQ_PTR(lens, 4); REQ_PTR(O, 8); OPT_PTR(row_lse, 4);

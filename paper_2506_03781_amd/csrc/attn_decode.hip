@@ -1,13 +1,15 @@
 // Attention of one new token per sequence over the paged key/value cache
 // (uniquan_attn_decode); layout, formulas and errors in uniquan.h.
 //
-// Split.  A workgroup of four wavefronts takes one sequence, one key/value
-// head, up to HEADS of its query heads and one chunk of the positions; its
-// wavefronts take steps of 32 positions in turn, each with a running maximum
-// and sum, and are joined in LDS.  The chunk length follows from all lengths
-// (plan_slot): as many chunks as fill the GPU, of equal size within a
-// sequence.  A sequence of one chunk is finished here, the others' chunks are
-// joined by attn_join_kernel.
+// Split.  A workgroup of four wavefronts takes one key/value head, up to 16 of
+// its query heads and an equal share of all sequences' positions, as many
+// workgroups as the GPU holds at once: positions count in blocks of 128 (each
+// wavefront a step of 32), and every sequence costs a block more, its end.  A
+// share is a run of blocks over one or several sequences (Share); its part of
+// one sequence is a chunk.  The wavefronts' steps of a chunk, each with a
+// running maximum and sum, are joined in LDS; a sequence that lies in one
+// share is finished there, the chunks of the others are joined by
+// attn_join_kernel.
 //
 // One step, v_mfma_f32_16x16x32_bf16 (C[m][n] += A[m][k] B[k][n]; lane l
 // supplies row l % 16 of A and column l % 16 of B at k = 8 (l / 16) .. + 8 and
@@ -38,6 +40,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "uq_device.h"
 #include "uq_kv.h"
@@ -57,9 +60,9 @@ constexpr float LOWEST = -3.402823466e38f;  // the running maximum before any po
 constexpr float SLACK = 8.0f;               // scores may exceed the reference by this (weights up to 2^8)
 constexpr int WAVES = 4;
 constexpr int STEP = 32;                    // positions of a wavefront's step
-constexpr int MIN_STEPS = 8;                // steps of the shortest chunk
-constexpr int TARGET = 1024;                // workgroups that a split aims at
-constexpr int MAX_SPLIT_SEQ = 4096;         // sequences up to which chunks are laid out
+constexpr int BLOCK = WAVES * STEP;         // positions of a workgroup's round
+constexpr int MIN_COST = 3;                 // least blocks of a share (ends counted)
+constexpr int CUS = 256;
 
 __device__ __forceinline__ f32x4d mfma16(const u32x4d& a, const u32x4d& b, const f32x4d& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8d, a), __builtin_bit_cast(bf16x8d, b), c, 0,
@@ -74,103 +77,105 @@ __device__ __forceinline__ uint32_t low_halves(uint32_t a, uint32_t b) {
   return __builtin_amdgcn_perm(b, a, 0x05040100u);
 }
 
-// Over the four lanes l % 16 + 16 k, in every one of them.
+// Over the four lanes l % 16 + 16 k, in every one of them: a swap of rows (of
+// halves) of x with itself leaves each row (half) beside its partner's copy.
+template <typename Op>
+__device__ __forceinline__ float over4(float x, Op op) {
+  const uint32_t u = __float_as_uint(x);
+  const auto a = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  const uint32_t v = __float_as_uint(op(__uint_as_float(a[0]), __uint_as_float(a[1])));
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return op(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
 __device__ __forceinline__ float max4(float x) {
-  x = fmaxf(x, __shfl_xor(x, 16));
-  return fmaxf(x, __shfl_xor(x, 32));
+  return over4(x, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ __forceinline__ float sum4(float x) {
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
+  return over4(x, [](float a, float b) { return a + b; });
+}
+
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Inclusive sums over the wavefront's lanes.
+template <typename T>
+__device__ __forceinline__ T wave_scan(T x) {
+  static_assert(sizeof(T) == 4, "");
+  auto add = [](T a, int moved) { return a + __builtin_bit_cast(T, moved); };
+  x = add(x, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x111, 0xF, 0xF, false));  // row_shr:1
+  x = add(x, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x112, 0xF, 0xF, false));
+  x = add(x, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x114, 0xF, 0xF, false));
+  x = add(x, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x118, 0xF, 0xF, false));
+  x = add(x, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x142, 0xA, 0xF, false));  // row_bcast:15
+  x = add(x, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x143, 0xC, 0xF, false));  // row_bcast:31
+  return x;
 }
 
 // ---------------------------------------------------------------------------
-// which chunk a workgroup takes
+// which positions a workgroup takes
 // ---------------------------------------------------------------------------
-struct Slot {
-  int64_t s;      // sequence, or -1: none
-  int chunk, n;   // its chunk and their number
-  int64_t first;  // slot of the sequence's first chunk
-  int len;
-};
-
 __device__ __forceinline__ int capped_len(const AttnDecodeLaunch& p, int64_t s) {
   const int64_t cap = p.c.max_pages << p.c.log_page;
   const int len = p.lens[s];
   return len < 0 ? 0 : int(len < cap ? len : cap);
 }
 
-__device__ __forceinline__ int64_t wave_sum64(int64_t x) {
-  for (int m = 1; m < 64; m <<= 1) x += __shfl_xor(x, m);
-  return x;
-}
-__device__ __forceinline__ int64_t wave_scan64(int64_t x, int lane) {
-  for (int m = 1; m < 64; m <<= 1) {
-    const int64_t y = __shfl_up(x, m);
-    if (lane >= m) x += y;
+__device__ __forceinline__ int blocks_of(int len) { return (len + BLOCK - 1) / BLOCK; }
+
+// Share `at` of `want`: [a, b) of the sequences' costs laid end to end, from
+// sequence s on, whose cost begins at `begin`.
+struct Share {
+  int a, b;
+  int s, begin;
+};
+
+// Every wavefront works it out by itself: its lanes add up runs of the
+// sequences, then the run that holds `a` is searched.  With little in all,
+// only the first shares get something, MIN_COST at least.
+__device__ __forceinline__ Share share_of(const AttnDecodeLaunch& p, int at, int want) {
+  const int lane = threadIdx.x & 63;
+  const int n = int(p.c.n_seq);
+  const int per = (n + 63) / 64;
+  auto cost = [&](int j) { return j < n ? blocks_of(capped_len(p, j)) + 1 : 0; };
+  int mine = 0;
+  for (int j = lane * per; j < lane * per + per; ++j) mine += cost(j);
+  int upto = wave_scan(mine);
+  const int total = __builtin_amdgcn_readlane(upto, 63);
+  const int parts = std::min(want, std::max(1, total / MIN_COST));
+  if (at >= parts) return Share{0, 0, 0, 0};
+  const int q = total / parts, r = total % parts;
+  Share h;
+  h.a = at * q + at * r / parts;
+  h.b = (at + 1) * q + (at + 1) * r / parts;
+  int in = __builtin_ctzll(__ballot(upto > h.a));
+  int before = __builtin_amdgcn_readlane(upto - mine, in);
+  int first = in * per;
+  if (per > 1) {
+    for (const int end = first + per;; first += 64) {
+      mine = first + lane < end ? cost(first + lane) : 0;
+      upto = wave_scan(mine) + before;
+      const uint64_t past = __ballot(upto > h.a);
+      if (past) {
+        in = __builtin_ctzll(past);
+        break;
+      }
+      before = __builtin_amdgcn_readlane(upto, 63);
+    }
+    before = __builtin_amdgcn_readlane(upto - mine, in);
+    first += in;
+  } else {
+    first = in;
   }
-  return x;
+  h.s = first;
+  h.begin = before;
+  return h;
 }
 
-// Slot `at` (or, by_seq, the slots of sequence `at`) of the chunks laid out in
-// the sequences' order.  With all lengths in steps of 32 and their sum T, a
-// chunk has at most c = max(MIN_STEPS, ceil(T / want)) steps, so there are at
-// most want + n_seq of them; a sequence has ceil(steps / c), one at least.
-// Every wavefront works it out by itself: the lanes take runs of the sequences.
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int64_t uniform(int64_t x) {
-  return int64_t(uint64_t(uint32_t(uniform(int(uint32_t(x))))) | uint64_t(uint32_t(uniform(int(x >> 32)))) << 32);
-}
-__device__ Slot plan_slot(const AttnDecodeLaunch& p, int64_t at, bool by_seq, int want) {
-  const int lane = threadIdx.x & 63;
-  const int64_t n = p.c.n_seq;
-  Slot r{-1, 0, 1, at, 0};
-  if (want == 0) {  // not split: slot and sequence are one
-    if (at < n) {
-      r.s = at;
-      r.len = capped_len(p, at);
-    }
-    return r;
-  }
-  const int64_t per = (n + 63) / 64;
-  int64_t total = 0;
-  for (int64_t j = lane * per; j < lane * per + per && j < n; ++j) total += (capped_len(p, j) + STEP - 1) / STEP;
-  total = wave_sum64(total);
-  const int64_t c = std::max<int64_t>(MIN_STEPS, (total + want - 1) / want);
-  auto chunks = [&](int64_t j) -> int64_t {
-    if (j >= n) return 0;
-    const int64_t k = ((capped_len(p, j) + STEP - 1) / STEP + c - 1) / c;
-    return k > 1 ? k : 1;
-  };
-  int64_t mine = 0;
-  for (int64_t j = lane * per; j < lane * per + per && j < n; ++j) mine += chunks(j);
-  int64_t upto = wave_scan64(mine, lane);
-  int64_t run, before;  // the run of sequences that holds it, and the slots before the run
-  if (by_seq) {
-    run = at / per;
-  } else {
-    const uint64_t past = __ballot(upto > at);
-    if (past == 0) return r;
-    run = __builtin_ctzll(past);
-  }
-  before = __shfl(upto - mine, int(run));
-  const int64_t j = run * per + lane;
-  mine = lane < per ? chunks(j) : 0;
-  upto = wave_scan64(mine, lane) + before;
-  int in;
-  if (by_seq) {
-    in = int(at - run * per);
-  } else {
-    const uint64_t past = __ballot(upto > at);
-    in = __builtin_ctzll(past);
-  }
-  r.s = uniform(run * per + in);
-  r.n = uniform(int(__shfl(mine, in)));
-  r.first = uniform(int64_t(__shfl(upto - mine, in)));
-  r.chunk = by_seq ? 0 : int(at - r.first);
-  r.len = uniform(capped_len(p, r.s));
-  return r;
-}
+// The workspace: the first and the last share of each sequence, then the
+// chunks, that of share i and sequence s at i + s (no two alike: from one chunk
+// to the next either grows), H rows each of (maximum, sum, -, -, D values)
+// against that maximum.
+__device__ __forceinline__ int2* shares_of(const AttnDecodeLaunch& p) { return reinterpret_cast<int2*>(p.ws); }
+__device__ __forceinline__ float* chunks_of(const AttnDecodeLaunch& p) { return p.ws + (p.c.n_seq * 2 + 3) / 4 * 4; }
 
 // ---------------------------------------------------------------------------
 // one chunk
@@ -266,29 +271,78 @@ __device__ __forceinline__ uint32_t value_pair(const uint32_t (&a)[Form<FMT, D>:
   }
 }
 
+// f(0) .. f(3), the argument a constant.
+template <typename F>
+__device__ __forceinline__ void each4(F f) {
+  f(std::integral_constant<int, 0>{});
+  f(std::integral_constant<int, 1>{});
+  f(std::integral_constant<int, 2>{});
+  f(std::integral_constant<int, 3>{});
+}
+
+// x of lane L of the lane's 16, which the using instruction takes as it reads it.
+template <int L>
+__device__ __forceinline__ float of16(float x) {
+  return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x150 + L, 0xF, 0xF, true));  // row_newbcast
+}
+
+// The statistics' part x of position 4 grp + I of tile t, group e (constants
+// once unrolled): 16 lanes hold 16 different words instead of 16 copies.
+template <int NG, int I>
+__device__ __forceinline__ float of_lane(float x, int t, int e) {
+  switch (NG == 1 ? t : e) {
+    case 0: return of16<I>(x);
+    case 1: return of16<4 + I>(x);
+    case 2: return of16<8 + I>(x);
+    default: return of16<12 + I>(x);
+  }
+}
+
+// Workgroups a CU holds (their registers are bounded to that).
+template <int FMT, int D, int NG>
+constexpr int kResident = D == 64 ? 4 : FMT == KV_BF16 ? 2 : 3;
+
 // WIDE: 16 query heads a workgroup, else 8 with the weights' rests in the upper columns.
 template <int FMT, int D, int NG, bool WIDE>
-__global__ __launch_bounds__(256) void attn_decode_kernel(AttnDecodeLaunch p, int want, int rtiles) {
+__global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kernel(AttnDecodeLaunch p, int want, int rtiles) {
   using F = Form<FMT, D>;
   constexpr int HEADS = WIDE ? 16 : 8;
   constexpr bool CODES = FMT != KV_BF16;
   constexpr int NGA = CODES ? NG : 1;
   constexpr float MID = FMT == KV_U8 ? 128.0f : 8.0f;
+  constexpr int SW = NGA == 1 ? 1 : 2;  // words of statistics a lane holds of a step's keys (values)
+  constexpr int LD = D + 4;
+  __shared__ __attribute__((aligned(16))) float so[WAVES][16][LD];
+  __shared__ float sm[WAVES][16], ss[WAVES][16];
   const KvCache& c = p.c;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int col = lane & 15, grp = lane >> 4;
   // consecutive workgroups go to the 8 XCDs in turn: the row tiles that read one head's cache 8 apart
-  const int64_t b = blockIdx.x;
-  const int64_t unit = b / (8 * rtiles) * 8 + b % 8;
+  const unsigned b = blockIdx.x;
+  const unsigned unit = b / (8 * rtiles) * 8 + b % 8;
   const int rt = int(b / 8 % rtiles);
-  const Slot sl = plan_slot(p, unit / c.H_kv, false, want);
-  if (sl.s < 0) return;
-  const int64_t s = sl.s;
-  const int g = int(unit % c.H_kv);
+  const int at = int(unit / c.H_kv), g = int(unit % c.H_kv);
+  if (at >= want) return;
+  const Share share = share_of(p, at, want);
   const int grp_heads = p.H / c.H_kv;
   const int h_in = rt * HEADS + (col & (HEADS - 1));  // head within its key/value head's group
   const bool rest = !WIDE && col >= 8;
   const uint32_t cut = rest ? 0xFFFF0000u : 0u;
+  const float cl = fabsf(p.scale) * LOG2E_D;
+
+  int end = share.begin;
+  for (int64_t s = share.s; s < c.n_seq && end < share.b; ++s) {
+  const int begin = end;
+  const int len = uniform(capped_len(p, s));
+  const int blocks = blocks_of(len);
+  end = begin + blocks + 1;
+  const int b0 = std::max(share.a - begin, 0), b1 = std::min(share.b - begin, blocks);
+  const bool opens = begin >= share.a, closes = begin + blocks <= share.b;  // the sequence starts, ends here
+  if (b0 >= b1 && !(blocks == 0 && opens)) continue;
+  if (want > 1 && g == 0 && rt == 0 && threadIdx.x == 0) {
+    if (opens) shares_of(p)[s].x = at;
+    if (closes) shares_of(p)[s].y = at;
+  }
 
   // queries, and (codes) their sums over each group of channels
   u32x4d q[F::NC];
@@ -299,6 +353,7 @@ __global__ __launch_bounds__(256) void attn_decode_kernel(AttnDecodeLaunch p, in
 #pragma unroll
     for (int k = 0; k < F::NC; ++k) {
       q[k] = h_in < grp_heads ? *reinterpret_cast<const u32x4d*>(row + 32 * k) : u32x4d{0, 0, 0, 0};
+      if (p.scale < 0.0f) q[k] ^= 0x80008000u;  // so that the scale can be taken as positive
       float t = 0.0f;
 #pragma unroll
       for (int i = 0; i < 4; ++i) t += __uint_as_float(q[k][i] << 16) + __uint_as_float(q[k][i] & 0xFFFF0000u);
@@ -316,102 +371,126 @@ __global__ __launch_bounds__(256) void attn_decode_kernel(AttnDecodeLaunch p, in
       qsum[0] = 0.0f;
     }
   }
-  const float cl = p.scale * LOG2E_D;
-
-  const int steps = (sl.len + STEP - 1) / STEP;
-  const int u0 = int(int64_t(steps) * sl.chunk / sl.n), u1 = int(int64_t(steps) * (sl.chunk + 1) / sl.n);
+  const int u1 = b1 * WAVES;
+  int u = b0 * WAVES + wave;
 
   f32x4d acc[F::NV] = {};
   float off[NGA] = {};  // sums of weight times the value of the codes' middle
   float m = LOWEST, l = 0.0f;
 
   const int32_t* pages = c.pages + s * c.max_pages;
-  const char* kc = static_cast<const char*>(c.k);
-  const char* vc = static_cast<const char*>(c.v);
-  const uint32_t* ks = reinterpret_cast<const uint32_t*>(c.k_stat);
-  const uint32_t* vs = reinterpret_cast<const uint32_t*>(c.v_stat);
+  const uint32_t page_bytes = uint32_t(c.H_kv) * uint32_t(c.page_len) * F::ROW;
+  const uint32_t page_stats = uint32_t(c.H_kv) * uint32_t(c.page_len) * NGA;
+  const uint32_t head_bytes = uint32_t(g) * uint32_t(c.page_len) * F::ROW;
+  // the lane's word of statistics: position 4 grp + col % 4 of tile col / 4 % 2 (one group), of both (several)
+  const uint32_t lane_stat = uint32_t(g) * uint32_t(c.page_len) * NGA + 4 * grp + (col & 3) +
+                             (NGA > 1 ? uint32_t(col / 4 % NGA) * uint32_t(c.page_len) : 0u);
 
-  for (int u = u0 + wave; u < u1; u += WAVES) {
-    // the step's two tiles: place in the cache and positions that take part
-    int64_t at[2];
-    int64_t sat[2];
-    int nv[2];
+  // a step's pages are looked up a step before its loads, its loads go out a step before its products
+  int page[2];
+  auto look_up = [&](int u) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int base = u * STEP + 16 * t;
-      int page = -1;
-      if (base < sl.len) page = pages[base >> c.log_page];
-      const bool is = page >= 0 && page < c.n_pages;
-      nv[t] = is ? (sl.len - base < 16 ? sl.len - base : 16) : 0;
-      const int64_t ph = int64_t(is ? page : 0) * c.H_kv + g;
-      const int place = is ? base & (c.page_len - 1) : 0;
-      at[t] = (ph * c.page_len + place) * F::ROW;
-      sat[t] = ph * NGA * c.page_len + place + 4 * grp;
+      page[t] = u < u1 && base < len ? pages[base >> c.log_page] : -1;
     }
-    if (nv[0] + nv[1] == 0) continue;
-    uint32_t kw[2][F::KW], vw[8][F::VW];
-    u32x4d kst[2][NGA], vst[2][NGA];
+  };
+  struct Step {
+    uint32_t k[2][F::KW], v[8][F::VW], kst[SW], vst[SW];
+    int nv[2];  // positions of each tile that take part
+  };
+  auto load = [&](Step& x, int u) {
+    uint64_t at[2];
+    uint64_t sat[2];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) load_key<FMT, D>(kc + at[t], lane, kw[t]);
+    for (int t = 0; t < 2; ++t) {
+      const int base = u * STEP + 16 * t;
+      const bool is = page[t] >= 0 && page[t] < c.n_pages;
+      const uint32_t pg = is ? uint32_t(page[t]) : 0u;
+      const uint32_t place = is ? uint32_t(base & (c.page_len - 1)) : 0u;
+      x.nv[t] = is ? std::min(16, len - base) : 0;
+      at[t] = uint64_t(pg) * page_bytes + head_bytes + place * F::ROW;
+      sat[t] = uint64_t(pg) * page_stats + place;
+    }
+    look_up(u + WAVES);
+    if (x.nv[0] + x.nv[1] == 0) return;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) load_key<FMT, D>(static_cast<const char*>(c.k) + at[t], lane, x.k[t]);
     if constexpr (CODES) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < NGA; ++i) {
-          kst[t][i] = *reinterpret_cast<const u32x4d*>(ks + sat[t] + i * c.page_len);
-          vst[t][i] = *reinterpret_cast<const u32x4d*>(vs + sat[t] + i * c.page_len);
-        }
+      for (int t = 0; t < SW; ++t) {
+        uint64_t o = sat[t];
+        if (SW == 1) o = col & 4 ? sat[1] : o;
+        o += lane_stat;
+        x.kst[t] = reinterpret_cast<const uint32_t*>(c.k_stat)[o];
+        x.vst[t] = reinterpret_cast<const uint32_t*>(c.v_stat)[o];
+      }
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) load_value<FMT, D>(vc + at[j / 4], 4 * grp + j % 4, lane, vw[j]);
-
+    for (int j = 0; j < 8; ++j) load_value<FMT, D>(static_cast<const char*>(c.v) + at[j / 4], 4 * grp + j % 4, lane, x.v[j]);
+  };
+  auto compute = [&](Step& y) {
+    if (y.nv[0] + y.nv[1] == 0) return;
     // scores of positions 4 grp + i of tile t
-    float x[2][4];
+    float x[8];
+    float sc[SW], lo[SW];
+    if constexpr (CODES) {
+#pragma unroll
+      for (int t = 0; t < SW; ++t) {
+        sc[t] = __uint_as_float(y.kst[t] << 16);
+        lo[t] = __uint_as_float(y.kst[t] & 0xFFFF0000u);
+      }
+    }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       if constexpr (CODES) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[t][i] = 0.0f;
+        for (int i = 0; i < 4; ++i) x[4 * t + i] = 0.0f;
 #pragma unroll
         for (int e = 0; e < NGA; ++e) {
           const float start = FMT == KV_U4 ? -128.0f * qsum[e] : 0.0f;
           f32x4d a = {start, start, start, start};
 #pragma unroll
-          for (int k = e * F::NC / NGA; k < (e + 1) * F::NC / NGA; ++k) a = mfma16(key_step<FMT, D>(kw[t], k), q[k], a);
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            x[t][i] = __builtin_fmaf(__uint_as_float(kst[t][e][i] << 16), a[i],
-                                     __builtin_fmaf(__uint_as_float(kst[t][e][i] & 0xFFFF0000u), qsum[e], x[t][i]));
+          for (int k = e * F::NC / NGA; k < (e + 1) * F::NC / NGA; ++k) a = mfma16(key_step<FMT, D>(y.k[t], k), q[k], a);
+          each4([&](auto ic) {
+            constexpr int i = decltype(ic)::value;
+            x[4 * t + i] = __builtin_fmaf(of_lane<NGA, i>(sc[SW == 1 ? 0 : t], t, e), a[i], x[4 * t + i]);
+            x[4 * t + i] = __builtin_fmaf(of_lane<NGA, i>(lo[SW == 1 ? 0 : t], t, e), qsum[e], x[4 * t + i]);
+          });
         }
       } else {
         f32x4d a = {};
 #pragma unroll
-        for (int k = 0; k < F::NC; ++k) a = mfma16(key_step<FMT, D>(kw[t], k), q[k], a);
+        for (int k = 0; k < F::NC; ++k) a = mfma16(key_step<FMT, D>(y.k[t], k), q[k], a);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[t][i] = a[i];
+        for (int i = 0; i < 4; ++i) x[4 * t + i] = a[i];
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) x[t][i] *= cl;
     }
-    if (nv[0] + nv[1] < 32) {  // positions that take no part: no weight, and nothing of theirs in the products
+    const bool tail = y.nv[0] + y.nv[1] < 32;
+    if (tail) {  // positions that take no part: no weight, and nothing of theirs in the products
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const bool in = 4 * grp + j % 4 < nv[j / 4];
-        x[j / 4][j % 4] = in ? x[j / 4][j % 4] : -__builtin_inff();
-        if constexpr (CODES) {
+        const bool in = 4 * grp + j % 4 < y.nv[j / 4];
+        x[j] = in ? x[j] : -__builtin_inff();
+        if constexpr (!CODES) {
 #pragma unroll
-          for (int e = 0; e < NGA; ++e) vst[j / 4][e][j % 4] = in ? vst[j / 4][e][j % 4] : 0u;
-        } else {
+          for (int i = 0; i < F::VW; ++i) y.v[j][i] = in ? y.v[j][i] : 0u;
+        }
+      }
+      if constexpr (CODES) {
 #pragma unroll
-          for (int i = 0; i < F::VW; ++i) vw[j][i] = in ? vw[j][i] : 0u;
+        for (int t = 0; t < SW; ++t) {
+          int nv = y.nv[t];
+          if (SW == 1) nv = col & 4 ? y.nv[1] : nv;
+          y.vst[t] = 4 * grp + (col & 3) < nv ? y.vst[t] : 0u;
         }
       }
     }
     // running maximum: the reference moves only when a score exceeds it by SLACK
-    float mx = x[0][0];
+    float mx = x[0];
 #pragma unroll
-    for (int j = 1; j < 8; ++j) mx = fmaxf(mx, x[j / 4][j % 4]);
-    mx = max4(mx);
+    for (int j = 1; j < 8; ++j) mx = fmaxf(mx, x[j]);
+    mx = max4(mx) * cl;
     if (__any(mx > m + SLACK)) {
       const float m1 = fmaxf(m, mx);
       const float f = __builtin_amdgcn_exp2f(m - m1);
@@ -426,58 +505,77 @@ __global__ __launch_bounds__(256) void attn_decode_kernel(AttnDecodeLaunch p, in
     }
     float w[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      w[j] = __builtin_amdgcn_exp2f(x[j / 4][j % 4] - m);
-      l += w[j];
+    for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], cl, -m));
+    if (tail) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = 4 * grp + j % 4 < y.nv[j / 4] ? w[j] : 0.0f;
+    }
+    l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+    if constexpr (CODES) {
+#pragma unroll
+      for (int t = 0; t < SW; ++t) {
+        sc[t] = __uint_as_float(y.vst[t] << 16);
+        lo[t] = __builtin_fmaf(sc[t], MID, __uint_as_float(y.vst[t] & 0xFFFF0000u));
+      }
     }
 #pragma unroll
     for (int e = 0; e < NGA; ++e) {
-      float y[8];
+      float z[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if constexpr (CODES) {
-          const uint32_t st = vst[j / 4][e][j % 4];
-          const float sc = __uint_as_float(st << 16);
-          y[j] = w[j] * sc;
-          off[e] = __builtin_fmaf(w[j], __builtin_fmaf(sc, MID, __uint_as_float(st & 0xFFFF0000u)), off[e]);
-        } else {
-          y[j] = w[j];
-        }
-      }
-      u32x4d hi, lo;
+      for (int t = 0; t < 2; ++t)
+        each4([&](auto ic) {
+          constexpr int i = decltype(ic)::value;
+          const float wi = w[4 * t + i];
+          if constexpr (CODES) {
+            z[4 * t + i] = of_lane<NGA, i>(sc[SW == 1 ? 0 : t], t, e) * wi;
+            off[e] = __builtin_fmaf(of_lane<NGA, i>(lo[SW == 1 ? 0 : t], t, e), wi, off[e]);
+          } else {
+            z[4 * t + i] = wi;
+          }
+        });
+      u32x4d hi, lw;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        uint32_t a = __float_as_uint(y[2 * i]), d = __float_as_uint(y[2 * i + 1]);
+        const uint32_t a = __float_as_uint(z[2 * i]), d = __float_as_uint(z[2 * i + 1]);
         if constexpr (WIDE) {
           hi[i] = top_halves(a, d);
-          lo[i] = top_halves(__float_as_uint(y[2 * i] - __uint_as_float(a & 0xFFFF0000u)),
-                             __float_as_uint(y[2 * i + 1] - __uint_as_float(d & 0xFFFF0000u)));
+          lw[i] = top_halves(__float_as_uint(z[2 * i] - __uint_as_float(a & 0xFFFF0000u)),
+                             __float_as_uint(z[2 * i + 1] - __uint_as_float(d & 0xFFFF0000u)));
         } else {
-          hi[i] = top_halves(__float_as_uint(y[2 * i] - __uint_as_float(a & cut)),
-                             __float_as_uint(y[2 * i + 1] - __uint_as_float(d & cut)));
+          hi[i] = top_halves(__float_as_uint(z[2 * i] - __uint_as_float(a & cut)),
+                             __float_as_uint(z[2 * i + 1] - __uint_as_float(d & cut)));
         }
       }
 #pragma unroll
       for (int k = e * F::NV / NGA; k < (e + 1) * F::NV / NGA; ++k) {
         u32x4d a;
         if constexpr (CODES) {
-          constexpr uint32_t z = FMT == KV_U8 ? 0xC300C300u : 0xC308C308u;  // -128; -136
-          const u32x4d mid = {z, z, z, z};
+          constexpr uint32_t mm = FMT == KV_U8 ? 0xC300C300u : 0xC308C308u;  // -128; -136
+          const u32x4d mid = {mm, mm, mm, mm};
           acc[k] = mfma16(mid, hi, acc[k]);
-          if constexpr (WIDE) acc[k] = mfma16(mid, lo, acc[k]);
+          if constexpr (WIDE) acc[k] = mfma16(mid, lw, acc[k]);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = value_pair<FMT, D>(vw[2 * i], vw[2 * i + 1], k);
+        for (int i = 0; i < 4; ++i) a[i] = value_pair<FMT, D>(y.v[2 * i], y.v[2 * i + 1], k);
         acc[k] = mfma16(a, hi, acc[k]);
-        if constexpr (WIDE) acc[k] = mfma16(a, lo, acc[k]);
+        if constexpr (WIDE) acc[k] = mfma16(a, lw, acc[k]);
       }
     }
+  };
+  Step s0, s1;
+  look_up(u);
+  if (u < u1) load(s0, u);
+  while (u < u1) {
+    if (u + WAVES < u1) load(s1, u + WAVES);
+    compute(s0);
+    u += WAVES;
+    if (u >= u1) break;
+    if (u + WAVES < u1) load(s0, u + WAVES);
+    compute(s1);
+    u += WAVES;
   }
 
   // join the wavefronts: row of column `col` in the order tile, row of the tile
-  constexpr int LD = D + 4;
-  __shared__ __attribute__((aligned(16))) float so[WAVES][16][LD];
-  __shared__ float sm[WAVES][16], ss[WAVES][16];
   l = sum4(l);
 #pragma unroll
   for (int e = 0; e < NGA; ++e) {
@@ -517,40 +615,52 @@ __global__ __launch_bounds__(256) void attn_decode_kernel(AttnDecodeLaunch p, in
       a1 += f * b1;
     }
     const int64_t head = int64_t(g) * grp_heads + hh;
-    if (sl.n == 1) {
+    if (opens && closes) {
       const float r = t == 0.0f ? 0.0f : 1.0f / t;
       *reinterpret_cast<uint32_t*>(p.O + s * p.ld_o + head * D + ch) = pack_bf16x2(a0 * r, a1 * r);
       if (ch == 0 && p.lse) p.lse[s * p.H + head] = t == 0.0f ? -__builtin_inff() : top + __builtin_amdgcn_logf(t);
     } else {
-      float* part = p.ws + ((sl.first + sl.chunk) * p.H + head) * (D + 4);
+      float* part = chunks_of(p) + ((at + s) * p.H + head) * (D + 4);
       *reinterpret_cast<float2*>(part + 4 + ch) = make_float2(a0, a1);
       if (ch == 0) *reinterpret_cast<float2*>(part) = make_float2(top, t);
     }
   }
+  __syncthreads();  // the next chunk writes LDS anew
+  }
 }
 
-// Joins the chunks of a sequence's head: D / 4 lanes a chunk, 256 / (D / 4)
-// chunks at a time.
+// Joins the chunks of a sequence's head: D / 4 lanes a chunk, PAR chunks at a
+// time, four of each in flight.
 template <int D>
-__global__ __launch_bounds__(256) void attn_join_kernel(AttnDecodeLaunch p, int want) {
-  constexpr int LANES = D / 4, PAR = 256 / LANES;
-  const int64_t s = blockIdx.x / p.H;
-  const int h = blockIdx.x % p.H;
-  const Slot sl = plan_slot(p, s, true, want);
-  if (sl.n == 1) return;
+__global__ __launch_bounds__(512) void attn_join_kernel(AttnDecodeLaunch p) {
+  constexpr int LANES = D / 4, PAR = 512 / LANES;
+  const int s = blockIdx.x / p.H, h = blockIdx.x % p.H;
+  const int2 in = shares_of(p)[s];
+  const int n = in.y - in.x + 1;
+  if (n <= 1) return;
   const int lane = threadIdx.x % LANES, row = threadIdx.x / LANES;
-  const float* base = p.ws + (sl.first * p.H + h) * (D + 4);
+  const float* base = chunks_of(p) + ((int64_t(in.x) + s) * p.H + h) * (D + 4);
   const int64_t ld = int64_t(p.H) * (D + 4);
   float m = LOWEST, t = 0.0f;
   f32x4d a = {};
-  for (int k = row; k < sl.n; k += PAR) {
-    const float2 ml = *reinterpret_cast<const float2*>(base + k * ld);
-    const f32x4d o = *reinterpret_cast<const f32x4d*>(base + k * ld + 4 + 4 * lane);
-    const float m1 = fmaxf(m, ml.x);
-    const float f0 = __builtin_amdgcn_exp2f(m - m1), f1 = __builtin_amdgcn_exp2f(ml.x - m1);
-    m = m1;
-    t = t * f0 + ml.y * f1;
-    a = a * f0 + o * f1;
+  for (int k = row; k < n; k += 4 * PAR) {
+    float2 ml[4];
+    f32x4d o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float* at = base + std::min(k + i * PAR, n - 1) * ld;
+      ml[i] = *reinterpret_cast<const float2*>(at);
+      o[i] = *reinterpret_cast<const f32x4d*>(at + 4 + 4 * lane);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (k + i * PAR >= n) break;
+      const float m1 = fmaxf(m, ml[i].x);
+      const float f0 = __builtin_amdgcn_exp2f(m - m1), f1 = __builtin_amdgcn_exp2f(ml[i].x - m1);
+      m = m1;
+      t = t * f0 + ml[i].y * f1;
+      a = a * f0 + o[i] * f1;
+    }
   }
   __shared__ f32x4d so[PAR][LANES];
   __shared__ float sm[PAR], st[PAR];
@@ -561,11 +671,12 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnDecodeLaunch p, int 
   }
   __syncthreads();
   if (row) return;
+  const int rows = std::min(PAR, n);
   float top = sm[0];
-  for (int k = 1; k < PAR; ++k) top = fmaxf(top, sm[k]);
+  for (int k = 1; k < rows; ++k) top = fmaxf(top, sm[k]);
   t = 0.0f;
   a = f32x4d{};
-  for (int k = 0; k < PAR; ++k) {
+  for (int k = 0; k < rows; ++k) {
     const float f = __builtin_amdgcn_exp2f(sm[k] - top);
     t += f * st[k];
     a += f * so[k][lane];
@@ -573,7 +684,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnDecodeLaunch p, int 
   const float r = t == 0.0f ? 0.0f : 1.0f / t;
   *reinterpret_cast<uint2*>(p.O + s * p.ld_o + int64_t(h) * D + 4 * lane) =
       make_uint2(pack_bf16x2(a[0] * r, a[1] * r), pack_bf16x2(a[2] * r, a[3] * r));
-  if (lane == 0 && p.lse) p.lse[s * p.H + h] = t == 0.0f ? -__builtin_inff() : top + __builtin_amdgcn_logf(t);
+  if (lane == 0 && p.lse) p.lse[int64_t(s) * p.H + h] = t == 0.0f ? -__builtin_inff() : top + __builtin_amdgcn_logf(t);
 }
 
 // Query heads a workgroup takes, and workgroups a key/value head's heads take.
@@ -583,52 +694,42 @@ int row_tiles(int H, int H_kv) {
   return (H / H_kv + r - 1) / r;
 }
 
-// Chunks aimed at for each key/value head's row tile (0: sequences are not
-// split), and how many there can be.
-struct Split {
-  int want;
-  int64_t slots;
-};
-Split split_of(int64_t n_seq, int H, int H_kv, int64_t max_pages, int page_len) {
-  const int64_t steps = (max_pages * page_len + STEP - 1) / STEP;
-  if (n_seq > MAX_SPLIT_SEQ || steps <= MIN_STEPS) return {0, n_seq};
-  const int64_t want = std::max<int64_t>(1, TARGET / (int64_t(H_kv) * row_tiles(H, H_kv)));
-  return {int(want), std::min(want + n_seq, n_seq * ((steps + MIN_STEPS - 1) / MIN_STEPS))};
+// Shares of each key/value head's row tile for `per` workgroups a CU; one where
+// no sequence can be longer than a block's cost, so that none is split.
+int shares(int64_t n_seq, int H, int H_kv, int64_t max_pages, int page_len, int per) {
+  const int64_t most = n_seq * ((max_pages * page_len + BLOCK - 1) / BLOCK + 1) / MIN_COST;
+  return int(std::max<int64_t>(1, std::min<int64_t>(most, per * CUS / (int64_t(H_kv) * row_tiles(H, H_kv)))));
 }
 
 template <int FMT, int D, int NG>
-void launch_form(const AttnDecodeLaunch& p, const Split& sp, int rt, hipStream_t st) {
-  const int64_t units = (sp.slots * p.c.H_kv + 7) / 8 * 8;
+hipError_t launch_form(const AttnDecodeLaunch& p, hipStream_t st) {
+  const int rt = row_tiles(p.H, p.c.H_kv);
+  const int want = shares(p.c.n_seq, p.H, p.c.H_kv, p.c.max_pages, p.c.page_len, kResident<FMT, D, NG>);
+  const int64_t units = (int64_t(want) * p.c.H_kv + 7) / 8 * 8;
   const dim3 grid{unsigned(units * rt)};
   if (p.H / p.c.H_kv > 8)
-    attn_decode_kernel<FMT, D, NG, true><<<grid, 256, 0, st>>>(p, sp.want, rt);
+    attn_decode_kernel<FMT, D, NG, true><<<grid, 256, 0, st>>>(p, want, rt);
   else
-    attn_decode_kernel<FMT, D, NG, false><<<grid, 256, 0, st>>>(p, sp.want, rt);
+    attn_decode_kernel<FMT, D, NG, false><<<grid, 256, 0, st>>>(p, want, rt);
+  if (hipError_t e = hipGetLastError()) return e;
+  if (want == 1) return hipSuccess;
+  attn_join_kernel<D><<<dim3(unsigned(p.c.n_seq * p.H)), 512, 0, st>>>(p);
+  return hipGetLastError();
 }
 
 template <int D>
 hipError_t launch_d(const AttnDecodeLaunch& p, hipStream_t st) {
-  const Split sp = split_of(p.c.n_seq, p.H, p.c.H_kv, p.c.max_pages, p.c.page_len);
-  const int rt = row_tiles(p.H, p.c.H_kv);
-  if (p.c.format == KV_BF16)
-    launch_form<KV_BF16, D, 1>(p, sp, rt, st);
-  else if (p.c.format == KV_U8)
-    p.c.group == D ? launch_form<KV_U8, D, 1>(p, sp, rt, st) : launch_form<KV_U8, D, D / 32>(p, sp, rt, st);
-  else
-    p.c.group == D ? launch_form<KV_U4, D, 1>(p, sp, rt, st) : launch_form<KV_U4, D, D / 32>(p, sp, rt, st);
-  if (hipError_t e = hipGetLastError()) return e;
-  if (sp.want) {
-    attn_join_kernel<D><<<dim3(unsigned(p.c.n_seq * p.H)), 256, 0, st>>>(p, sp.want);
-    return hipGetLastError();
-  }
-  return hipSuccess;
+  const bool one = p.c.group == D;
+  if (p.c.format == KV_BF16) return launch_form<KV_BF16, D, 1>(p, st);
+  if (p.c.format == KV_U8) return one ? launch_form<KV_U8, D, 1>(p, st) : launch_form<KV_U8, D, D / 32>(p, st);
+  return one ? launch_form<KV_U4, D, 1>(p, st) : launch_form<KV_U4, D, D / 32>(p, st);
 }
 
 }  // namespace
 
 size_t attn_decode_ws(int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len) {
-  const Split sp = split_of(n_seq, H, H_kv, max_pages, page_len);
-  return sp.want ? size_t(sp.slots) * size_t(H) * size_t(d + 4) : 0;
+  const int64_t want = shares(n_seq, H, H_kv, max_pages, page_len, 4);  // the most of any form
+  return want > 1 ? size_t(n_seq * 2 + 3) / 4 * 4 + size_t(want + n_seq) * size_t(H) * size_t(d + 4) : 0;
 }
 
 hipError_t launch_attn_decode(const AttnDecodeLaunch& p, hipStream_t st) {

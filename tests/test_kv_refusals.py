@@ -123,6 +123,7 @@ def test_read(L, kw, status, text):
 @pytest.mark.parametrize("kw,status,text", [
     (dict(H=9), uq.UQ_EINVAL, "H=9"),
     (dict(n_seq=1 << 22), uq.UQ_EUNSUPPORTED, "2^24"),
+    (dict(n_seq=1 << 13, max_pages=1 << 20), uq.UQ_EUNSUPPORTED, "2^37"),
     (dict(ld_q=1028), uq.UQ_EINVAL, "ld_q"),
     (dict(ld_o=1030), uq.UQ_EINVAL, "ld_o"),
     (dict(ld_o=512), uq.UQ_EINVAL, "ld_o"),
