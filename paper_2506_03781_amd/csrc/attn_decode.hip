@@ -25,17 +25,32 @@
 // The heads are columns in both products, so maximum, sum and rescaling are
 // per lane.  No data passes through LDS before the join.
 //
+// Statistics.  The scale and offset of a position belong to a row of S^T and
+// are wanted in every column; the matrix cores spread them: a lane loads the
+// (scale, offset) pair of position l % 16 as it stands (two bf16 values), and a
+// product with a column of constants gives the scale, the offset times sum q
+// or the value of the codes' middle in the layout of S^T
+// (v_mfma_f32_16x16x16_bf16, k = 4 (l / 16) .. + 4: the pair is slots 0 and 1
+// of the lane's four, and with several groups lane / 16 takes one each).
+//
 // Precision.  Scores are fp32 sums of exact products.  A weight p (times the
 // group's scale for codes) enters the second product as two bf16 terms, the
 // truncated value and the truncated rest, so what is lost is below 2^-16 of
 // it: with up to 8 heads the rest stands in the columns 8..15, which costs
-// nothing, above that in a second product.  Codes are fed as c, 4-bit ones as
-// 128 + c (one AND-OR makes two of them); the 128 leaves the scores through
-// the product's start value -128 sum q.  In the output every step takes the
-// codes' middle away again with the same bf16 terms (a product with a
-// constant), and the exact weights carry the middle's value: what truncation
-// takes off the terms then scales values around zero, not their offset, which
-// in a long row is hundreds of times the output.
+// nothing, above that in a second product.  Every step takes the codes'
+// middle away again with the same bf16 terms (a product with a constant), and
+// the exact weights carry the middle's value: what truncation takes off the
+// terms then scales values around zero, not their offset, which in a long row
+// is hundreds of times the output.
+//
+// Codes as bf16.  4-bit ones as 128 + c (one AND-OR makes two); the 128 leaves
+// the scores through the product's start value -128 sum q.  8-bit ones as
+// c 2^-133: the byte stands in the low half of a bf16 word (one byte
+// permutation makes two), which is that number below 128 (subnormal) and
+// above (exponent 1) alike, and exact.  The queries of a head are scaled by a
+// power of two to a largest magnitude in [2^120, 2^121) and the values' scales
+// by 2^64 against it, so values up to 2^63 and down to 2^-57 keep full
+// precision.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -54,6 +69,7 @@ typedef __bf16 bf16x8d __attribute__((ext_vector_type(8)));
 typedef float f32x4d __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x4d __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2d __attribute__((ext_vector_type(2)));
+typedef short s16x4d __attribute__((ext_vector_type(4)));
 
 constexpr float LOG2E_D = 1.44269504088896341f;
 constexpr float LOWEST = -3.402823466e38f;  // the running maximum before any position
@@ -67,6 +83,11 @@ constexpr int CUS = 256;
 __device__ __forceinline__ f32x4d mfma16(const u32x4d& a, const u32x4d& b, const f32x4d& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8d, a), __builtin_bit_cast(bf16x8d, b), c, 0,
                                                  0, 0);
+}
+
+__device__ __forceinline__ f32x4d mfma16(const u32x2d& a, const u32x2d& b, const f32x4d& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(s16x4d, a), __builtin_bit_cast(s16x4d, b), c, 0, 0,
+                                                   0);
 }
 
 // Upper halves of two words: the bf16 values that a and b truncate to, a first.
@@ -113,9 +134,14 @@ __device__ __forceinline__ T wave_scan(T x) {
 // ---------------------------------------------------------------------------
 // which positions a workgroup takes
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ int capped_len(const AttnDecodeLaunch& p, int64_t s) {
+// Element i of an array that no kernel running now writes, i the same in every
+// lane: a scalar load, which does not wait for the vector loads before it.
+__device__ __forceinline__ int scalar(const int32_t* p, int64_t i) {
+  return reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(reinterpret_cast<uintptr_t>(p))[i];
+}
+
+__device__ __forceinline__ int capped(const AttnDecodeLaunch& p, int len) {
   const int64_t cap = p.c.max_pages << p.c.log_page;
-  const int len = p.lens[s];
   return len < 0 ? 0 : int(len < cap ? len : cap);
 }
 
@@ -135,7 +161,7 @@ __device__ __forceinline__ Share share_of(const AttnDecodeLaunch& p, int at, int
   const int lane = threadIdx.x & 63;
   const int n = int(p.c.n_seq);
   const int per = (n + 63) / 64;
-  auto cost = [&](int j) { return j < n ? blocks_of(capped_len(p, j)) + 1 : 0; };
+  auto cost = [&](int j) { return j < n ? blocks_of(capped(p, p.lens[j])) + 1 : 0; };
   int mine = 0;
   for (int j = lane * per; j < lane * per + per; ++j) mine += cost(j);
   int upto = wave_scan(mine);
@@ -168,6 +194,32 @@ __device__ __forceinline__ Share share_of(const AttnDecodeLaunch& p, int at, int
   h.s = first;
   h.begin = before;
   return h;
+}
+
+// A share's part of one sequence: blocks [b0, b1); the sequence's first and
+// last lie in it where it opens and closes.
+struct Chunk {
+  int64_t s;
+  int len, b0, b1, end;  // end: of the sequence's cost
+  bool opens, closes;
+};
+
+// The share's next chunk after c (the first for c.s = share.s - 1, c.end =
+// share.begin); false: none.  A sequence without positions is a chunk too,
+// where it opens.
+__device__ __forceinline__ bool next_chunk(const AttnDecodeLaunch& p, const Share& h, Chunk& c) {
+  while (c.end < h.b && ++c.s < p.c.n_seq) {
+    const int begin = c.end;
+    c.len = capped(p, scalar(p.lens, c.s));
+    const int blocks = blocks_of(c.len);
+    c.end = begin + blocks + 1;
+    c.b0 = std::max(h.a - begin, 0);
+    c.b1 = std::min(h.b - begin, blocks);
+    c.opens = begin >= h.a;
+    c.closes = begin + blocks <= h.b;
+    if (c.b0 < c.b1 || (blocks == 0 && c.opens)) return true;
+  }
+  return false;
 }
 
 // The workspace: the first and the last share of each sequence, then the
@@ -216,22 +268,20 @@ __device__ __forceinline__ void load_key(const char* __restrict__ tile, int lane
   }
 }
 
-// The eight channels of contraction step c of a key as bf16 (4-bit codes as 128 + c).
+// The eight channels of contraction step c of a key as bf16.  magic: 0x43004300
+// in a register (two scalar constants would not fit one AND-OR).
 template <int FMT, int D>
-__device__ __forceinline__ u32x4d key_step(const uint32_t (&w)[Form<FMT, D>::KW], int c) {
+__device__ __forceinline__ u32x4d key_step(const uint32_t (&w)[Form<FMT, D>::KW], int c, uint32_t magic) {
   u32x4d a;
   if constexpr (FMT == KV_BF16) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) a[i] = w[4 * c + i];
   } else if constexpr (FMT == KV_U8) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t x = w[2 * c + i / 2] >> (16 * (i & 1));
-      a[i] = top_halves(__float_as_uint(float(x & 255u)), __float_as_uint(float(x >> 8 & 255u)));
-    }
+    for (int i = 0; i < 4; ++i) a[i] = __builtin_amdgcn_perm(0u, w[2 * c + i / 2], i & 1 ? 0x0C030C02u : 0x0C010C00u);
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) a[i] = (w[c] >> (4 * i) & 0x000F000Fu) | 0x43004300u;
+    for (int i = 0; i < 4; ++i) a[i] = (w[c] >> (4 * i) & 0x000F000Fu) | magic;
   }
   return a;
 }
@@ -256,61 +306,38 @@ __device__ __forceinline__ void load_value(const char* __restrict__ tile, int ro
   }
 }
 
-// Two positions' values at the lane's channel c, as bf16 (4-bit codes as 128 + c).
+// Two positions' values at the lane's channel c, as bf16.
 template <int FMT, int D>
 __device__ __forceinline__ uint32_t value_pair(const uint32_t (&a)[Form<FMT, D>::VW],
-                                               const uint32_t (&b)[Form<FMT, D>::VW], int c) {
+                                               const uint32_t (&b)[Form<FMT, D>::VW], int c, uint32_t magic) {
   if constexpr (FMT == KV_BF16) {
     return c & 1 ? top_halves(a[c / 2], b[c / 2]) : low_halves(a[c / 2], b[c / 2]);
   } else if constexpr (FMT == KV_U8) {
-    const int sh = 8 * (c & 3);
-    return top_halves(__float_as_uint(float(a[c / 4] >> sh & 255u)), __float_as_uint(float(b[c / 4] >> sh & 255u)));
+    return __builtin_amdgcn_perm(b[c / 4], a[c / 4], 0x0C040C00u + 0x00010001u * uint32_t(c & 3));
   } else {
     const uint32_t x = c < 4 ? low_halves(a[0], b[0]) : top_halves(a[0], b[0]);
-    return (x >> (4 * (c & 3)) & 0x000F000Fu) | 0x43004300u;
+    return (x >> (4 * (c & 3)) & 0x000F000Fu) | magic;
   }
 }
 
-// f(0) .. f(3), the argument a constant.
-template <typename F>
-__device__ __forceinline__ void each4(F f) {
-  f(std::integral_constant<int, 0>{});
-  f(std::integral_constant<int, 1>{});
-  f(std::integral_constant<int, 2>{});
-  f(std::integral_constant<int, 3>{});
-}
-
-// x of lane L of the lane's 16, which the using instruction takes as it reads it.
-template <int L>
-__device__ __forceinline__ float of16(float x) {
-  return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(x), 0x150 + L, 0xF, 0xF, true));  // row_newbcast
-}
-
-// The statistics' part x of position 4 grp + I of tile t, group e (constants
-// once unrolled): 16 lanes hold 16 different words instead of 16 copies.
-template <int NG, int I>
-__device__ __forceinline__ float of_lane(float x, int t, int e) {
-  switch (NG == 1 ? t : e) {
-    case 0: return of16<I>(x);
-    case 1: return of16<4 + I>(x);
-    case 2: return of16<8 + I>(x);
-    default: return of16<12 + I>(x);
-  }
-}
+// bf16 pair (lo, hi) of two values, truncated.
+__device__ __forceinline__ uint32_t pair(float lo, float hi) { return top_halves(__float_as_uint(lo), __float_as_uint(hi)); }
 
 // Workgroups a CU holds (their registers are bounded to that).
 template <int FMT, int D, int NG>
-constexpr int kResident = D == 64 ? 4 : FMT == KV_BF16 ? 2 : 3;
+constexpr int kResident = D == 64 ? 4 : FMT == KV_BF16 || NG > 1 ? 2 : 3;
 
 // WIDE: 16 query heads a workgroup, else 8 with the weights' rests in the upper columns.
 template <int FMT, int D, int NG, bool WIDE>
-__global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kernel(AttnDecodeLaunch p, int want, int rtiles) {
+__global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kernel(AttnDecodeLaunch p, int want,
+                                                                                   int rtiles) {
   using F = Form<FMT, D>;
   constexpr int HEADS = WIDE ? 16 : 8;
   constexpr bool CODES = FMT != KV_BF16;
-  constexpr int NGA = CODES ? NG : 1;
   constexpr float MID = FMT == KV_U8 ? 128.0f : 8.0f;
-  constexpr int SW = NGA == 1 ? 1 : 2;  // words of statistics a lane holds of a step's keys (values)
+  constexpr uint32_t MID_TERM = FMT == KV_U8 ? 0x80808080u : 0xC308C308u;  // minus the middle, as the codes are fed
+  constexpr float VSCALE = FMT == KV_U8 ? 0x1p64f : 1.0f;                  // on the values' scales
+  constexpr float VBACK = FMT == KV_U8 ? 0x1p69f : 1.0f;                   // 2^133 / VSCALE
   constexpr int LD = D + 4;
   __shared__ __attribute__((aligned(16))) float so[WAVES][16][LD];
   __shared__ float sm[WAVES][16], ss[WAVES][16];
@@ -328,304 +355,314 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
   const int h_in = rt * HEADS + (col & (HEADS - 1));  // head within its key/value head's group
   const bool rest = !WIDE && col >= 8;
   const uint32_t cut = rest ? 0xFFFF0000u : 0u;
-  const float cl = fabsf(p.scale) * LOG2E_D;
+  uint32_t magic = 0x43004300u;
+  asm("" : "+v"(magic));
 
-  int end = share.begin;
-  for (int64_t s = share.s; s < c.n_seq && end < share.b; ++s) {
-  const int begin = end;
-  const int len = uniform(capped_len(p, s));
-  const int blocks = blocks_of(len);
-  end = begin + blocks + 1;
-  const int b0 = std::max(share.a - begin, 0), b1 = std::min(share.b - begin, blocks);
-  const bool opens = begin >= share.a, closes = begin + blocks <= share.b;  // the sequence starts, ends here
-  if (b0 >= b1 && !(blocks == 0 && opens)) continue;
-  if (want > 1 && g == 0 && rt == 0 && threadIdx.x == 0) {
-    if (opens) shares_of(p)[s].x = at;
-    if (closes) shares_of(p)[s].y = at;
-  }
-
-  // queries, and (codes) their sums over each group of channels
-  u32x4d q[F::NC];
-  float qsum[NGA];
-  {
-    const uint16_t* row = p.Q + s * p.ld_q + (int64_t(g) * grp_heads + h_in) * D + 8 * grp;
-    float part[F::NC];
-#pragma unroll
-    for (int k = 0; k < F::NC; ++k) {
-      q[k] = h_in < grp_heads ? *reinterpret_cast<const u32x4d*>(row + 32 * k) : u32x4d{0, 0, 0, 0};
-      if (p.scale < 0.0f) q[k] ^= 0x80008000u;  // so that the scale can be taken as positive
-      float t = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) t += __uint_as_float(q[k][i] << 16) + __uint_as_float(q[k][i] & 0xFFFF0000u);
-      part[k] = t;
-    }
-    if constexpr (CODES) {
-#pragma unroll
-      for (int i = 0; i < NGA; ++i) {
-        float t = 0.0f;
-#pragma unroll
-        for (int k = i * F::NC / NGA; k < (i + 1) * F::NC / NGA; ++k) t += part[k];
-        qsum[i] = sum4(t);
-      }
-    } else {
-      qsum[0] = 0.0f;
-    }
-  }
-  const int u1 = b1 * WAVES;
-  int u = b0 * WAVES + wave;
-
-  f32x4d acc[F::NV] = {};
-  float off[NGA] = {};  // sums of weight times the value of the codes' middle
-  float m = LOWEST, l = 0.0f;
-
-  const int32_t* pages = c.pages + s * c.max_pages;
   const uint32_t page_bytes = uint32_t(c.H_kv) * uint32_t(c.page_len) * F::ROW;
-  const uint32_t page_stats = uint32_t(c.H_kv) * uint32_t(c.page_len) * NGA;
+  const uint32_t page_stats = uint32_t(c.H_kv) * uint32_t(c.page_len) * NG;
   const uint32_t head_bytes = uint32_t(g) * uint32_t(c.page_len) * F::ROW;
-  // the lane's word of statistics: position 4 grp + col % 4 of tile col / 4 % 2 (one group), of both (several)
-  const uint32_t lane_stat = uint32_t(g) * uint32_t(c.page_len) * NGA + 4 * grp + (col & 3) +
-                             (NGA > 1 ? uint32_t(col / 4 % NGA) * uint32_t(c.page_len) : 0u);
-
-  // a step's pages are looked up a step before its loads, its loads go out a step before its products
-  int page[2];
-  auto look_up = [&](int u) {
+  // the lane's word of statistics in a tile: position l % 16 of group l / 16
+  const uint32_t lane_stat = (uint32_t(g) * NG + uint32_t(grp % NG)) * uint32_t(c.page_len) + col;
+  // columns of constants that take a group's scale (times VSCALE), and its middle's value, out of the pairs
+  uint32_t pick[NG], mids[NG];
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int base = u * STEP + 16 * t;
-      page[t] = u < u1 && base < len ? pages[base >> c.log_page] : -1;
-    }
-  };
-  struct Step {
-    uint32_t k[2][F::KW], v[8][F::VW], kst[SW], vst[SW];
+  for (int e = 0; e < NG; ++e) {
+    pick[e] = grp == e ? pair(VSCALE, 0.0f) : 0u;
+    mids[e] = grp == e ? pair(MID, 1.0f) : 0u;
+  }
+
+  // The loads run a step ahead of the products, over the chunks' ends: the next
+  // step's keys are asked for when this step's scores are done, its values when
+  // they are used up, in the same registers; its pages were looked up before.
+  // Behind the last step, and for a tile on no page, the loads go to page 0.
+  struct Ahead {
+    Chunk c;
+    bool is;
+    int u, u1, page[2];
+    uint64_t place[2], stat[2];
     int nv[2];  // positions of each tile that take part
-  };
-  auto load = [&](Step& x, int u) {
-    uint64_t at[2];
-    uint64_t sat[2];
+  } next;
+  uint32_t kw[2][F::KW], vw[8][F::VW], kst[2], vst[2];
+  auto look_up = [&] {
+    const int32_t* pages = c.pages + next.c.s * c.max_pages;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const int base = u * STEP + 16 * t;
-      const bool is = page[t] >= 0 && page[t] < c.n_pages;
-      const uint32_t pg = is ? uint32_t(page[t]) : 0u;
-      const uint32_t place = is ? uint32_t(base & (c.page_len - 1)) : 0u;
-      x.nv[t] = is ? std::min(16, len - base) : 0;
-      at[t] = uint64_t(pg) * page_bytes + head_bytes + place * F::ROW;
-      sat[t] = uint64_t(pg) * page_stats + place;
+      const int base = next.u * STEP + 16 * t;
+      next.page[t] = next.is && base < next.c.len ? scalar(pages, base >> c.log_page) : -1;
     }
-    look_up(u + WAVES);
-    if (x.nv[0] + x.nv[1] == 0) return;
-#pragma unroll
-    for (int t = 0; t < 2; ++t) load_key<FMT, D>(static_cast<const char*>(c.k) + at[t], lane, x.k[t]);
-    if constexpr (CODES) {
-#pragma unroll
-      for (int t = 0; t < SW; ++t) {
-        uint64_t o = sat[t];
-        if (SW == 1) o = col & 4 ? sat[1] : o;
-        o += lane_stat;
-        x.kst[t] = reinterpret_cast<const uint32_t*>(c.k_stat)[o];
-        x.vst[t] = reinterpret_cast<const uint32_t*>(c.v_stat)[o];
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) load_value<FMT, D>(static_cast<const char*>(c.v) + at[j / 4], 4 * grp + j % 4, lane, x.v[j]);
   };
-  auto compute = [&](Step& y) {
-    if (y.nv[0] + y.nv[1] == 0) return;
-    // scores of positions 4 grp + i of tile t
-    float x[8];
-    float sc[SW], lo[SW];
-    if constexpr (CODES) {
+  auto open_chunk = [&] {  // of the chunks with positions
+    do next.is = next_chunk(p, share, next.c);
+    while (next.is && next.c.b0 >= next.c.b1);
+    next.u = next.c.b0 * WAVES + wave;
+    next.u1 = next.c.b1 * WAVES;
+  };
+  auto load_keys = [&] {
 #pragma unroll
-      for (int t = 0; t < SW; ++t) {
-        sc[t] = __uint_as_float(y.kst[t] << 16);
-        lo[t] = __uint_as_float(y.kst[t] & 0xFFFF0000u);
-      }
+    for (int t = 0; t < 2; ++t) {
+      const int base = next.u * STEP + 16 * t;
+      const bool is = next.page[t] >= 0 && next.page[t] < c.n_pages;
+      const uint32_t pg = is ? uint32_t(next.page[t]) : 0u;
+      const uint32_t r = is ? uint32_t(base & (c.page_len - 1)) : 0u;
+      next.nv[t] = is ? std::min(16, next.c.len - base) : 0;
+      next.place[t] = uint64_t(pg) * page_bytes + (head_bytes + r * F::ROW);
+      next.stat[t] = uint64_t(pg) * page_stats + r;
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      if constexpr (CODES) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[4 * t + i] = 0.0f;
-#pragma unroll
-        for (int e = 0; e < NGA; ++e) {
-          const float start = FMT == KV_U4 ? -128.0f * qsum[e] : 0.0f;
-          f32x4d a = {start, start, start, start};
-#pragma unroll
-          for (int k = e * F::NC / NGA; k < (e + 1) * F::NC / NGA; ++k) a = mfma16(key_step<FMT, D>(y.k[t], k), q[k], a);
-          each4([&](auto ic) {
-            constexpr int i = decltype(ic)::value;
-            x[4 * t + i] = __builtin_fmaf(of_lane<NGA, i>(sc[SW == 1 ? 0 : t], t, e), a[i], x[4 * t + i]);
-            x[4 * t + i] = __builtin_fmaf(of_lane<NGA, i>(lo[SW == 1 ? 0 : t], t, e), qsum[e], x[4 * t + i]);
-          });
-        }
-      } else {
-        f32x4d a = {};
-#pragma unroll
-        for (int k = 0; k < F::NC; ++k) a = mfma16(key_step<FMT, D>(y.k[t], k), q[k], a);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[4 * t + i] = a[i];
-      }
-    }
-    const bool tail = y.nv[0] + y.nv[1] < 32;
-    if (tail) {  // positions that take no part: no weight, and nothing of theirs in the products
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const bool in = 4 * grp + j % 4 < y.nv[j / 4];
-        x[j] = in ? x[j] : -__builtin_inff();
-        if constexpr (!CODES) {
-#pragma unroll
-          for (int i = 0; i < F::VW; ++i) y.v[j][i] = in ? y.v[j][i] : 0u;
-        }
-      }
-      if constexpr (CODES) {
-#pragma unroll
-        for (int t = 0; t < SW; ++t) {
-          int nv = y.nv[t];
-          if (SW == 1) nv = col & 4 ? y.nv[1] : nv;
-          y.vst[t] = 4 * grp + (col & 3) < nv ? y.vst[t] : 0u;
-        }
-      }
-    }
-    // running maximum: the reference moves only when a score exceeds it by SLACK
-    float mx = x[0];
-#pragma unroll
-    for (int j = 1; j < 8; ++j) mx = fmaxf(mx, x[j]);
-    mx = max4(mx) * cl;
-    if (__any(mx > m + SLACK)) {
-      const float m1 = fmaxf(m, mx);
-      const float f = __builtin_amdgcn_exp2f(m - m1);
-      m = m1;
-      l *= f;
-#pragma unroll
-      for (int k = 0; k < F::NV; ++k) acc[k] *= f;
-      if constexpr (CODES) {
-#pragma unroll
-        for (int e = 0; e < NGA; ++e) off[e] *= f;
-      }
-    }
-    float w[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], cl, -m));
-    if (tail) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) w[j] = 4 * grp + j % 4 < y.nv[j / 4] ? w[j] : 0.0f;
-    }
-    l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-    if constexpr (CODES) {
-#pragma unroll
-      for (int t = 0; t < SW; ++t) {
-        sc[t] = __uint_as_float(y.vst[t] << 16);
-        lo[t] = __builtin_fmaf(sc[t], MID, __uint_as_float(y.vst[t] & 0xFFFF0000u));
-      }
-    }
-#pragma unroll
-    for (int e = 0; e < NGA; ++e) {
-      float z[8];
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        each4([&](auto ic) {
-          constexpr int i = decltype(ic)::value;
-          const float wi = w[4 * t + i];
-          if constexpr (CODES) {
-            z[4 * t + i] = of_lane<NGA, i>(sc[SW == 1 ? 0 : t], t, e) * wi;
-            off[e] = __builtin_fmaf(of_lane<NGA, i>(lo[SW == 1 ? 0 : t], t, e), wi, off[e]);
-          } else {
-            z[4 * t + i] = wi;
-          }
-        });
-      u32x4d hi, lw;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t a = __float_as_uint(z[2 * i]), d = __float_as_uint(z[2 * i + 1]);
-        if constexpr (WIDE) {
-          hi[i] = top_halves(a, d);
-          lw[i] = top_halves(__float_as_uint(z[2 * i] - __uint_as_float(a & 0xFFFF0000u)),
-                             __float_as_uint(z[2 * i + 1] - __uint_as_float(d & 0xFFFF0000u)));
-        } else {
-          hi[i] = top_halves(__float_as_uint(z[2 * i] - __uint_as_float(a & cut)),
-                             __float_as_uint(z[2 * i + 1] - __uint_as_float(d & cut)));
-        }
-      }
-#pragma unroll
-      for (int k = e * F::NV / NGA; k < (e + 1) * F::NV / NGA; ++k) {
-        u32x4d a;
-        if constexpr (CODES) {
-          constexpr uint32_t mm = FMT == KV_U8 ? 0xC300C300u : 0xC308C308u;  // -128; -136
-          const u32x4d mid = {mm, mm, mm, mm};
-          acc[k] = mfma16(mid, hi, acc[k]);
-          if constexpr (WIDE) acc[k] = mfma16(mid, lw, acc[k]);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) a[i] = value_pair<FMT, D>(y.v[2 * i], y.v[2 * i + 1], k);
-        acc[k] = mfma16(a, hi, acc[k]);
-        if constexpr (WIDE) acc[k] = mfma16(a, lw, acc[k]);
-      }
+      load_key<FMT, D>(static_cast<const char*>(c.k) + next.place[t], lane, kw[t]);
+      if constexpr (CODES) kst[t] = (reinterpret_cast<const uint32_t*>(c.k_stat) + next.stat[t])[lane_stat];
     }
   };
-  Step s0, s1;
-  look_up(u);
-  if (u < u1) load(s0, u);
-  while (u < u1) {
-    if (u + WAVES < u1) load(s1, u + WAVES);
-    compute(s0);
-    u += WAVES;
-    if (u >= u1) break;
-    if (u + WAVES < u1) load(s0, u + WAVES);
-    compute(s1);
-    u += WAVES;
-  }
+  auto load_values = [&] {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      if constexpr (CODES) vst[t] = (reinterpret_cast<const uint32_t*>(c.v_stat) + next.stat[t])[lane_stat];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      load_value<FMT, D>(static_cast<const char*>(c.v) + next.place[j / 4], 4 * grp + j % 4, lane, vw[j]);
+    next.u += WAVES;
+    if (next.u >= next.u1) open_chunk();
+    look_up();
+  };
+  Chunk ch{int64_t(share.s) - 1, 0, 0, 0, share.begin, false, false};
+  next.c = ch;
+  open_chunk();
+  look_up();
+  load_keys();
+  int nv[2] = {next.nv[0], next.nv[1]};
+  load_values();
 
-  // join the wavefronts: row of column `col` in the order tile, row of the tile
-  l = sum4(l);
-#pragma unroll
-  for (int e = 0; e < NGA; ++e) {
-    if constexpr (CODES) {
-      off[e] = rest ? 0.0f : sum4(off[e]);
+  while (next_chunk(p, share, ch)) {
+    const int64_t s = ch.s;
+    const bool opens = ch.opens, closes = ch.closes;
+    if (want > 1 && g == 0 && rt == 0 && threadIdx.x == 0) {
+      if (opens) shares_of(p)[s].x = at;
+      if (closes) shares_of(p)[s].y = at;
     }
+
+    // queries (a negative scale's sign put on them), and for codes their sums over each group of channels
+    u32x4d q[F::NC];
+    float cl = fabsf(p.scale) * LOG2E_D;  // scores to exponents of 2
+    float qsum[NG];
+    uint32_t qs[3];  // the sum of the lane's group in three bf16 terms, against the offset
+    {
+      const uint16_t* row = p.Q + s * p.ld_q + (int64_t(g) * grp_heads + h_in) * D + 8 * grp;
 #pragma unroll
-    for (int k = e * F::NV / NGA; k < (e + 1) * F::NV / NGA; ++k)
-      *reinterpret_cast<f32x4d*>(&so[wave][col][16 * k + 4 * grp]) = CODES ? acc[k] + off[e] : acc[k];
-  }
-  if (grp == 0) {
-    sm[wave][col] = m;
-    ss[wave][col] = l;
-  }
-  __syncthreads();
-  // two neighbouring channels of one head a thread
-  for (int o = threadIdx.x; o < HEADS * D / 2; o += 256) {
-    const int h = o / (D / 2), ch = o % (D / 2) * 2;
-    const int hh = rt * HEADS + h;
-    if (hh >= grp_heads) break;
-    const int i0 = CODES ? ch : ch % F::NV * 16 + ch / F::NV;
-    const int i1 = CODES ? ch + 1 : i0 + 16;
-    float top = sm[0][h];
-#pragma unroll
-    for (int v = 1; v < WAVES; ++v) top = fmaxf(top, sm[v][h]);
-    float t = 0.0f, a0 = 0.0f, a1 = 0.0f;
-#pragma unroll
-    for (int v = 0; v < WAVES; ++v) {
-      const float f = __builtin_amdgcn_exp2f(sm[v][h] - top);
-      float b0 = so[v][h][i0], b1 = so[v][h][i1];
-      if constexpr (!WIDE) {
-        b0 += so[v][h + 8][i0];
-        b1 += so[v][h + 8][i1];
+      for (int k = 0; k < F::NC; ++k) {
+        q[k] = h_in < grp_heads ? *reinterpret_cast<const u32x4d*>(row + 32 * k) : u32x4d{0, 0, 0, 0};
+        if (p.scale < 0.0f) q[k] ^= 0x80008000u;
       }
-      t += f * ss[v][h];
-      a0 += f * b0;
-      a1 += f * b1;
+      if constexpr (FMT == KV_U8) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int k = 0; k < F::NC; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top = std::max(top, std::max(q[k][i] << 16 & 0x7FFF0000u, q[k][i] & 0x7FFF0000u));
+        const int ex = int(__float_as_uint(max4(__uint_as_float(top))) >> 23) - 127;
+        const float up = ldexpf(1.0f, 120 - std::max(ex, -7));
+        cl = cl * ldexpf(1.0f, 13 + std::max(ex, -7));
+#pragma unroll
+        for (int k = 0; k < F::NC; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            q[k][i] = pair(__uint_as_float(q[k][i] << 16) * up, __uint_as_float(q[k][i] & 0xFFFF0000u) * up);
+      }
+      if constexpr (CODES) {
+        float mine = 0.0f;
+#pragma unroll
+        for (int e = 0; e < NG; ++e) {
+          float t = 0.0f;
+#pragma unroll
+          for (int k = e * F::NC / NG; k < (e + 1) * F::NC / NG; ++k)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float scaled = FMT == KV_U8 ? 0x1p-60f : 1.0f;
+              t += __uint_as_float(q[k][i] << 16) * scaled + __uint_as_float(q[k][i] & 0xFFFF0000u) * scaled;
+            }
+          qsum[e] = sum4(t) * (FMT == KV_U8 ? 0x1p-73f : 1.0f);
+          if (grp == e) mine = qsum[e];
+        }
+        const float h0 = __uint_as_float(__float_as_uint(mine) & 0xFFFF0000u);
+        const float h1 = __uint_as_float(__float_as_uint(mine - h0) & 0xFFFF0000u);
+        qs[0] = pair(0.0f, h0);
+        qs[1] = pair(0.0f, h1);
+        qs[2] = pair(0.0f, (mine - h0) - h1);
+      }
     }
-    const int64_t head = int64_t(g) * grp_heads + hh;
-    if (opens && closes) {
-      const float r = t == 0.0f ? 0.0f : 1.0f / t;
-      *reinterpret_cast<uint32_t*>(p.O + s * p.ld_o + head * D + ch) = pack_bf16x2(a0 * r, a1 * r);
-      if (ch == 0 && p.lse) p.lse[s * p.H + head] = t == 0.0f ? -__builtin_inff() : top + __builtin_amdgcn_logf(t);
-    } else {
-      float* part = chunks_of(p) + ((at + s) * p.H + head) * (D + 4);
-      *reinterpret_cast<float2*>(part + 4 + ch) = make_float2(a0, a1);
-      if (ch == 0) *reinterpret_cast<float2*>(part) = make_float2(top, t);
+
+    f32x4d acc[F::NV] = {};
+    float off[NG] = {};  // sums of weight times the value of the codes' middle
+    float m = LOWEST, l = 0.0f;
+
+    for (int u = ch.b0; u < ch.b1; ++u) {  // the wavefront's steps
+      // scores of positions 4 grp + i of tile t
+      float x[8];
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        f32x4d sum = {};
+        if constexpr (CODES) {
+          const u32x2d st = {kst[t], 0u};
+#pragma unroll
+          for (int i = 0; i < 3; ++i) sum = mfma16(st, u32x2d{qs[i], 0u}, sum);
+#pragma unroll
+          for (int e = 0; e < NG; ++e) {
+            const float start = FMT == KV_U4 ? -128.0f * qsum[e] : 0.0f;
+            f32x4d a = {start, start, start, start};
+#pragma unroll
+            for (int k = e * F::NC / NG; k < (e + 1) * F::NC / NG; ++k)
+              a = mfma16(key_step<FMT, D>(kw[t], k, magic), q[k], a);
+            const f32x4d sc = mfma16(st, u32x2d{grp == e ? pair(1.0f, 0.0f) : 0u, 0u}, f32x4d{});
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf(sc[i], a[i], sum[i]);
+          }
+        } else {
+#pragma unroll
+          for (int k = 0; k < F::NC; ++k) sum = mfma16(key_step<FMT, D>(kw[t], k, magic), q[k], sum);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[4 * t + i] = sum[i];
+      }
+      load_keys();
+      const bool tail = nv[0] + nv[1] < 32;
+      if (tail) {  // positions that take no part: no weight, and nothing of theirs in the products
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const bool in = 4 * grp + j % 4 < nv[j / 4];
+          x[j] = in ? x[j] : -__builtin_inff();
+          if constexpr (!CODES) {
+#pragma unroll
+            for (int i = 0; i < F::VW; ++i) vw[j][i] = in ? vw[j][i] : 0u;
+          }
+        }
+        if constexpr (CODES) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) vst[t] = col < nv[t] ? vst[t] : 0u;
+        }
+      }
+      // running maximum: the reference moves only when a score exceeds it by SLACK
+      float mx = x[0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) mx = fmaxf(mx, x[j]);
+      mx = max4(mx) * cl;
+      if (__any(mx > m + SLACK)) {
+        const float m1 = fmaxf(m, mx);
+        const float f = __builtin_amdgcn_exp2f(m - m1);
+        m = m1;
+        l *= f;
+#pragma unroll
+        for (int k = 0; k < F::NV; ++k) acc[k] *= f;
+        if constexpr (CODES) {
+#pragma unroll
+          for (int e = 0; e < NG; ++e) off[e] *= f;
+        }
+      }
+      float w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], cl, -m));
+      if (tail) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = 4 * grp + j % 4 < nv[j / 4] ? w[j] : 0.0f;
+      }
+      l += ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+#pragma unroll
+      for (int e = 0; e < NG; ++e) {
+        float z[8];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if constexpr (CODES) {
+            const u32x2d st = {vst[t], 0u};
+            const f32x4d sc = mfma16(st, u32x2d{pick[e], 0u}, f32x4d{});
+            const f32x4d md = mfma16(st, u32x2d{mids[e], 0u}, f32x4d{});
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              z[4 * t + i] = w[4 * t + i] * sc[i];
+              off[e] = __builtin_fmaf(w[4 * t + i], md[i], off[e]);
+            }
+          } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) z[4 * t + i] = w[4 * t + i];
+          }
+        }
+        u32x4d hi, lo;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          auto less = [](float v, uint32_t bits) { return v - __uint_as_float(__float_as_uint(v) & bits); };
+          if constexpr (WIDE) {
+            hi[i] = pair(z[2 * i], z[2 * i + 1]);
+            lo[i] = pair(less(z[2 * i], 0xFFFF0000u), less(z[2 * i + 1], 0xFFFF0000u));
+          } else {
+            hi[i] = pair(less(z[2 * i], cut), less(z[2 * i + 1], cut));
+          }
+        }
+#pragma unroll
+        for (int k = e * F::NV / NG; k < (e + 1) * F::NV / NG; ++k) {
+          if constexpr (CODES) {
+            const u32x4d mid = {MID_TERM, MID_TERM, MID_TERM, MID_TERM};
+            acc[k] = mfma16(mid, hi, acc[k]);
+            if constexpr (WIDE) acc[k] = mfma16(mid, lo, acc[k]);
+          }
+          u32x4d a;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) a[i] = value_pair<FMT, D>(vw[2 * i], vw[2 * i + 1], k, magic);
+          acc[k] = mfma16(a, hi, acc[k]);
+          if constexpr (WIDE) acc[k] = mfma16(a, lo, acc[k]);
+        }
+      }
+      nv[0] = next.nv[0];
+      nv[1] = next.nv[1];
+      load_values();
     }
-  }
-  __syncthreads();  // the next chunk writes LDS anew
+
+    // join the wavefronts: row of column `col` in the order tile, row of the tile
+    l = sum4(l);
+#pragma unroll
+    for (int e = 0; e < NG; ++e) {
+      if constexpr (CODES) off[e] = rest ? 0.0f : sum4(off[e]);
+#pragma unroll
+      for (int k = e * F::NV / NG; k < (e + 1) * F::NV / NG; ++k)
+        *reinterpret_cast<f32x4d*>(&so[wave][col][16 * k + 4 * grp]) = CODES ? acc[k] * VBACK + off[e] : acc[k];
+    }
+    if (grp == 0) {
+      sm[wave][col] = m;
+      ss[wave][col] = l;
+    }
+    __syncthreads();
+    // two neighbouring channels of one head a thread
+    for (int o = threadIdx.x; o < HEADS * D / 2; o += 256) {
+      const int h = o / (D / 2), cn = o % (D / 2) * 2;
+      const int hh = rt * HEADS + h;
+      if (hh >= grp_heads) break;
+      const int i0 = CODES ? cn : cn % F::NV * 16 + cn / F::NV;
+      const int i1 = CODES ? cn + 1 : i0 + 16;
+      float top = sm[0][h];
+#pragma unroll
+      for (int v = 1; v < WAVES; ++v) top = fmaxf(top, sm[v][h]);
+      float t = 0.0f, a0 = 0.0f, a1 = 0.0f;
+#pragma unroll
+      for (int v = 0; v < WAVES; ++v) {
+        const float f = __builtin_amdgcn_exp2f(sm[v][h] - top);
+        float x0 = so[v][h][i0], x1 = so[v][h][i1];
+        if constexpr (!WIDE) {
+          x0 += so[v][h + 8][i0];
+          x1 += so[v][h + 8][i1];
+        }
+        t += f * ss[v][h];
+        a0 += f * x0;
+        a1 += f * x1;
+      }
+      const int64_t head = int64_t(g) * grp_heads + hh;
+      if (opens && closes) {
+        const float r = t == 0.0f ? 0.0f : 1.0f / t;
+        *reinterpret_cast<uint32_t*>(p.O + s * p.ld_o + head * D + cn) = pack_bf16x2(a0 * r, a1 * r);
+        if (cn == 0 && p.lse) p.lse[s * p.H + head] = t == 0.0f ? -__builtin_inff() : top + __builtin_amdgcn_logf(t);
+      } else {
+        float* part = chunks_of(p) + ((at + s) * p.H + head) * (D + 4);
+        *reinterpret_cast<float2*>(part + 4 + cn) = make_float2(a0, a1);
+        if (cn == 0) *reinterpret_cast<float2*>(part) = make_float2(top, t);
+      }
+    }
+    __syncthreads();  // the next chunk writes LDS anew
   }
 }
 
