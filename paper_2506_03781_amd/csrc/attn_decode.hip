@@ -44,12 +44,12 @@
 // is hundreds of times the output.
 //
 // Codes as bf16.  4-bit ones as 128 + c (one AND-OR makes two); the 128 leaves
-// the scores through the product's start value -128 sum q.  8-bit ones as
+// the scores with the offsets, as -128 scale sum q.  8-bit ones as
 // c 2^-133: the byte stands in the low half of a bf16 word (one byte
 // permutation makes two), which is that number below 128 (subnormal) and
 // above (exponent 1) alike, and exact.  The queries of a head are scaled by a
-// power of two to a largest magnitude in [2^120, 2^121) and the values' scales
-// by 2^64 against it, so values up to 2^63 and down to 2^-57 keep full
+// power of two to a largest magnitude in [2^120, 2^121) and the scales by 2^64
+// against it, so keys and values up to 2^60 and down to 2^-57 keep full
 // precision.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -336,7 +336,7 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
   constexpr bool CODES = FMT != KV_BF16;
   constexpr float MID = FMT == KV_U8 ? 128.0f : 8.0f;
   constexpr uint32_t MID_TERM = FMT == KV_U8 ? 0x80808080u : 0xC308C308u;  // minus the middle, as the codes are fed
-  constexpr float VSCALE = FMT == KV_U8 ? 0x1p64f : 1.0f;                  // on the values' scales
+  constexpr float VSCALE = FMT == KV_U8 ? 0x1p64f : 1.0f;                  // on the scales
   constexpr float VBACK = FMT == KV_U8 ? 0x1p69f : 1.0f;                   // 2^133 / VSCALE
   constexpr int LD = D + 4;
   __shared__ __attribute__((aligned(16))) float so[WAVES][16][LD];
@@ -444,8 +444,7 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
     // queries (a negative scale's sign put on them), and for codes their sums over each group of channels
     u32x4d q[F::NC];
     float cl = fabsf(p.scale) * LOG2E_D;  // scores to exponents of 2
-    float qsum[NG];
-    uint32_t qs[3];  // the sum of the lane's group in three bf16 terms, against the offset
+    uint32_t qs[3];  // the sum of the lane's group in three bf16 terms, against (scale, offset)
     {
       const uint16_t* row = p.Q + s * p.ld_q + (int64_t(g) * grp_heads + h_in) * D + 8 * grp;
 #pragma unroll
@@ -461,7 +460,7 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
           for (int i = 0; i < 4; ++i) top = std::max(top, std::max(q[k][i] << 16 & 0x7FFF0000u, q[k][i] & 0x7FFF0000u));
         const int ex = int(__float_as_uint(max4(__uint_as_float(top))) >> 23) - 127;
         const float up = ldexpf(1.0f, 120 - std::max(ex, -7));
-        cl = cl * ldexpf(1.0f, 13 + std::max(ex, -7));
+        cl = cl * ldexpf(1.0f, 13 - 64 + std::max(ex, -7));  // 2^133 over the queries' power and the scales'
 #pragma unroll
         for (int k = 0; k < F::NC; ++k)
 #pragma unroll
@@ -469,6 +468,7 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
             q[k][i] = pair(__uint_as_float(q[k][i] << 16) * up, __uint_as_float(q[k][i] & 0xFFFF0000u) * up);
       }
       if constexpr (CODES) {
+        constexpr float down = FMT == KV_U8 ? 0x1p-69f : 1.0f;  // 2^-133 times the scales' 2^64
         float mine = 0.0f;
 #pragma unroll
         for (int e = 0; e < NG; ++e) {
@@ -476,18 +476,19 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
 #pragma unroll
           for (int k = e * F::NC / NG; k < (e + 1) * F::NC / NG; ++k)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              const float scaled = FMT == KV_U8 ? 0x1p-60f : 1.0f;
-              t += __uint_as_float(q[k][i] << 16) * scaled + __uint_as_float(q[k][i] & 0xFFFF0000u) * scaled;
-            }
-          qsum[e] = sum4(t) * (FMT == KV_U8 ? 0x1p-73f : 1.0f);
-          if (grp == e) mine = qsum[e];
+            for (int i = 0; i < 4; ++i)
+              t += __uint_as_float(q[k][i] << 16) * down + __uint_as_float(q[k][i] & 0xFFFF0000u) * down;
+          t = sum4(t);
+          if (grp == e) mine = t;
         }
-        const float h0 = __uint_as_float(__float_as_uint(mine) & 0xFFFF0000u);
-        const float h1 = __uint_as_float(__float_as_uint(mine - h0) & 0xFFFF0000u);
-        qs[0] = pair(0.0f, h0);
-        qs[1] = pair(0.0f, h1);
-        qs[2] = pair(0.0f, (mine - h0) - h1);
+        // 4-bit codes come with 128 too much: minus 128 sum q against the scale
+        constexpr float over = FMT == KV_U4 ? -128.0f : 0.0f;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+          const float h = __uint_as_float(__float_as_uint(mine) & 0xFFFF0000u);
+          qs[i] = pair(over * h, h);
+          mine -= h;
+        }
       }
     }
 
@@ -507,12 +508,11 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
           for (int i = 0; i < 3; ++i) sum = mfma16(st, u32x2d{qs[i], 0u}, sum);
 #pragma unroll
           for (int e = 0; e < NG; ++e) {
-            const float start = FMT == KV_U4 ? -128.0f * qsum[e] : 0.0f;
-            f32x4d a = {start, start, start, start};
+            f32x4d a = {};
 #pragma unroll
             for (int k = e * F::NC / NG; k < (e + 1) * F::NC / NG; ++k)
               a = mfma16(key_step<FMT, D>(kw[t], k, magic), q[k], a);
-            const f32x4d sc = mfma16(st, u32x2d{grp == e ? pair(1.0f, 0.0f) : 0u, 0u}, f32x4d{});
+            const f32x4d sc = mfma16(st, u32x2d{pick[e], 0u}, f32x4d{});
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf(sc[i], a[i], sum[i]);
           }
