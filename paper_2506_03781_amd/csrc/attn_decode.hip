@@ -671,7 +671,8 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
 template <int D>
 __global__ __launch_bounds__(512) void attn_join_kernel(AttnDecodeLaunch p) {
   constexpr int LANES = D / 4, PAR = 512 / LANES;
-  const int s = blockIdx.x / p.H, h = blockIdx.x % p.H;
+  const int s = int(workgroup() / p.H), h = int(workgroup() % p.H);
+  if (s >= p.c.n_seq) return;
   const int2 in = shares_of(p)[s];
   const int n = in.y - in.x + 1;
   if (n <= 1) return;
@@ -750,7 +751,7 @@ hipError_t launch_form(const AttnDecodeLaunch& p, hipStream_t st) {
     attn_decode_kernel<FMT, D, NG, false><<<grid, 256, 0, st>>>(p, want, rt);
   if (hipError_t e = hipGetLastError()) return e;
   if (want == 1) return hipSuccess;
-  attn_join_kernel<D><<<dim3(unsigned(p.c.n_seq * p.H)), 512, 0, st>>>(p);
+  attn_join_kernel<D><<<grid_of(p.c.n_seq * p.H), 512, 0, st>>>(p);
   return hipGetLastError();
 }
 

@@ -1,9 +1,20 @@
 // The paged key/value cache: new rows written (rotated, quantized) and ranges
 // of positions read back.  Layout, quantiser and errors in uniquan.h.
 //
-// 16 lanes take one head of one row; lane l holds its channels l + 16 c, so a
-// rotary pair (i, i + d/2) is in one lane and a group of 32 channels is two
-// values of each of the 16 lanes.
+// Both are bound by memory: every kernel moves 16 bytes a lane where the
+// layout lets it and keeps several rows in flight.
+//
+// Append.  A workgroup takes a row (few rows: a tile of heads of a row).
+// Heads that are stored in channel order (queries, keys, values of a bf16
+// cache) take D / 16 lanes each, a lane the channels 8 l .. 8 l + 7 and their
+// rotary partners D / 2 further on, whose eight (cos, sin) pairs it keeps for
+// all its heads; a group of 32 channels is one half of four lanes.  Values
+// that become codes take 16 lanes, a lane the channels l + 16 c that lie side
+// by side in the row.
+//
+// Read.  A workgroup takes 64 positions of one head of one sequence; a lane 16
+// bytes of the output.  Its codes of a key are one word (two), those of a
+// value as many bytes from one cache line.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -19,20 +30,27 @@ __device__ __forceinline__ float load1(const void* p, int64_t i, bool f32) {
   return f32 ? static_cast<const float*>(p)[i] : bf16_to_f32(static_cast<const uint16_t*>(p)[i]);
 }
 
-__device__ __forceinline__ uint16_t to_bf16(float x) { return uint16_t(pack_bf16x2(x, x)); }
-
-// Minimum, maximum and whether all values are finite, over 16 lanes.
+// Minimum, maximum and whether all values are finite.
 struct Span {
   float lo, hi;
   bool fine;
 };
-__device__ __forceinline__ Span span16(Span s) {
+__device__ __forceinline__ Span join(const Span& a, const Span& b) {
+  return Span{fminf(a.lo, b.lo), fmaxf(a.hi, b.hi), a.fine && b.fine};
+}
+template <int N>
+__device__ __forceinline__ Span span_of(const float (&x)[N]) {
+  Span s{x[0], x[0], x[0] - x[0] == 0.0f};
 #pragma unroll
-  for (int m = 8; m >= 1; m >>= 1) {
-    s.lo = fminf(s.lo, __shfl_xor(s.lo, m));
-    s.hi = fmaxf(s.hi, __shfl_xor(s.hi, m));
-    s.fine = bool(__shfl_xor(int(s.fine), m)) && s.fine;
-  }
+  for (int i = 1; i < N; ++i) s = join(s, Span{x[i], x[i], x[i] - x[i] == 0.0f});
+  return s;
+}
+// Over LANES neighbouring lanes.
+template <int LANES>
+__device__ __forceinline__ Span across(Span s) {
+#pragma unroll
+  for (int m = 1; m < LANES; m <<= 1)
+    s = join(s, Span{__shfl_xor(s.lo, m), __shfl_xor(s.hi, m), bool(__shfl_xor(int(s.fine), m))});
   return s;
 }
 
@@ -61,176 +79,326 @@ __device__ __forceinline__ uint32_t code_of(float x, const Quant& q, float top) 
   return c == c ? uint32_t(fminf(fmaxf(c, 0.0f), top)) : 0u;
 }
 
-enum Kind : int { Q_HEAD = 0, K_HEAD = 1, V_HEAD = 2 };
-
-template <int D>
-__global__ __launch_bounds__(256) void kv_append_kernel(KvAppendLaunch p) {
-  constexpr int N = D / 16;
+// Where a row goes: its sequence, position and page (-1: none).
+struct Row {
+  int64_t seq;
+  int pos, page;
+};
+// False: padding.
+__device__ __forceinline__ bool row_of(const KvAppendLaunch& p, int64_t t, Row& r) {
   const KvCache& c = p.c;
-  const int l = threadIdx.x & 15;
-  const int heads = (p.q ? p.H : 0) + 2 * c.H_kv;
-  const int64_t vec = int64_t(blockIdx.x) * 16 + (threadIdx.x >> 4);
-  const int64_t t = vec / heads;
-  if (t >= p.T) return;
-  int h = int(vec % heads);
-  int kind = V_HEAD;
-  const int n_q = p.q ? p.H : 0;
-  if (h < n_q) {
-    kind = Q_HEAD;
-  } else if (h < n_q + c.H_kv) {
-    kind = K_HEAD;
-    h -= n_q;
-  } else {
-    h -= n_q + c.H_kv;
-  }
-  const int pos = p.pos[t];
-  const int64_t s = p.seq ? p.seq[t] : t;
-  if (pos < 0 || pos >= c.max_pages << c.log_page || (p.cs && pos >= p.n_cs) || s < 0 || s >= c.n_seq) return;
+  r.pos = p.pos[t];
+  r.seq = p.seq ? p.seq[t] : t;
+  if (r.pos < 0 || r.pos >= c.max_pages << c.log_page || (p.cs && r.pos >= p.n_cs) || r.seq < 0 || r.seq >= c.n_seq)
+    return false;
+  r.page = kv_page(c, r.seq, r.pos);
+  return true;
+}
 
-  const bool f32 = p.in_dtype == F32;
-  const void* src = kind == Q_HEAD ? p.q : kind == K_HEAD ? p.k : p.v;
-  const int64_t off = t * (kind == Q_HEAD ? p.ld_q : kind == K_HEAD ? p.ld_k : p.ld_v) + int64_t(h) * D;
-  float x[N];
+// Codes of a run of eight channels of a key, where they lie in the row (in
+// bytes): run r at (r % 4)(D / 4) + 8 (r / 4) codes.
+template <int D, int FMT>
+__device__ __forceinline__ void store_run(uint8_t* row, int r, const float (&x)[8], const Quant& q) {
+  const int at = r % 4 * (D / 4) + 8 * (r / 4);
+  uint32_t c[8];
 #pragma unroll
-  for (int i = 0; i < N; ++i) x[i] = load1(src, off + l + 16 * i, f32);
-  if (kind != V_HEAD && p.cs) {
-    const float2* cs = reinterpret_cast<const float2*>(p.cs) + int64_t(pos) * (D / 2);
+  for (int i = 0; i < 8; ++i) c[i] = code_of(x[i], q, FMT == KV_U8 ? 255.0f : 15.0f);
+  if constexpr (FMT == KV_U8) {
+    *reinterpret_cast<uint2*>(row + at) =
+        make_uint2(c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24, c[4] | c[5] << 8 | c[6] << 16 | c[7] << 24);
+  } else {
+    *reinterpret_cast<uint32_t*>(row + at / 2) = c[0] | c[2] << 4 | c[4] << 8 | c[6] << 12 | c[1] << 16 | c[3] << 20 |
+                                                 c[5] << 24 | c[7] << 28;
+  }
+}
+
+template <int D, int FMT, bool F32>
+__global__ __launch_bounds__(256) void kv_append_kernel(KvAppendLaunch p) {
+  constexpr int LANES = D / 16, SLOTS = 256 / LANES;  // of a head in channel order, heads of a tile
+  constexpr int DT = F32 ? DType::F32 : DType::BF16;
+  constexpr bool CODES = FMT != KV_BF16;
+  constexpr float top = FMT == KV_U8 ? 255.0f : 15.0f;
+  constexpr int ROW = FMT == KV_BF16 ? 2 * D : FMT == KV_U8 ? D : D / 2;
+  const KvCache& c = p.c;
+  const int64_t t = workgroup();
+  Row r;
+  if (t >= p.T || !row_of(p, t, r)) return;
+  const int place = r.pos & (c.page_len - 1);
+  const int64_t ph0 = int64_t(r.page) * c.H_kv;
+  const int n_q = p.q ? p.H : 0;
+  const int plain = n_q + c.H_kv * (CODES ? 1 : 2);  // heads in channel order
+  const int tiles = (plain + SLOTS - 1) / SLOTS, vtiles = CODES ? (c.H_kv + 15) / 16 : 0;
+  const int lane = threadIdx.x % LANES;
+  float co[8], si[8];
+  if (p.cs && int(blockIdx.z) < tiles) {
+    const float4* cs = reinterpret_cast<const float4*>(p.cs + int64_t(r.pos) * D + 16 * lane);
 #pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
-      const float2 a = cs[l + 16 * i];
-      const float x1 = x[i], x2 = x[i + N / 2];
-      x[i] = x1 * a.x - x2 * a.y;
-      x[i + N / 2] = x2 * a.x + x1 * a.y;
+    for (int i = 0; i < 4; ++i) {
+      const float4 a = cs[i];
+      co[2 * i] = a.x;
+      si[2 * i] = a.y;
+      co[2 * i + 1] = a.z;
+      si[2 * i + 1] = a.w;
     }
   }
-  if (kind == Q_HEAD) {
-    uint16_t* o = p.q_out + (t * p.H + h) * D;
+  for (int tile = blockIdx.z; tile < tiles; tile += gridDim.z) {
+    int h = tile * SLOTS + threadIdx.x / LANES;
+    if (h >= plain) break;
+    const bool is_q = h < n_q, is_k = !is_q && h < n_q + c.H_kv;
+    if (!is_q) h -= is_k ? n_q : n_q + c.H_kv;
+    if (!is_q && r.page < 0) break;  // queries come first
+    const void* src = is_q ? p.q : is_k ? p.k : p.v;
+    const int64_t off = t * (is_q ? p.ld_q : is_k ? p.ld_k : p.ld_v) + int64_t(h) * D + 8 * lane;
+    float a[8], b[8];
+    load8<DT>(src, off, a);
+    load8<DT>(src, off + D / 2, b);
+    if (p.cs && (is_q || is_k)) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) o[l + 16 * i] = to_bf16(x[i]);
-    return;
-  }
-  const int page = kv_page(c, s, pos);
-  if (page < 0) return;
-  const int place = pos & (c.page_len - 1);
-  const int64_t ph = int64_t(page) * c.H_kv + h;
-  const int64_t row = ph * c.page_len + place;
-  if (c.format == KV_BF16) {
-    uint16_t* o = static_cast<uint16_t*>(kind == K_HEAD ? c.k : c.v) + row * D;
-#pragma unroll
-    for (int i = 0; i < N; ++i) o[l + 16 * i] = to_bf16(x[i]);
-    return;
-  }
-  const float top = c.format == KV_U8 ? 255.0f : 15.0f;
-  const int per = c.group / 16;  // values of a lane in one group: 2 or N
-  uint32_t* stat = reinterpret_cast<uint32_t*>(kind == K_HEAD ? c.k_stat : c.v_stat);
-  uint8_t* o = static_cast<uint8_t*>(kind == K_HEAD ? c.k : c.v) + row * (c.format == KV_U8 ? D : D / 2);
-  uint32_t code[N];
-  Span all{x[0], x[0], true};
-  Quant q;
-#pragma unroll
-  for (int i = 0; i < N; i += 2) {
-    Span sp{fminf(x[i], x[i + 1]), fmaxf(x[i], x[i + 1]), x[i] - x[i] == 0.0f && x[i + 1] - x[i + 1] == 0.0f};
-    sp = span16(sp);
-    if (per == 2) {
-      q = quant_of(sp, top);
-      code[i] = code_of(x[i], q, top);
-      code[i + 1] = code_of(x[i + 1], q, top);
-      if (l == 0) stat[(ph * (D / 32) + i / 2) * c.page_len + place] = pack_bf16x2(q.scale, q.lo);
-    }
-    all = Span{fminf(all.lo, sp.lo), fmaxf(all.hi, sp.hi), all.fine && sp.fine};
-  }
-  if (per != 2) {
-    q = quant_of(all, top);
-#pragma unroll
-    for (int i = 0; i < N; ++i) code[i] = code_of(x[i], q, top);
-    if (l == 0) stat[ph * c.page_len + place] = pack_bf16x2(q.scale, q.lo);
-  }
-  if (kind == K_HEAD) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      const int ch = l + 16 * i, run = (ch / 8 % 4) * (D / 4) + 8 * (ch / 32);
-      if (c.format == KV_U8) {
-        o[run + ch % 8] = uint8_t(code[i]);
-      } else {  // channels j and j + 2 of a run of eight share a byte
-        const uint32_t other = uint32_t(__shfl_xor(int(code[i]), 2));
-        if ((l & 2) == 0) o[(run + (ch % 8) / 2 + 4 * (ch % 2)) / 2] = uint8_t(code[i] | other << 4);
+      for (int i = 0; i < 8; ++i) {
+        const float x1 = a[i], x2 = b[i];
+        a[i] = x1 * co[i] - x2 * si[i];
+        b[i] = x2 * co[i] + x1 * si[i];
       }
     }
-  } else if (c.format == KV_U8) {
+    const int64_t ph = ph0 + h;
+    if (is_q || !CODES) {
+      uint16_t* o = is_q ? p.q_out + (t * p.H + h) * D
+                         : static_cast<uint16_t*>(is_k ? c.k : c.v) + (ph * c.page_len + place) * D;
+      store8<BF16>(o, 8 * lane, a);
+      store8<BF16>(o, 8 * lane + D / 2, b);
+      continue;
+    }
+    // a key as codes
+    uint8_t* row = static_cast<uint8_t*>(c.k) + (ph * c.page_len + place) * ROW;
+    uint32_t* stat = reinterpret_cast<uint32_t*>(c.k_stat) + ph * (D / c.group) * c.page_len + place;
+    Span sa = span_of(a), sb = span_of(b);
+    if (c.group == 32) {
+      const Quant qa = quant_of(across<4>(sa), top), qb = quant_of(across<4>(sb), top);
+      store_run<D, FMT>(row, lane, a, qa);
+      store_run<D, FMT>(row, lane + D / 16, b, qb);
+      if (lane % 4 == 0) {
+        stat[lane / 4 * c.page_len] = pack_bf16x2(qa.scale, qa.lo);
+        stat[(lane / 4 + D / 64) * c.page_len] = pack_bf16x2(qb.scale, qb.lo);
+      }
+    } else {
+      const Quant q = quant_of(across<LANES>(join(sa, sb)), top);
+      store_run<D, FMT>(row, lane, a, q);
+      store_run<D, FMT>(row, lane + D / 16, b, q);
+      if (lane == 0) stat[0] = pack_bf16x2(q.scale, q.lo);
+    }
+  }
+  if constexpr (CODES) {
+    constexpr int N = D / 16;
+    if (r.page < 0) return;
+    const int l = threadIdx.x & 15;
+    for (int tile = int(blockIdx.z) < tiles ? (gridDim.z == 1 ? 0 : vtiles) : int(blockIdx.z) - tiles; tile < vtiles;
+         tile += gridDim.z) {
+      const int h = tile * 16 + threadIdx.x / 16;
+      if (h >= c.H_kv) break;
+      const int64_t off = t * p.ld_v + int64_t(h) * D + l;
+      float x[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) o[l * N + i] = uint8_t(code[i]);
-  } else {
+      for (int i = 0; i < N; ++i) x[i] = load1(p.v, off + 16 * i, F32);
+      const int64_t ph = ph0 + h;
+      uint32_t* stat = reinterpret_cast<uint32_t*>(c.v_stat) + ph * (D / c.group) * c.page_len + place;
+      uint32_t code[N];
+      if (c.group == 32) {
 #pragma unroll
-    for (int i = 0; i < N; i += 2) o[(l * N + i) / 2] = uint8_t(code[i] | code[i + 1] << 4);
+        for (int i = 0; i < N; i += 2) {
+          const float two[2] = {x[i], x[i + 1]};
+          const Quant q = quant_of(across<16>(span_of(two)), top);
+          code[i] = code_of(x[i], q, top);
+          code[i + 1] = code_of(x[i + 1], q, top);
+          if (l == 0) stat[i / 2 * c.page_len] = pack_bf16x2(q.scale, q.lo);
+        }
+      } else {
+        const Quant q = quant_of(across<16>(span_of(x)), top);
+#pragma unroll
+        for (int i = 0; i < N; ++i) code[i] = code_of(x[i], q, top);
+        if (l == 0) stat[0] = pack_bf16x2(q.scale, q.lo);
+      }
+      uint32_t* row =
+          reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(c.v) + (ph * c.page_len + place) * ROW + l * (ROW / 16));
+      constexpr int BITS = FMT == KV_U8 ? 8 : 4, PER = 32 / BITS;
+      if constexpr (N >= PER) {
+#pragma unroll
+        for (int w = 0; w < N / PER; ++w) {
+          uint32_t v = 0;
+#pragma unroll
+          for (int i = 0; i < PER; ++i) v |= code[w * PER + i] << (BITS * i);
+          row[w] = v;
+        }
+      } else {
+        *reinterpret_cast<uint16_t*>(row) = uint16_t(code[0] | code[1] << 4 | code[2] << 8 | code[3] << 12);
+      }
+    }
   }
 }
 
-// Value of channel ch at a cache row.
-template <int D>
-__device__ __forceinline__ float kv_value(const KvCache& c, bool key, int64_t ph, int place, int ch) {
-  const int64_t row = ph * c.page_len + place;
-  const void* base = key ? c.k : c.v;
-  if (c.format == KV_BF16) return bf16_to_f32(static_cast<const uint16_t*>(base)[row * D + ch]);
-  const bool u8 = c.format == KV_U8;
-  int at;
-  if (key)
-    at = (ch / 8 % 4) * (D / 4) + 8 * (ch / 32) + (u8 ? ch % 8 : (ch % 8) / 2 + 4 * (ch % 2));
-  else
-    at = (ch % 16) * (D / 16) + ch / 16;
-  const uint8_t* o = static_cast<const uint8_t*>(base) + row * (u8 ? D : D / 2);
-  const uint32_t code = u8 ? o[at] : o[at / 2] >> (4 * (at & 1)) & 15u;
-  const uint32_t st = reinterpret_cast<const uint32_t*>(key ? c.k_stat : c.v_stat)[
-      (ph * (D / c.group) + ch / c.group) * c.page_len + place];
-  const float scale = __uint_as_float(st << 16), lo = __uint_as_float(st & 0xFFFF0000u);
-  return lo + scale * float(code);
+constexpr int READ_ROWS = 64;  // positions of a workgroup
+
+// N channels from ch on (N divides ch) of a cache row: codes or bf16 bits, as
+// they are loaded.
+template <int D, int FMT, bool KEY, int N>
+struct Piece {
+  static constexpr int WORDS = FMT == KV_BF16 ? N / 2 : KEY ? (FMT == KV_U8 ? N / 4 : 1) : N;
+  uint32_t w[WORDS], st;
+
+  __device__ __forceinline__ void load(const void* base, const uint32_t* stat, int64_t ph, int group, int page_len,
+                                       int place, int ch) {
+    const int64_t row = ph * page_len + place;
+    if constexpr (FMT == KV_BF16) {
+      const uint16_t* at = static_cast<const uint16_t*>(base) + row * D + ch;
+      if constexpr (N == 8) {
+        const uint4 v = *reinterpret_cast<const uint4*>(at);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+      } else {
+        const uint2 v = *reinterpret_cast<const uint2*>(at);
+        w[0] = v.x; w[1] = v.y;
+      }
+      st = 0;
+      return;
+    } else {
+      constexpr int ROW = FMT == KV_U8 ? D : D / 2;
+      const uint8_t* at = static_cast<const uint8_t*>(base) + row * ROW;
+      if constexpr (KEY) {
+        const int run = ch / 8 % 4 * (D / 4) + 8 * (ch / 32);
+        if constexpr (FMT == KV_U8) {
+          const uint32_t* v = reinterpret_cast<const uint32_t*>(at + run + ch % 8);
+#pragma unroll
+          for (int i = 0; i < WORDS; ++i) w[i] = v[i];
+        } else {
+          w[0] = *reinterpret_cast<const uint32_t*>(at + run / 2);
+          if (ch % 8) w[0] >>= 8;  // channels 4..7 of the run
+        }
+      } else {
+        const int first = ch % 16 * (D / 16) + ch / 16;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int p = first + i * (D / 16);
+          w[i] = FMT == KV_U8 ? at[p] : at[p / 2] >> (4 * (p & 1));
+        }
+      }
+      st = stat[(ph * (D / group) + ch / group) * page_len + place];
+    }
+  }
+
+  __device__ __forceinline__ float value(int i) const {
+    if constexpr (FMT == KV_BF16) return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+    uint32_t c;
+    if constexpr (!KEY)
+      c = w[i % WORDS];
+    else if constexpr (FMT == KV_U8)
+      c = w[i / 4 % WORDS] >> (8 * (i & 3));
+    else
+      c = w[0] >> (4 * (i / 2) + 16 * (i & 1));
+    return __uint_as_float(st & 0xFFFF0000u) + __uint_as_float(st << 16) * float(c & (FMT == KV_U8 ? 255u : 15u));
+  }
+};
+
+template <int D, int FMT, bool F32, bool KEY>
+__device__ __forceinline__ void read_rows(const KvReadLaunch& p, void* out, int64_t run, int64_t s, int h, int64_t i0) {
+  constexpr int N = F32 ? 4 : 8, LANES = D / N, PAR = 256 / LANES, ITER = READ_ROWS / PAR, AT_ONCE = ITER < 4 ? ITER : 4;
+  const KvCache& c = p.c;
+  const int ch = threadIdx.x % LANES * N, row = threadIdx.x / LANES;
+  const int64_t start = p.start ? p.start[s] : 0;
+  const int64_t end = p.lens[s] < c.max_pages << c.log_page ? int64_t(p.lens[s]) : c.max_pages << c.log_page;
+  for (int k = 0; k < ITER; k += AT_ONCE) {
+    Piece<D, FMT, KEY, N> x[AT_ONCE];
+    bool is[AT_ONCE];
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int64_t i = i0 + row + (k + j) * PAR, pos = start + i;
+      int page = -1;
+      if (i < p.L && pos >= 0 && pos < end) page = kv_page(c, s, int(pos));
+      is[j] = page >= 0;
+      if (is[j])
+        x[j].load(KEY ? c.k : c.v, reinterpret_cast<const uint32_t*>(KEY ? c.k_stat : c.v_stat),
+                  int64_t(page) * c.H_kv + h, c.group, c.page_len, int(pos) & (c.page_len - 1), ch);
+    }
+#pragma unroll
+    for (int j = 0; j < AT_ONCE; ++j) {
+      const int64_t i = i0 + row + (k + j) * PAR;
+      if (i >= p.L) break;
+      float v[N];
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = is[j] ? x[j].value(e) : 0.0f;
+      const int64_t o = (run + i) * D + ch;
+      if constexpr (F32)
+        *reinterpret_cast<float4*>(static_cast<float*>(out) + o) = make_float4(v[0], v[1], v[2], v[3]);
+      else
+        store8<BF16>(out, o, v);
+    }
+  }
 }
 
-template <int D>
+template <int D, int FMT, bool F32>
 __global__ __launch_bounds__(256) void kv_read_kernel(KvReadLaunch p) {
-  const KvCache& c = p.c;
-  const int l = threadIdx.x & 15;
-  const int64_t vec = int64_t(blockIdx.x) * 16 + (threadIdx.x >> 4);  // (h, s, i)
-  if (vec >= c.H_kv * c.n_seq * p.L) return;
-  const int64_t i = vec % p.L, s = vec / p.L % c.n_seq;
-  const int h = int(vec / p.L / c.n_seq);
-  const int64_t pos = i + (p.start ? p.start[s] : 0);
-  int page = -1;
-  if (pos >= 0 && pos < p.lens[s] && pos < c.max_pages << c.log_page) page = kv_page(c, s, int(pos));
-  for (int side = 0; side < 2; ++side) {
-    void* out = side ? p.V : p.K;
-    if (!out) continue;
-#pragma unroll
-    for (int e = 0; e < D / 16; ++e) {
-      const int ch = l + 16 * e;
-      const float x = page < 0 ? 0.0f
-                               : kv_value<D>(c, side == 0, int64_t(page) * c.H_kv + h, int(pos) & (c.page_len - 1), ch);
-      if (p.out_dtype == F32)
-        static_cast<float*>(out)[vec * D + ch] = x;
-      else
-        static_cast<uint16_t*>(out)[vec * D + ch] = to_bf16(x);
-    }
+  const int64_t per = (p.L + READ_ROWS - 1) / READ_ROWS;
+  const int64_t hs = workgroup() / per, i0 = workgroup() % per * READ_ROWS;  // (head, sequence), first position
+  if (hs >= p.c.H_kv * p.c.n_seq) return;
+  const int64_t s = hs % p.c.n_seq;
+  const int h = int(hs / p.c.n_seq);
+  if (p.K) read_rows<D, FMT, F32, true>(p, p.K, hs * p.L, s, h, i0);
+  if (p.V) read_rows<D, FMT, F32, false>(p, p.V, hs * p.L, s, h, i0);
+}
+
+}  // namespace
+
+namespace {
+
+template <int D, int FMT, bool F32>
+void append_form(const KvAppendLaunch& p, hipStream_t st) {
+  constexpr int SLOTS = 256 * 16 / D;
+  const int plain = (p.q ? p.H : 0) + p.c.H_kv * (FMT == KV_BF16 ? 2 : 1);
+  const int tiles = (plain + SLOTS - 1) / SLOTS + (FMT == KV_BF16 ? 0 : (p.c.H_kv + 15) / 16);
+  // few rows: a workgroup for every tile of heads
+  dim3 grid = grid_of(p.T);
+  grid.z = p.T < 512 ? unsigned(tiles) : 1u;
+  kv_append_kernel<D, FMT, F32><<<grid, 256, 0, st>>>(p);
+}
+template <int D>
+void append_d(const KvAppendLaunch& p, hipStream_t st) {
+  const bool f32 = p.in_dtype == F32;
+  switch (p.c.format) {
+    case KV_BF16: return f32 ? append_form<D, KV_BF16, true>(p, st) : append_form<D, KV_BF16, false>(p, st);
+    case KV_U8: return f32 ? append_form<D, KV_U8, true>(p, st) : append_form<D, KV_U8, false>(p, st);
+    default: return f32 ? append_form<D, KV_U4, true>(p, st) : append_form<D, KV_U4, false>(p, st);
+  }
+}
+
+template <int D, int FMT>
+void read_form(const KvReadLaunch& p, hipStream_t st) {
+  const dim3 grid = grid_of(p.c.H_kv * p.c.n_seq * ((p.L + READ_ROWS - 1) / READ_ROWS));
+  if (p.out_dtype == F32)
+    kv_read_kernel<D, FMT, true><<<grid, 256, 0, st>>>(p);
+  else
+    kv_read_kernel<D, FMT, false><<<grid, 256, 0, st>>>(p);
+}
+template <int D>
+void read_d(const KvReadLaunch& p, hipStream_t st) {
+  switch (p.c.format) {
+    case KV_BF16: return read_form<D, KV_BF16>(p, st);
+    case KV_U8: return read_form<D, KV_U8>(p, st);
+    default: return read_form<D, KV_U4>(p, st);
   }
 }
 
 }  // namespace
 
 hipError_t launch_kv_append(const KvAppendLaunch& p, hipStream_t st) {
-  const int64_t n = p.T * ((p.q ? p.H : 0) + 2 * p.c.H_kv);
-  const dim3 grid{unsigned((n + 15) / 16)};
   if (p.c.d == 128)
-    kv_append_kernel<128><<<grid, 256, 0, st>>>(p);
+    append_d<128>(p, st);
   else
-    kv_append_kernel<64><<<grid, 256, 0, st>>>(p);
+    append_d<64>(p, st);
   return hipGetLastError();
 }
 
 hipError_t launch_kv_read(const KvReadLaunch& p, hipStream_t st) {
-  const int64_t n = p.c.H_kv * p.c.n_seq * p.L;
-  const dim3 grid{unsigned((n + 15) / 16)};
   if (p.c.d == 128)
-    kv_read_kernel<128><<<grid, 256, 0, st>>>(p);
+    read_d<128>(p, st);
   else
-    kv_read_kernel<64><<<grid, 256, 0, st>>>(p);
+    read_d<64>(p, st);
   return hipGetLastError();
 }
 

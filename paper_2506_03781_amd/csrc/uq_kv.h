@@ -9,6 +9,14 @@
 
 namespace uq {
 
+// Grid of n workgroups, n up to 2^35 (a dimension's work items count in 32
+// bits), and the number of the running one, which may be n or more.
+inline dim3 grid_of(int64_t n) {
+  const int64_t x = n < (int64_t(1) << 20) ? n : int64_t(1) << 20;
+  return dim3(unsigned(x), unsigned((n + x - 1) / x));
+}
+__device__ __forceinline__ int64_t workgroup() { return int64_t(blockIdx.y) * gridDim.x + blockIdx.x; }
+
 // Page that holds position pos of sequence s, or -1: pos is in
 // [0, max_pages page_len), and the table's entry may be anything.
 __device__ __forceinline__ int kv_page(const KvCache& c, int64_t s, int pos) {
