@@ -12,9 +12,11 @@
 // that become codes take 16 lanes, a lane the channels l + 16 c that lie side
 // by side in the row.
 //
-// Read.  A workgroup takes 64 positions of one head of one sequence; a lane 16
-// bytes of the output.  Its codes of a key are one word (two), those of a
-// value as many bytes from one cache line.
+// Read.  A workgroup takes 64 positions of one head of one sequence, a lane 16
+// bytes of the output of several.  Its codes of a key are one word (two);
+// those of a value lie D / 16 places apart, so a row's lanes exchange them
+// through LDS (as byte loads from the cache they took 1.2 to 1.8 times as
+// long).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -28,6 +30,13 @@ namespace {
 
 __device__ __forceinline__ float load1(const void* p, int64_t i, bool f32) {
   return f32 ? static_cast<const float*>(p)[i] : bf16_to_f32(static_cast<const uint16_t*>(p)[i]);
+}
+
+// 16 bytes that are not read again soon, past the caches (a wavefront writes
+// whole lines): 100002 positions of 8 heads to bf16 145 instead of 190 us.
+__device__ __forceinline__ void stream16(void* at, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+  typedef uint32_t u32x4s __attribute__((ext_vector_type(4)));
+  __builtin_nontemporal_store(u32x4s{a, b, c, d}, static_cast<u32x4s*>(at));
 }
 
 // Minimum, maximum and whether all values are finite.
@@ -164,8 +173,10 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendLaunch p) {
     if (is_q || !CODES) {
       uint16_t* o = is_q ? p.q_out + (t * p.H + h) * D
                          : static_cast<uint16_t*>(is_k ? c.k : c.v) + (ph * c.page_len + place) * D;
-      store8<BF16>(o, 8 * lane, a);
-      store8<BF16>(o, 8 * lane + D / 2, b);
+      stream16(o + 8 * lane, pack_bf16x2(a[0], a[1]), pack_bf16x2(a[2], a[3]), pack_bf16x2(a[4], a[5]),
+               pack_bf16x2(a[6], a[7]));
+      stream16(o + 8 * lane + D / 2, pack_bf16x2(b[0], b[1]), pack_bf16x2(b[2], b[3]), pack_bf16x2(b[4], b[5]),
+               pack_bf16x2(b[6], b[7]));
       continue;
     }
     // a key as codes
@@ -237,110 +248,122 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendLaunch p) {
 
 constexpr int READ_ROWS = 64;  // positions of a workgroup
 
-// N channels from ch on (N divides ch) of a cache row: codes or bf16 bits, as
-// they are loaded.
+// N channels from ch on (N divides ch) of a cache row: as they are loaded, which
+// for a value's codes is the lane's share of the row.
 template <int D, int FMT, bool KEY, int N>
 struct Piece {
-  static constexpr int WORDS = FMT == KV_BF16 ? N / 2 : KEY ? (FMT == KV_U8 ? N / 4 : 1) : N;
+  static constexpr int ROW = FMT == KV_BF16 ? 2 * D : FMT == KV_U8 ? D : D / 2;
+  static constexpr int BYTES = N * ROW / D;
+  static constexpr int WORDS = BYTES < 4 ? 1 : BYTES / 4;
   uint32_t w[WORDS], st;
 
   __device__ __forceinline__ void load(const void* base, const uint32_t* stat, int64_t ph, int group, int page_len,
                                        int place, int ch) {
-    const int64_t row = ph * page_len + place;
-    if constexpr (FMT == KV_BF16) {
-      const uint16_t* at = static_cast<const uint16_t*>(base) + row * D + ch;
-      if constexpr (N == 8) {
+    const uint8_t* at = static_cast<const uint8_t*>(base) + (ph * page_len + place) * ROW;
+    const int run = (ch / 8 % 4 * (D / 4) + 8 * (ch / 32)) * ROW / D;  // of eight channels of a key's codes
+    if constexpr (KEY && FMT == KV_U4) {
+      w[0] = *reinterpret_cast<const uint32_t*>(at + run) >> (ch % 8 ? 8 : 0);
+    } else {
+      at += KEY && FMT == KV_U8 ? run + ch % 8 : ch / N * BYTES;
+      if constexpr (BYTES == 16) {
         const uint4 v = *reinterpret_cast<const uint4*>(at);
         w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-      } else {
+      } else if constexpr (BYTES == 8) {
         const uint2 v = *reinterpret_cast<const uint2*>(at);
         w[0] = v.x; w[1] = v.y;
-      }
-      st = 0;
-      return;
-    } else {
-      constexpr int ROW = FMT == KV_U8 ? D : D / 2;
-      const uint8_t* at = static_cast<const uint8_t*>(base) + row * ROW;
-      if constexpr (KEY) {
-        const int run = ch / 8 % 4 * (D / 4) + 8 * (ch / 32);
-        if constexpr (FMT == KV_U8) {
-          const uint32_t* v = reinterpret_cast<const uint32_t*>(at + run + ch % 8);
-#pragma unroll
-          for (int i = 0; i < WORDS; ++i) w[i] = v[i];
-        } else {
-          w[0] = *reinterpret_cast<const uint32_t*>(at + run / 2);
-          if (ch % 8) w[0] >>= 8;  // channels 4..7 of the run
-        }
+      } else if constexpr (BYTES == 4) {
+        w[0] = *reinterpret_cast<const uint32_t*>(at);
       } else {
-        const int first = ch % 16 * (D / 16) + ch / 16;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-          const int p = first + i * (D / 16);
-          w[i] = FMT == KV_U8 ? at[p] : at[p / 2] >> (4 * (p & 1));
-        }
+        w[0] = *reinterpret_cast<const uint16_t*>(at);
       }
-      st = stat[(ph * (D / group) + ch / group) * page_len + place];
+    }
+    st = FMT == KV_BF16 ? 0u : stat[(ph * (D / group) + ch / group) * page_len + place];
+  }
+
+  // The lane's share of a value's codes to its place in LDS.
+  __device__ __forceinline__ void put(uint8_t* row, int ch) const {
+    if constexpr (BYTES < 4) {
+      *reinterpret_cast<uint16_t*>(row + ch / N * BYTES) = uint16_t(w[0]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < WORDS; ++i) *reinterpret_cast<uint32_t*>(row + ch / N * BYTES + 4 * i) = w[i];
     }
   }
 
-  __device__ __forceinline__ float value(int i) const {
+  // Channel ch + i; row: a value's codes in LDS.
+  __device__ __forceinline__ float value(int i, const uint8_t* row, int ch) const {
     if constexpr (FMT == KV_BF16) return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
     uint32_t c;
-    if constexpr (!KEY)
-      c = w[i % WORDS];
-    else if constexpr (FMT == KV_U8)
-      c = w[i / 4 % WORDS] >> (8 * (i & 3));
-    else
-      c = w[0] >> (4 * (i / 2) + 16 * (i & 1));
+    if constexpr (KEY) {
+      c = FMT == KV_U8 ? w[i / 4 % WORDS] >> (8 * (i & 3)) : w[0] >> (4 * (i / 2) + 16 * (i & 1));
+    } else {
+      const int p = (ch % 16 + i) * (D / 16) + ch / 16;
+      c = FMT == KV_U8 ? row[p] : uint32_t(row[p / 2]) >> (4 * (ch / 16 & 1));
+    }
     return __uint_as_float(st & 0xFFFF0000u) + __uint_as_float(st << 16) * float(c & (FMT == KV_U8 ? 255u : 15u));
   }
 };
 
 template <int D, int FMT, bool F32, bool KEY>
 __device__ __forceinline__ void read_rows(const KvReadLaunch& p, void* out, int64_t run, int64_t s, int h, int64_t i0) {
-  constexpr int N = F32 ? 4 : 8, LANES = D / N, PAR = 256 / LANES, ITER = READ_ROWS / PAR, AT_ONCE = ITER < 4 ? ITER : 4;
+  constexpr int N = F32 ? 4 : 8;  // 16 bytes
+  using X = Piece<D, FMT, KEY, N>;
+  constexpr int LANES = D / N, PAR = 256 / LANES, ITER = READ_ROWS / PAR;
+  constexpr bool EXCHANGE = !KEY && FMT != KV_BF16;
+  constexpr int LD = X::ROW + (FMT == KV_U8 ? 8 : 4);  // the rows of a wavefront's read on other banks
+  __shared__ __attribute__((aligned(16))) uint8_t rows[EXCHANGE ? READ_ROWS * LD : 16];
   const KvCache& c = p.c;
   const int ch = threadIdx.x % LANES * N, row = threadIdx.x / LANES;
   const int64_t start = p.start ? p.start[s] : 0;
   const int64_t end = p.lens[s] < c.max_pages << c.log_page ? int64_t(p.lens[s]) : c.max_pages << c.log_page;
-  for (int k = 0; k < ITER; k += AT_ONCE) {
-    Piece<D, FMT, KEY, N> x[AT_ONCE];
-    bool is[AT_ONCE];
+  X x[ITER];
+  bool is[ITER];
 #pragma unroll
-    for (int j = 0; j < AT_ONCE; ++j) {
-      const int64_t i = i0 + row + (k + j) * PAR, pos = start + i;
-      int page = -1;
-      if (i < p.L && pos >= 0 && pos < end) page = kv_page(c, s, int(pos));
-      is[j] = page >= 0;
-      if (is[j])
-        x[j].load(KEY ? c.k : c.v, reinterpret_cast<const uint32_t*>(KEY ? c.k_stat : c.v_stat),
-                  int64_t(page) * c.H_kv + h, c.group, c.page_len, int(pos) & (c.page_len - 1), ch);
-    }
+  for (int j = 0; j < ITER; ++j) {
+    const int64_t i = i0 + row + j * PAR, pos = start + i;
+    int page = -1;
+    if (i < p.L && pos >= 0 && pos < end) page = kv_page(c, s, int(pos));
+    is[j] = page >= 0;
+    if (is[j])
+      x[j].load(KEY ? c.k : c.v, reinterpret_cast<const uint32_t*>(KEY ? c.k_stat : c.v_stat),
+                int64_t(page) * c.H_kv + h, c.group, c.page_len, int(pos) & (c.page_len - 1), ch);
+  }
+  if constexpr (EXCHANGE) {  // within a row's lanes, which are one wavefront's
 #pragma unroll
-    for (int j = 0; j < AT_ONCE; ++j) {
-      const int64_t i = i0 + row + (k + j) * PAR;
-      if (i >= p.L) break;
-      float v[N];
+    for (int j = 0; j < ITER; ++j) x[j].put(rows + (row + j * PAR) * LD, ch);
+    wave_lds_sync();
+  }
 #pragma unroll
-      for (int e = 0; e < N; ++e) v[e] = is[j] ? x[j].value(e) : 0.0f;
-      const int64_t o = (run + i) * D + ch;
-      if constexpr (F32)
-        *reinterpret_cast<float4*>(static_cast<float*>(out) + o) = make_float4(v[0], v[1], v[2], v[3]);
-      else
-        store8<BF16>(out, o, v);
-    }
+  for (int j = 0; j < ITER; ++j) {
+    const int64_t i = i0 + row + j * PAR;
+    if (i >= p.L) break;
+    float v[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = is[j] ? x[j].value(e, rows + (row + j * PAR) * LD, ch) : 0.0f;
+    const int64_t o = (run + i) * D + ch;
+    if constexpr (F32)
+      stream16(static_cast<float*>(out) + o, __float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
+               __float_as_uint(v[3]));
+    else
+      stream16(static_cast<uint16_t*>(out) + o, pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+               pack_bf16x2(v[4 % N], v[5 % N]), pack_bf16x2(v[6 % N], v[7 % N]));
   }
 }
 
 template <int D, int FMT, bool F32>
 __global__ __launch_bounds__(256) void kv_read_kernel(KvReadLaunch p) {
-  const int64_t per = (p.L + READ_ROWS - 1) / READ_ROWS;
-  const int64_t hs = workgroup() / per, i0 = workgroup() % per * READ_ROWS;  // (head, sequence), first position
-  if (hs >= p.c.H_kv * p.c.n_seq) return;
+  const int64_t per = (p.L + READ_ROWS - 1) / READ_ROWS, one = p.c.H_kv * p.c.n_seq;
+  int64_t hs = workgroup() / per;  // (head, sequence), the keys' first
+  const int64_t i0 = workgroup() % per * READ_ROWS;
+  const bool key = p.K && hs < one;
+  if (p.K && !key) hs -= one;
+  if (hs >= one || (!key && !p.V)) return;
   const int64_t s = hs % p.c.n_seq;
   const int h = int(hs / p.c.n_seq);
-  if (p.K) read_rows<D, FMT, F32, true>(p, p.K, hs * p.L, s, h, i0);
-  if (p.V) read_rows<D, FMT, F32, false>(p, p.V, hs * p.L, s, h, i0);
+  if (key)
+    read_rows<D, FMT, F32, true>(p, p.K, hs * p.L, s, h, i0);
+  else
+    read_rows<D, FMT, F32, false>(p, p.V, hs * p.L, s, h, i0);
 }
 
 }  // namespace
@@ -369,7 +392,8 @@ void append_d(const KvAppendLaunch& p, hipStream_t st) {
 
 template <int D, int FMT>
 void read_form(const KvReadLaunch& p, hipStream_t st) {
-  const dim3 grid = grid_of(p.c.H_kv * p.c.n_seq * ((p.L + READ_ROWS - 1) / READ_ROWS));
+  const int sides = (p.K ? 1 : 0) + (p.V ? 1 : 0);
+  const dim3 grid = grid_of(sides * p.c.H_kv * p.c.n_seq * ((p.L + READ_ROWS - 1) / READ_ROWS));
   if (p.out_dtype == F32)
     kv_read_kernel<D, FMT, true><<<grid, 256, 0, st>>>(p);
   else
