@@ -12,8 +12,8 @@
 // that become codes take 16 lanes, a lane the channels l + 16 c that lie side
 // by side in the row.
 //
-// Read.  A workgroup takes 64 positions of one head of one sequence, a lane 16
-// bytes of the output of several.  Its codes of a key are one word (two);
+// Read.  A wavefront takes 16 positions of one head of one sequence, which lie
+// on two pages at most, a lane 16 bytes of the output of several.  Its codes of a key are one word (two);
 // those of a value lie D / 16 places apart, so a row's lanes exchange them
 // through LDS (as byte loads from the cache they took 1.2 to 1.8 times as
 // long).
@@ -246,7 +246,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendLaunch p) {
   }
 }
 
-constexpr int READ_ROWS = 64;  // positions of a workgroup
+constexpr int WAVE_ROWS = 16;  // positions of a wavefront
 
 // N channels from ch on (N divides ch) of a cache row: as they are loaded, which
 // for a value's codes is the lane's share of the row.
@@ -257,9 +257,10 @@ struct Piece {
   static constexpr int WORDS = BYTES < 4 ? 1 : BYTES / 4;
   uint32_t w[WORDS], st;
 
-  __device__ __forceinline__ void load(const void* base, const uint32_t* stat, int64_t ph, int group, int page_len,
-                                       int place, int ch) {
-    const uint8_t* at = static_cast<const uint8_t*>(base) + (ph * page_len + place) * ROW;
+  // at, stat: of the head in its page; lane_stat: of the channels' group there.
+  __device__ __forceinline__ void load(const uint8_t* at, const uint32_t* stat, uint32_t place, uint32_t lane_stat,
+                                       int ch) {
+    at += place * ROW;
     const int run = (ch / 8 % 4 * (D / 4) + 8 * (ch / 32)) * ROW / D;  // of eight channels of a key's codes
     if constexpr (KEY && FMT == KV_U4) {
       w[0] = *reinterpret_cast<const uint32_t*>(at + run) >> (ch % 8 ? 8 : 0);
@@ -277,7 +278,7 @@ struct Piece {
         w[0] = *reinterpret_cast<const uint16_t*>(at);
       }
     }
-    st = FMT == KV_BF16 ? 0u : stat[(ph * (D / group) + ch / group) * page_len + place];
+    st = FMT == KV_BF16 ? 0u : stat[lane_stat + place];
   }
 
   // The lane's share of a value's codes to its place in LDS.
@@ -308,58 +309,85 @@ template <int D, int FMT, bool F32, bool KEY>
 __device__ __forceinline__ void read_rows(const KvReadLaunch& p, void* out, int64_t run, int64_t s, int h, int64_t i0) {
   constexpr int N = F32 ? 4 : 8;  // 16 bytes
   using X = Piece<D, FMT, KEY, N>;
-  constexpr int LANES = D / N, PAR = 256 / LANES, ITER = READ_ROWS / PAR;
+  constexpr int LANES = D / N, PAR = 64 / LANES, ITER = WAVE_ROWS / PAR;
   constexpr bool EXCHANGE = !KEY && FMT != KV_BF16;
   constexpr int LD = X::ROW + (FMT == KV_U8 ? 8 : 4);  // the rows of a wavefront's read on other banks
-  __shared__ __attribute__((aligned(16))) uint8_t rows[EXCHANGE ? READ_ROWS * LD : 16];
+  __shared__ __attribute__((aligned(16))) uint8_t rows[EXCHANGE ? 4 * WAVE_ROWS * LD : 16];
   const KvCache& c = p.c;
-  const int ch = threadIdx.x % LANES * N, row = threadIdx.x / LANES;
-  const int64_t start = p.start ? p.start[s] : 0;
-  const int64_t end = p.lens[s] < c.max_pages << c.log_page ? int64_t(p.lens[s]) : c.max_pages << c.log_page;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int ch = lane % LANES * N, row = lane / LANES;
+  const int64_t first = (p.start ? p.start[s] : 0) + i0;  // the wavefront's first position
+  const int64_t cap = c.max_pages << c.log_page;
+  const int64_t end = p.lens[s] < cap ? int64_t(p.lens[s]) : cap;
+  // rows [r0, r1) exist, those below cut on the first page, the others on the second
+  const int r0 = int(first < 0 ? (first < -WAVE_ROWS ? WAVE_ROWS : -first) : 0);
+  const int r1 = int(end - first < 0 ? 0 : end - first < WAVE_ROWS ? end - first : WAVE_ROWS);
+  const int64_t from = first < 0 ? 0 : first;
+  const int place = int(from & (c.page_len - 1)) - r0, cut = c.page_len - place;
+  int page[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int64_t pos = (from >> c.log_page << c.log_page) + k * c.page_len;
+    page[k] = r0 < r1 && pos < end ? kv_page(c, s, int(pos)) : -1;
+  }
+  const uint32_t rows_of_page = uint32_t(c.H_kv) * uint32_t(c.page_len);
+  const uint32_t stats = FMT == KV_BF16 ? 0u : uint32_t(D / c.group);
+  const uint32_t lane_stat = FMT == KV_BF16 ? 0u : uint32_t(ch / c.group) * c.page_len;
+  const uint8_t* at[2];
+  const uint32_t* stat[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const uint64_t pg = page[k] < 0 ? 0u : uint32_t(page[k]);
+    at[k] = static_cast<const uint8_t*>(KEY ? c.k : c.v) + pg * (rows_of_page * X::ROW) + uint32_t(h) * c.page_len * X::ROW;
+    stat[k] = reinterpret_cast<const uint32_t*>(KEY ? c.k_stat : c.v_stat) + pg * (rows_of_page * stats) +
+              uint32_t(h) * stats * c.page_len;
+  }
   X x[ITER];
   bool is[ITER];
 #pragma unroll
   for (int j = 0; j < ITER; ++j) {
-    const int64_t i = i0 + row + j * PAR, pos = start + i;
-    int page = -1;
-    if (i < p.L && pos >= 0 && pos < end) page = kv_page(c, s, int(pos));
-    is[j] = page >= 0;
+    const int r = j * PAR + row;
+    const bool second = r >= cut;
+    is[j] = r >= r0 && r < r1 && (second ? page[1] : page[0]) >= 0;
     if (is[j])
-      x[j].load(KEY ? c.k : c.v, reinterpret_cast<const uint32_t*>(KEY ? c.k_stat : c.v_stat),
-                int64_t(page) * c.H_kv + h, c.group, c.page_len, int(pos) & (c.page_len - 1), ch);
+      x[j].load(second ? at[1] : at[0], second ? stat[1] : stat[0], uint32_t(second ? r - cut : place + r), lane_stat, ch);
   }
-  if constexpr (EXCHANGE) {  // within a row's lanes, which are one wavefront's
+  uint8_t* mine = rows + (EXCHANGE ? (wave * WAVE_ROWS + row) * LD : 0);
+  if constexpr (EXCHANGE) {  // within a row's lanes
 #pragma unroll
-    for (int j = 0; j < ITER; ++j) x[j].put(rows + (row + j * PAR) * LD, ch);
+    for (int j = 0; j < ITER; ++j) x[j].put(mine + j * PAR * LD, ch);
     wave_lds_sync();
   }
+  const int64_t o = (run + i0 + row) * D + ch;
+  const int left = int(p.L - i0 < WAVE_ROWS ? p.L - i0 : WAVE_ROWS);
 #pragma unroll
   for (int j = 0; j < ITER; ++j) {
-    const int64_t i = i0 + row + j * PAR;
-    if (i >= p.L) break;
+    if (j * PAR + row >= left) break;
     float v[N];
 #pragma unroll
-    for (int e = 0; e < N; ++e) v[e] = is[j] ? x[j].value(e, rows + (row + j * PAR) * LD, ch) : 0.0f;
-    const int64_t o = (run + i) * D + ch;
+    for (int e = 0; e < N; ++e) v[e] = is[j] ? x[j].value(e, mine + j * PAR * LD, ch) : 0.0f;
     if constexpr (F32)
-      stream16(static_cast<float*>(out) + o, __float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]),
-               __float_as_uint(v[3]));
+      stream16(static_cast<float*>(out) + o + j * PAR * D, __float_as_uint(v[0]), __float_as_uint(v[1]),
+               __float_as_uint(v[2]), __float_as_uint(v[3]));
     else
-      stream16(static_cast<uint16_t*>(out) + o, pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
+      stream16(static_cast<uint16_t*>(out) + o + j * PAR * D, pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
                pack_bf16x2(v[4 % N], v[5 % N]), pack_bf16x2(v[6 % N], v[7 % N]));
   }
 }
 
 template <int D, int FMT, bool F32>
 __global__ __launch_bounds__(256) void kv_read_kernel(KvReadLaunch p) {
-  const int64_t per = (p.L + READ_ROWS - 1) / READ_ROWS, one = p.c.H_kv * p.c.n_seq;
-  int64_t hs = workgroup() / per;  // (head, sequence), the keys' first
-  const int64_t i0 = workgroup() % per * READ_ROWS;
+  // wavefront's (side, head, sequence, 16 positions), the keys first; fewer than 2^30 of them
+  const uint32_t per = uint32_t((p.L + WAVE_ROWS - 1) / WAVE_ROWS), n_seq = uint32_t(p.c.n_seq);
+  const uint32_t one = uint32_t(p.c.H_kv) * n_seq;
+  const uint32_t unit = uint32_t(workgroup()) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t hs = unit / per;
+  const int64_t i0 = int64_t(unit % per) * WAVE_ROWS;
   const bool key = p.K && hs < one;
   if (p.K && !key) hs -= one;
   if (hs >= one || (!key && !p.V)) return;
-  const int64_t s = hs % p.c.n_seq;
-  const int h = int(hs / p.c.n_seq);
+  const int h = int(hs / n_seq);
+  const int64_t s = hs % n_seq;
   if (key)
     read_rows<D, FMT, F32, true>(p, p.K, hs * p.L, s, h, i0);
   else
@@ -393,7 +421,8 @@ void append_d(const KvAppendLaunch& p, hipStream_t st) {
 template <int D, int FMT>
 void read_form(const KvReadLaunch& p, hipStream_t st) {
   const int sides = (p.K ? 1 : 0) + (p.V ? 1 : 0);
-  const dim3 grid = grid_of(sides * p.c.H_kv * p.c.n_seq * ((p.L + READ_ROWS - 1) / READ_ROWS));
+  const int64_t units = sides * p.c.H_kv * p.c.n_seq * ((p.L + WAVE_ROWS - 1) / WAVE_ROWS);
+  const dim3 grid = grid_of((units + 3) / 4);
   if (p.out_dtype == F32)
     kv_read_kernel<D, FMT, true><<<grid, 256, 0, st>>>(p);
   else
