@@ -759,7 +759,8 @@ uq_status uniquan_bcq_matmul(int T, int64_t R, int64_t C, int k, int g,
  *   c     = rint((x - lo) fl(1 / scale)), at most top; 0 where scale is 0
  * so every value comes back to within half a scale.  A group with a
  * non-finite value, or whose max x - lo overflows, gets NaN for scale and lo
- * and comes back as NaN.
+ * and comes back as NaN.  (The attention takes a value one of whose groups is
+ * NaN as NaN in every channel.)
  * A page id outside [0, n_pages) is no page (-1: not allocated, or evicted):
  * nothing is written there and its positions take no part in an attention.
  * Sequences may share pages that are only read.  Two rows of one append must
@@ -768,7 +769,7 @@ uq_status uniquan_bcq_matmul(int T, int64_t R, int64_t C, int k, int g,
  * Rules shared by the three calls.  d is 64 or 128 (UQ_EUNSUPPORTED
  * otherwise); group is 0 for UQ_KV_BF16, else 32 or d; page_len a power of
  * two in [16, 1024]; H a multiple of H_kv <= 4096, head h reading key/value
- * head h / (H / H_kv); max_pages page_len < 2^31.  Cache arrays and fp32/bf16
+ * head h / (H / H_kv); max_pages page_len <= 2^30.  Cache arrays and fp32/bf16
  * rows 16-byte, int32 arrays 4-byte aligned.  k_stat and v_stat are NULL for
  * UQ_KV_BF16.
  */
@@ -825,7 +826,8 @@ uq_status uniquan_kv_read(int64_t n_seq, int H_kv, int d, int64_t L,
  *   row_lse = log2 sum_t 2^(x_t log2 e)   (the base-2 log-sum-exp of
  *                                          uniquan_attn_fwd; may be NULL)
  *   O = sum_t 2^(x_t log2 e - row_lse) v_t
- * in fp32 from the stored values, O rounded to bf16.  Where no position
+ * in fp32 from the stored values, O rounded to bf16 (UQ_KV_U8: scales below
+ * 2^55; what is below 2^-50 of a value may be lost).  Where no position
  * takes part O is 0 and row_lse -infinity.  What the cache holds at other
  * positions has no influence, whatever it is.  Long sequences are split over
  * workgroups and joined in a fixed order, so results do not change from run
@@ -833,11 +835,11 @@ uq_status uniquan_kv_read(int64_t n_seq, int H_kv, int d, int64_t L,
  *
  * Q [n_seq] rows of H d bf16, ld_q elements apart (a multiple of 8; 0: H d);
  * O [n_seq] rows of H d bf16, ld_o elements apart (a multiple of 4; 0: H d);
- * row_lse [n_seq x H] fp32.  ws [ws_len] fp32 workspace of at least
- * uniquan_attn_decode_ws(n_seq, H, H_kv, d, max_pages, page_len) floats
- * (16-byte aligned; 0: may be NULL), free to be reused once the call is done;
- * calls that overlap need one each.  n_seq H <= 2^24, n_seq (max_pages page_len
- * + 256) <= 2^37.
+ * row_lse [n_seq x H] fp32.  The outputs must not overlap Q.  ws [ws_len] fp32
+ * workspace of at least uniquan_attn_decode_ws(n_seq, H, H_kv, d, max_pages,
+ * page_len) floats (16-byte aligned; 0: may be NULL), of any contents, free to
+ * be reused once the call is done; calls that overlap need one each.
+ * n_seq H <= 2^24, n_seq (max_pages page_len + 256) <= 2^37.
  */
 size_t uniquan_attn_decode_ws(int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len);
 uq_status uniquan_attn_decode(int64_t n_seq, int H, int H_kv, int d,

@@ -775,8 +775,8 @@ static uq_status check_cache(const char* fn, uq::KvCache* c, int H_kv, int d, co
   const int64_t lim = int64_t(1) << 31;
   if (n_pages < 1 || n_pages >= lim) return fail(UQ_EINVAL, "%s: n_pages=%lld must be in [1, 2^31)", fn, (long long)n_pages);
   if (n_seq < 1 || n_seq >= lim) return fail(UQ_EINVAL, "%s: n_seq=%lld must be in [1, 2^31)", fn, (long long)n_seq);
-  if (max_pages < 1 || max_pages > (lim - 1) / page_len)
-    return fail(UQ_EINVAL, "%s: max_pages=%lld must be >= 1 and max_pages * page_len < 2^31", fn, (long long)max_pages);
+  if (max_pages < 1 || max_pages > (lim / 2) / page_len)
+    return fail(UQ_EINVAL, "%s: max_pages=%lld must be >= 1 and max_pages * page_len <= 2^30", fn, (long long)max_pages);
   REQ_PTR(pages, 4); REQ_PTR(k_cache, 16); REQ_PTR(v_cache, 16);
   if (format != UQ_KV_BF16) {
     REQ_PTR(k_stat, 16); REQ_PTR(v_stat, 16);

@@ -77,7 +77,7 @@ constexpr float SLACK = 8.0f;               // scores may exceed the reference b
 constexpr int WAVES = 4;
 constexpr int STEP = 32;                    // positions of a wavefront's step
 constexpr int BLOCK = WAVES * STEP;         // positions of a workgroup's round
-constexpr int MIN_COST = 3;                 // least blocks of a share (ends counted)
+constexpr int MIN_COST = 2;                 // least blocks of a share (ends counted)
 constexpr int CUS = 256;
 
 __device__ __forceinline__ f32x4d mfma16(const u32x4d& a, const u32x4d& b, const f32x4d& c) {
@@ -158,6 +158,7 @@ struct Share {
 // sequences, then the run that holds `a` is searched.  With little in all,
 // only the first shares get something, MIN_COST at least.
 __device__ __forceinline__ Share share_of(const AttnDecodeLaunch& p, int at, int want) {
+  if (want == 1) return Share{0, 0x7FFFFFFF, 0, 0};
   const int lane = threadIdx.x & 63;
   const int n = int(p.c.n_seq);
   const int per = (n + 63) / 64;
@@ -172,28 +173,24 @@ __device__ __forceinline__ Share share_of(const AttnDecodeLaunch& p, int at, int
   Share h;
   h.a = at * q + at * r / parts;
   h.b = (at + 1) * q + (at + 1) * r / parts;
-  int in = __builtin_ctzll(__ballot(upto > h.a));
-  int before = __builtin_amdgcn_readlane(upto - mine, in);
-  int first = in * per;
-  if (per > 1) {
-    for (const int end = first + per;; first += 64) {
-      mine = first + lane < end ? cost(first + lane) : 0;
-      upto = wave_scan(mine) + before;
-      const uint64_t past = __ballot(upto > h.a);
-      if (past) {
-        in = __builtin_ctzll(past);
-        break;
-      }
-      before = __builtin_amdgcn_readlane(upto, 63);
+  // the run that holds a (it is below total), then the sequence in it, 64 at a time
+  int in = __builtin_ctzll(__ballot(upto > h.a) | 1ull << 63);
+  h.s = in * per;
+  h.begin = __builtin_amdgcn_readlane(upto - mine, in);
+  if (per == 1) return h;
+  for (const int end = h.s + per; h.s < end; h.s += 64) {
+    mine = h.s + lane < end ? cost(h.s + lane) : 0;
+    upto = wave_scan(mine) + h.begin;
+    const uint64_t past = __ballot(upto > h.a);
+    if (past) {
+      in = __builtin_ctzll(past);
+      h.s += in;
+      h.begin = __builtin_amdgcn_readlane(upto - mine, in);
+      return h;
     }
-    before = __builtin_amdgcn_readlane(upto - mine, in);
-    first += in;
-  } else {
-    first = in;
+    h.begin = __builtin_amdgcn_readlane(upto, 63);
   }
-  h.s = first;
-  h.begin = before;
-  return h;
+  return Share{0, 0, 0, 0};
 }
 
 // A share's part of one sequence: blocks [b0, b1); the sequence's first and
@@ -323,9 +320,14 @@ __device__ __forceinline__ uint32_t value_pair(const uint32_t (&a)[Form<FMT, D>:
 // bf16 pair (lo, hi) of two values, truncated.
 __device__ __forceinline__ uint32_t pair(float lo, float hi) { return top_halves(__float_as_uint(lo), __float_as_uint(hi)); }
 
-// Workgroups a CU holds (their registers are bounded to that).
+// Workgroups a CU holds (their registers are bounded to that): the most for
+// which nothing is spilled in the loop, measured one less and one more.  bf16
+// with 128 channels has room for three and loses by it (7B block, 4 x 2048:
+// 30.0 us against 31.2; 64 x up to 16384 352 against 355); 4-bit groups of 32 46
+// us with three against 40 (100001 positions), 8-bit ones 138 against 90 (48
+// ragged sequences) and, with 64 channels, 55 with four against 50.
 template <int FMT, int D, int NG>
-constexpr int kResident = D == 64 ? 4 : FMT == KV_BF16 || NG > 1 ? 2 : 3;
+constexpr int kResident = D == 64 ? (FMT == KV_U8 && NG > 1 ? 3 : 4) : FMT == KV_BF16 || NG > 1 ? 2 : 3;
 
 // WIDE: 16 query heads a workgroup, else 8 with the weights' rests in the upper columns.
 template <int FMT, int D, int NG, bool WIDE>
@@ -436,7 +438,7 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
   while (next_chunk(p, share, ch)) {
     const int64_t s = ch.s;
     const bool opens = ch.opens, closes = ch.closes;
-    if (want > 1 && g == 0 && rt == 0 && threadIdx.x == 0) {
+    if (p.ws && g == 0 && rt == 0 && threadIdx.x == 0) {
       if (opens) shares_of(p)[s].x = at;
       if (closes) shares_of(p)[s].y = at;
     }
@@ -732,17 +734,20 @@ int row_tiles(int H, int H_kv) {
   return (H / H_kv + r - 1) / r;
 }
 
-// Shares of each key/value head's row tile for `per` workgroups a CU; one where
-// no sequence can be longer than a block's cost, so that none is split.
+// Shares of each key/value head's row tile for `per` workgroups a CU.
 int shares(int64_t n_seq, int H, int H_kv, int64_t max_pages, int page_len, int per) {
   const int64_t most = n_seq * ((max_pages * page_len + BLOCK - 1) / BLOCK + 1) / MIN_COST;
   return int(std::max<int64_t>(1, std::min<int64_t>(most, per * CUS / (int64_t(H_kv) * row_tiles(H, H_kv)))));
 }
+// Whether a sequence can lie in several shares: not where there is one, nor
+// where none is longer than a block.
+bool splits(int want, int64_t max_pages, int page_len) { return want > 1 && max_pages * page_len > BLOCK; }
 
 template <int FMT, int D, int NG>
-hipError_t launch_form(const AttnDecodeLaunch& p, hipStream_t st) {
+hipError_t launch_form(AttnDecodeLaunch p, hipStream_t st) {
   const int rt = row_tiles(p.H, p.c.H_kv);
   const int want = shares(p.c.n_seq, p.H, p.c.H_kv, p.c.max_pages, p.c.page_len, kResident<FMT, D, NG>);
+  if (!splits(want, p.c.max_pages, p.c.page_len)) p.ws = nullptr;
   const int64_t units = (int64_t(want) * p.c.H_kv + 7) / 8 * 8;
   const dim3 grid{unsigned(units * rt)};
   if (p.H / p.c.H_kv > 8)
@@ -750,7 +755,7 @@ hipError_t launch_form(const AttnDecodeLaunch& p, hipStream_t st) {
   else
     attn_decode_kernel<FMT, D, NG, false><<<grid, 256, 0, st>>>(p, want, rt);
   if (hipError_t e = hipGetLastError()) return e;
-  if (want == 1) return hipSuccess;
+  if (!p.ws) return hipSuccess;
   attn_join_kernel<D><<<grid_of(p.c.n_seq * p.H), 512, 0, st>>>(p);
   return hipGetLastError();
 }
@@ -767,7 +772,8 @@ hipError_t launch_d(const AttnDecodeLaunch& p, hipStream_t st) {
 
 size_t attn_decode_ws(int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len) {
   const int64_t want = shares(n_seq, H, H_kv, max_pages, page_len, 4);  // the most of any form
-  return want > 1 ? size_t(n_seq * 2 + 3) / 4 * 4 + size_t(want + n_seq) * size_t(H) * size_t(d + 4) : 0;
+  if (!splits(int(want), max_pages, page_len)) return 0;
+  return size_t(n_seq * 2 + 3) / 4 * 4 + size_t(want + n_seq) * size_t(H) * size_t(d + 4);
 }
 
 hipError_t launch_attn_decode(const AttnDecodeLaunch& p, hipStream_t st) {

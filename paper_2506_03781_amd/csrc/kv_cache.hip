@@ -403,9 +403,11 @@ void append_form(const KvAppendLaunch& p, hipStream_t st) {
   constexpr int SLOTS = 256 * 16 / D;
   const int plain = (p.q ? p.H : 0) + p.c.H_kv * (FMT == KV_BF16 ? 2 : 1);
   const int tiles = (plain + SLOTS - 1) / SLOTS + (FMT == KV_BF16 ? 0 : (p.c.H_kv + 15) / 16);
-  // few rows: a workgroup for every tile of heads
+  // Few rows: a workgroup for every tile of heads (32 + 8 heads at 8 bits, one row 3.0 us against 4.3 with
+  // a workgroup a row, 1024 rows 9.2 against 9.7); many: a row's tiles share its angles (2048 rows 14.8
+  // against 15.9, 4096 29.6 against 32.4).
   dim3 grid = grid_of(p.T);
-  grid.z = p.T < 512 ? unsigned(tiles) : 1u;
+  grid.z = p.T < 1536 ? unsigned(tiles) : 1u;
   kv_append_kernel<D, FMT, F32><<<grid, 256, 0, st>>>(p);
 }
 template <int D>

@@ -130,6 +130,69 @@ def test_non_finite_values_in_use():
     assert np.isfinite(o[2]).all() and bool(torch.isfinite(lse[1:]).all())
 
 
+@pytest.mark.parametrize("fmt,group", [("u8", 32), ("u8", None), ("u4", 32), ("u4", None)])
+def test_groups_that_came_out_nan(fmt, group):
+    """A key or value with a non-finite group: NaN in every channel of its head's rows, as the header states, and
+    nowhere else; the same groups behind the length change nothing."""
+    rs = np.random.default_rng(21)
+    lens = [40, 40, 40, 33]
+    c = filled(rs, lens, 2, 128, 16, fmt, group)
+    q = rounded(rs, 4, 4, 128)
+    for s, p, stat in ((0, 20, c.k_stat), (1, 39, c.v_stat), (2, 40, c.v_stat), (3, 33, c.k_stat)):
+        stat[c.page(s, p), 1, -1, p % 16] = 0x7FC0
+    O, lse = attend(c, on_device(c), q, lens, 0.09)
+    o = O.float().cpu().numpy().reshape(4, 4, 128)
+    assert np.isnan(o[0, 2:]).all() and np.isnan(o[1, 2:]).all()
+    assert np.isnan(lse[0, 2:].cpu().numpy()).all() and bool(torch.isfinite(lse[1]).all())
+    o[0, 2:], o[1, 2:] = 0, 0
+    assert np.isfinite(o).all() and bool(torch.isfinite(lse[2:]).all())
+
+
+@pytest.mark.parametrize("fmt,group", FORMS)
+@pytest.mark.parametrize("kmag,vmag", [(1e10, 1e12), (1e-10, 1e-12), (1.0, 3e14), (1e15, 1.0)])
+def test_magnitudes(fmt, group, kmag, vmag):
+    """Keys, values and queries of other magnitudes, with scores of order one: fp32 and bf16 have the range."""
+    rs = np.random.default_rng(22)
+    c = KV.Cache(8, 1, 128, 16, fmt, group_of(group, 128) if fmt != "bf16" else 0, [[3, 1, 0, 5], [2, 7, 6, 4]])
+    for s in range(2):
+        for p in range(60):
+            c.put(True, c.page(s, p), p % 16, (rs.standard_normal((1, 128)) * kmag).astype(F32))
+            c.put(False, c.page(s, p), p % 16, (rs.standard_normal((1, 128)) * vmag).astype(F32))
+    q = KV.from_bf16(KV.bf16((rs.standard_normal((2, 3, 128)) / kmag).astype(F32)))
+    O, lse = attend(c, on_device(c), q, [60, 41], 0.088)
+    check_attend(O, lse, c, q, [60, 41], 0.088, f"{kmag} {vmag}")
+
+
+def test_zero_queries_and_zero_caches():
+    """All weights alike: O is the mean; a cache of zeros gives zeros and log2 of the length."""
+    for fmt, group in FORMS:
+        rs = np.random.default_rng(23)
+        c = filled(rs, [77, 20], 1, 64, 16, fmt, group)
+        q = np.zeros((2, 2, 64), F32)
+        O, lse = attend(c, on_device(c), q, [77, 20], 0.125)
+        check_attend(O, lse, c, q, [77, 20], 0.125, fmt)
+        z = KV.Cache(4, 1, 64, 16, fmt, group_of(group, 64) if fmt != "bf16" else 0, [[0, 1, -1], [2, 3, -1]])
+        O, lse = attend(z, on_device(z), rounded(rs, 2, 2, 64), [32, 5], 1.0)
+        assert not bool(O.any()) and np.allclose(lse.cpu().numpy(), np.log2([[32, 32], [5, 5]]), rtol=1e-6)
+
+
+def test_thousands_of_rows():
+    """More sequences than a wavefront's lanes hold one each of: the shares are found run by run."""
+    rs = np.random.default_rng(24)
+    n = 9000
+    lens = rs.integers(0, 3, n)
+    lens[[5, 4000, 8999]] = [700, 90, 300]
+    c = filled(rs, lens, 1, 64, 16, "bf16", 0, outlier=False)
+    q = rounded(rs, n, 1, 64)
+    O, lse = attend(c, on_device(c), q, lens, 0.125)
+    some = np.unique(np.concatenate([[0, 5, 63, 64, 140, 141, 4000, 8998, 8999], rs.integers(0, n, 200)]))
+    part = KV.Cache(c.n_pages, 1, 64, 16, "bf16", 0, c.table[some])
+    part.k, part.v = c.k, c.v
+    check_attend(O[torch.from_numpy(some).cuda()], lse[torch.from_numpy(some).cuda()], part, q[some], lens[some], 0.125)
+    o = O.float().cpu().numpy()
+    assert np.all(o[lens == 0] == 0) and np.all(np.isfinite(o))
+
+
 def test_strided_rows_and_no_lse():
     """Q and O as column slices of wider rows; what lies beside O stays."""
     rs = np.random.default_rng(14)

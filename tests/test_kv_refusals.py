@@ -39,7 +39,7 @@ SHARED = [
     (dict(n_pages=1 << 31), uq.UQ_EINVAL, "n_pages"),
     (dict(n_seq=0), uq.UQ_EINVAL, "n_seq=0"),
     (dict(max_pages=0), uq.UQ_EINVAL, "max_pages=0"),
-    (dict(max_pages=1 << 25), uq.UQ_EINVAL, "max_pages"),
+    (dict(max_pages=(1 << 24) + 1), uq.UQ_EINVAL, "max_pages"),
     (dict(H_kv=0), uq.UQ_EINVAL, "H_kv=0"),
     (dict(H_kv=4097, H=4097), uq.UQ_EINVAL, "H_kv=4097"),
     (dict(pages=None), uq.UQ_EINVAL, "pages"),
