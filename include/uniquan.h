@@ -828,7 +828,7 @@ uq_status uniquan_kv_read(int64_t n_seq, int H_kv, int d, int64_t L,
  *   O = sum_t 2^(x_t log2 e - row_lse) v_t
  * in fp32 from the stored values, O rounded to bf16 (UQ_KV_U8: scales below
  * 2^55; what is below 2^-50 of a value may be lost).  Where no position
- * takes part O is 0 and row_lse -infinity.  What the cache holds at other
+ * takes part, or every score is -infinity, O is 0 and row_lse -infinity.  What the cache holds at other
  * positions has no influence, whatever it is.  Long sequences are split over
  * workgroups and joined in a fixed order, so results do not change from run
  * to run; how they are split depends on lens alone.

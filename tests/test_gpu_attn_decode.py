@@ -130,6 +130,26 @@ def test_non_finite_values_in_use():
     assert np.isfinite(o[2]).all() and bool(torch.isfinite(lse[1:]).all())
 
 
+def test_scores_of_minus_infinity():
+    """Positions whose score is -infinity have no weight; a row of nothing else is an empty one."""
+    rs = np.random.default_rng(26)
+    c = filled(rs, [40, 40], 1, 64, 16, "bf16", 0, outlier=False)
+    q = rounded(rs, 2, 2, 64)
+    q[:, :, 5] = 1
+    for s, places in ((0, range(40)), (1, range(0, 40, 3))):
+        for p in places:
+            c.k[c.page(s, p), 0, p % 16, 5] = 0xFF80
+    O, lse = attend(c, on_device(c), q, [40, 40], 0.125)
+    assert not bool(O[0].any()) and bool((lse[0] == float("-inf")).all())
+    # the second row: what is left of it, moved to the front of a row of its own
+    left = [p for p in range(40) if p % 3]
+    e = KV.Cache(2, 1, 64, 16, "bf16", 0, [[0, 1]])
+    for i, p in enumerate(left):
+        for a, b in ((e.k, c.k), (e.v, c.v)):
+            a[i // 16, 0, i % 16] = b[c.page(1, p), 0, p % 16]
+    check_attend(O[1:], lse[1:], e, q[1:], [len(left)], 0.125)
+
+
 @pytest.mark.parametrize("fmt,group", [("u8", 32), ("u8", None), ("u4", 32), ("u4", None)])
 def test_groups_that_came_out_nan(fmt, group):
     """A key or value with a non-finite group: NaN in every channel of its head's rows, as the header states, and
@@ -191,6 +211,24 @@ def test_thousands_of_rows():
     check_attend(O[torch.from_numpy(some).cuda()], lse[torch.from_numpy(some).cuda()], part, q[some], lens[some], 0.125)
     o = O.float().cpu().numpy()
     assert np.all(o[lens == 0] == 0) and np.all(np.isfinite(o))
+
+
+def test_a_million_heads_rows():
+    """More (sequence, head) rows than a grid dimension's workgroups, some of them split and joined."""
+    rs = np.random.default_rng(27)
+    n, grp = (1 << 16) + 30, 16
+    lens = rs.integers(0, 2, n)
+    lens[[7, 40000, n - 2]] = [400, 130, 700]
+    c = filled(rs, lens, 1, 64, 16, "u4", None, outlier=False)
+    some = np.unique(np.concatenate([[0, 7, 8, 39999, 40000, n - 2, n - 1], rs.integers(0, n, 60)]))
+    q = np.zeros((n, grp, 64), F32)
+    q[some] = rounded(rs, len(some), grp, 64)
+    O, lse = attend(c, on_device(c), q, lens, 0.125)
+    part = KV.Cache(c.n_pages, 1, 64, 16, "u4", 64, c.table[some])
+    part.k, part.v, part.k_stat, part.v_stat = c.k, c.v, c.k_stat, c.v_stat
+    at = torch.from_numpy(some).cuda()
+    check_attend(O[at], lse[at], part, q[some], lens[some], 0.125)
+    assert not bool(O.isnan().any()) and not bool(O[torch.from_numpy(lens == 0).cuda()].any())
 
 
 def test_strided_rows_and_no_lse():

@@ -71,6 +71,21 @@ def test_append_prompts(fmt, group, d, n_kv, grp, P, dt):
 
 
 @pytest.mark.parametrize("fmt,group", FORMS)
+@pytest.mark.parametrize("d,n_kv,grp", [(64, 18, 4), (128, 17, 1)])
+def test_append_many_rows_of_many_heads(fmt, group, d, n_kv, grp):
+    """A prompt whose rows have a workgroup each, several tiles of heads to a row."""
+    rs = np.random.default_rng(n_kv)
+    T, P = 1601, 32
+    t, n_pages = tables(rs, [T], P)
+    c = KV.Cache(n_pages, n_kv, d, P, fmt, group_of(group, d) if fmt != "bf16" else 0, t)
+    poison(c)
+    q, k, v = (rs.standard_normal((T, n, d)).astype(F32) for n in (n_kv * grp, n_kv, n_kv))
+    pos = np.arange(T)
+    pos[[3, 900]] = -1
+    run_append(c, q, k, v, pos, np.zeros(T, np.int32), cos_sin(T, d), torch.bfloat16)
+
+
+@pytest.mark.parametrize("fmt,group", FORMS)
 def test_append_rows_that_go_nowhere(fmt, group):
     """Padding, positions behind the table or the rotary table, sequences and pages that are none: nothing is written
     for them and their queries stay, except that a row without a page still gets its query."""
@@ -184,3 +199,41 @@ def test_offsets_past_32_bits():
     assert torch.equal(K[:, :, 0].transpose(0, 1).reshape(2, -1), k)
     assert torch.equal(V[:, :, 0].transpose(0, 1).reshape(2, -1), v)
     assert torch.equal(k_cache[far, :, 255].float().reshape(-1), k[0])
+
+
+def test_append_millions_of_rows():
+    """More rows than a grid dimension's workgroups: the first and the last one stored, the rest padding."""
+    T, d, P = (1 << 20) + 77, 64, 16
+    rs = np.random.default_rng(19)
+    c = KV.Cache(2, 1, d, P, "bf16", 0, [[1]])
+    poison(c)
+    m = on_device(c)
+    x = torch.zeros(T, d, dtype=torch.bfloat16, device="cuda")
+    at = [0, 1 << 20, T - 1]
+    rows = rounded(rs, 3, 1, d)
+    x[at] = dev(rows[:, 0]).bfloat16()
+    pos = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    pos[at] = torch.tensor([2, 3, 4], dtype=torch.int32, device="cuda")
+    uq.uniquan_kv_append(T, 1, 1, d, None, x, x, pos, seq=torch.zeros_like(pos), **m)
+    torch.cuda.synchronize()
+    c.append(rows, rows, [2, 3, 4], seq=[0, 0, 0])
+    same_cache(m, c)
+
+
+def test_read_millions_of_sequences():
+    """More sequences than a grid dimension's workgroups take: the first and the last ones hold something."""
+    n, d, P = (1 << 21) + 9, 64, 16
+    rs = np.random.default_rng(20)
+    some = [0, 1 << 20, 1 << 21, n - 1]
+    c = filled(rs, [16] * 4, 1, d, P, "u8", 32)
+    m = on_device(c)
+    table = torch.full((n, 1), -1, dtype=torch.int32, device="cuda")
+    table[some] = m["table"]
+    m["table"] = table
+    lens, start = (torch.full((n,), x, dtype=torch.int32, device="cuda") for x in (16, 7))
+    K, V = (torch.full((1, n, 1, d), float("nan"), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    uq.uniquan_kv_read(n, 1, d, 1, lens, K=K, V=V, start=start, **m)
+    torch.cuda.synchronize()
+    for got, want in zip((K, V), c.read([16] * 4, 1, [7] * 4)):
+        assert np.array_equal(host_bits(got[0, some, 0]), KV.bf16(want[0, :, 0]))
+        assert int((got != 0).any(-1).sum()) == 4 and not bool(got.isnan().any())

@@ -160,3 +160,20 @@ def test_binding_refuses_host_tensors_and_wrong_shapes():
         uq.uniquan_attn_decode(2, 1, 1, 64, x, t[0], t, x, x, 0.1, x, fmt=9)
     with pytest.raises(TypeError):
         uq.uniquan_kv_append(2, 1, 1, 64, None, None, x, t[0], t, x, x)
+
+
+def test_binding_refuses_tensors_of_another_device():
+    """The calls run on the current device's stream; a tensor that lies elsewhere is refused, in any argument."""
+    class Far(torch.Tensor):
+        is_cuda = True
+        device = torch.device("cuda", 7)
+
+    far = torch.zeros(2, 64).as_subclass(Far)
+    t = torch.zeros(2, 2, dtype=torch.int32)
+    x = torch.zeros(2, 64, dtype=torch.bfloat16)
+    for call in (lambda: uq.uniquan_kv_append(2, 1, 1, 64, None, x, x, t[0], t, x, far),
+                 lambda: uq.uniquan_kv_append(2, 1, 1, 64, None, x, x, t[0], t, x, x, cs=far),
+                 lambda: uq.uniquan_kv_read(2, 1, 64, 1, t[0], t, x, x, x, far),
+                 lambda: uq.uniquan_attn_decode(2, 1, 1, 64, x, t[0], t, x, x, 0.1, x, ws=far)):
+        with pytest.raises(ValueError, match="cuda:7"):
+            call()
