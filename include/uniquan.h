@@ -826,7 +826,7 @@ uq_status uniquan_kv_read(int64_t n_seq, int H_kv, int d, int64_t L,
  *   row_lse = log2 sum_t 2^(x_t log2 e)   (the base-2 log-sum-exp of
  *                                          uniquan_attn_fwd; may be NULL)
  *   O = sum_t 2^(x_t log2 e - row_lse) v_t
- * in fp32 from the stored values, O rounded to bf16 (UQ_KV_U8: scales below
+ * in fp32 from the stored values, O rounded to bf16 (codes: scales below
  * 2^55; what is below 2^-50 of a value may be lost).  Where no position
  * takes part, or every score is -infinity, O is 0 and row_lse -infinity.  What the cache holds at other
  * positions has no influence, whatever it is.  Long sequences are split over

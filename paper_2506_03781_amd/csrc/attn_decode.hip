@@ -31,7 +31,8 @@
 // product with a column of constants gives the scale, the offset times sum q
 // or the value of the codes' middle in the layout of S^T
 // (v_mfma_f32_16x16x16_bf16, k = 4 (l / 16) .. + 4: the pair is slots 0 and 1
-// of the lane's four, and with several groups lane / 16 takes one each).
+// of the lane's four, and with several groups lane / 16 takes one each; sum q
+// in three bf16 terms against three copies of the pair, 32 deep).
 //
 // Precision.  Scores are fp32 sums of exact products.  A weight p (times the
 // group's scale for codes) enters the second product as two bf16 terms, the
@@ -43,12 +44,15 @@
 // terms then scales values around zero, not their offset, which in a long row
 // is hundreds of times the output.
 //
-// Codes as bf16.  4-bit ones as 128 + c (one AND-OR makes two); the 128 leaves
-// the scores with the offsets, as -128 scale sum q.  8-bit ones as
-// c 2^-133: the byte stands in the low half of a bf16 word (one byte
-// permutation makes two), which is that number below 128 (subnormal) and
-// above (exponent 1) alike, and exact.  The queries of a head are scaled by a
-// power of two to a largest magnitude in [2^120, 2^121) and the scales by 2^64
+// Codes as bf16.  A code c enters as c 2^-133: its bits at the foot of a bf16
+// word, which is that number below 128 (subnormal) and above (exponent 1)
+// alike, and exact.  An 8-bit code takes half a byte permutation; of a byte
+// with two 4-bit codes one AND takes the lower, another the upper as 16 c, for
+// which its query channels are 16 times smaller and its output channels are
+// divided by 16.  (Fed as 128 + c the codes need a shift and an AND-OR each and
+// the 128 taken away again: as fast, but scores of short rows were off by up to
+// 6e-6 of their size, now 3e-7.)  The queries of a head are scaled by a power
+// of two to a largest magnitude in [2^120, 2^121) and the scales by 2^64
 // against it, so keys and values up to 2^60 and down to 2^-57 keep full
 // precision.
 #include <hip/hip_runtime.h>
@@ -265,10 +269,9 @@ __device__ __forceinline__ void load_key(const char* __restrict__ tile, int lane
   }
 }
 
-// The eight channels of contraction step c of a key as bf16.  magic: 0x43004300
-// in a register (two scalar constants would not fit one AND-OR).
+// The eight channels of contraction step c of a key as bf16.
 template <int FMT, int D>
-__device__ __forceinline__ u32x4d key_step(const uint32_t (&w)[Form<FMT, D>::KW], int c, uint32_t magic) {
+__device__ __forceinline__ u32x4d key_step(const uint32_t (&w)[Form<FMT, D>::KW], int c) {
   u32x4d a;
   if constexpr (FMT == KV_BF16) {
 #pragma unroll
@@ -278,7 +281,7 @@ __device__ __forceinline__ u32x4d key_step(const uint32_t (&w)[Form<FMT, D>::KW]
     for (int i = 0; i < 4; ++i) a[i] = __builtin_amdgcn_perm(0u, w[2 * c + i / 2], i & 1 ? 0x0C030C02u : 0x0C010C00u);
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) a[i] = (w[c] >> (4 * i) & 0x000F000Fu) | magic;
+    for (int i = 0; i < 4; ++i) a[i] = w[c] >> (8 * (i / 2)) & (i & 1 ? 0x00F000F0u : 0x000F000Fu);
   }
   return a;
 }
@@ -306,14 +309,14 @@ __device__ __forceinline__ void load_value(const char* __restrict__ tile, int ro
 // Two positions' values at the lane's channel c, as bf16.
 template <int FMT, int D>
 __device__ __forceinline__ uint32_t value_pair(const uint32_t (&a)[Form<FMT, D>::VW],
-                                               const uint32_t (&b)[Form<FMT, D>::VW], int c, uint32_t magic) {
+                                               const uint32_t (&b)[Form<FMT, D>::VW], int c) {
   if constexpr (FMT == KV_BF16) {
     return c & 1 ? top_halves(a[c / 2], b[c / 2]) : low_halves(a[c / 2], b[c / 2]);
   } else if constexpr (FMT == KV_U8) {
     return __builtin_amdgcn_perm(b[c / 4], a[c / 4], 0x0C040C00u + 0x00010001u * uint32_t(c & 3));
   } else {
-    const uint32_t x = c < 4 ? low_halves(a[0], b[0]) : top_halves(a[0], b[0]);
-    return (x >> (4 * (c & 3)) & 0x000F000Fu) | magic;
+    const uint32_t x = __builtin_amdgcn_perm(b[0], a[0], 0x0C040C00u + 0x00010001u * uint32_t(c / 2));
+    return x & (c & 1 ? 0x00F000F0u : 0x000F000Fu);
   }
 }
 
@@ -337,9 +340,10 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
   constexpr int HEADS = WIDE ? 16 : 8;
   constexpr bool CODES = FMT != KV_BF16;
   constexpr float MID = FMT == KV_U8 ? 128.0f : 8.0f;
-  constexpr uint32_t MID_TERM = FMT == KV_U8 ? 0x80808080u : 0xC308C308u;  // minus the middle, as the codes are fed
-  constexpr float VSCALE = FMT == KV_U8 ? 0x1p64f : 1.0f;                  // on the scales
-  constexpr float VBACK = FMT == KV_U8 ? 0x1p69f : 1.0f;                   // 2^133 / VSCALE
+  constexpr float VSCALE = 0x1p64f;  // on the scales
+  constexpr float VBACK = 0x1p69f;   // 2^133 / VSCALE
+  // 4-bit codes of the odd channel tiles come 16-fold
+  auto sixteenfold = [](int k) { return FMT == KV_U4 && k % 2 == 1; };
   constexpr int LD = D + 4;
   __shared__ __attribute__((aligned(16))) float so[WAVES][16][LD];
   __shared__ float sm[WAVES][16], ss[WAVES][16];
@@ -357,8 +361,6 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
   const int h_in = rt * HEADS + (col & (HEADS - 1));  // head within its key/value head's group
   const bool rest = !WIDE && col >= 8;
   const uint32_t cut = rest ? 0xFFFF0000u : 0u;
-  uint32_t magic = 0x43004300u;
-  asm("" : "+v"(magic));
 
   const uint32_t page_bytes = uint32_t(c.H_kv) * uint32_t(c.page_len) * F::ROW;
   const uint32_t page_stats = uint32_t(c.H_kv) * uint32_t(c.page_len) * NG;
@@ -457,13 +459,13 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
 
     // queries (a negative scale's sign put on them), and for codes their sums over each group of channels
     float cl = fabsf(p.scale) * LOG2E_D;  // scores to exponents of 2
-    uint32_t qs[3];  // the sum of the lane's group in three bf16 terms, against (scale, offset)
+    u32x4d qs = {};  // the sum of the lane's group in three bf16 terms, against (scale, offset)
     {
       if (p.scale < 0.0f) {
 #pragma unroll
         for (int k = 0; k < F::NC; ++k) q[k] ^= 0x80008000u;
       }
-      if constexpr (FMT == KV_U8) {
+      if constexpr (CODES) {
         uint32_t top = 0;
 #pragma unroll
         for (int k = 0; k < F::NC; ++k)
@@ -477,9 +479,6 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             q[k][i] = pair(__uint_as_float(q[k][i] << 16) * up, __uint_as_float(q[k][i] & 0xFFFF0000u) * up);
-      }
-      if constexpr (CODES) {
-        constexpr float down = FMT == KV_U8 ? 0x1p-69f : 1.0f;  // 2^-133 times the scales' 2^64
         float mine = 0.0f;
 #pragma unroll
         for (int e = 0; e < NG; ++e) {
@@ -488,17 +487,22 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
           for (int k = e * F::NC / NG; k < (e + 1) * F::NC / NG; ++k)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-              t += __uint_as_float(q[k][i] << 16) * down + __uint_as_float(q[k][i] & 0xFFFF0000u) * down;
+              t += __uint_as_float(q[k][i] << 16) * 0x1p-69f + __uint_as_float(q[k][i] & 0xFFFF0000u) * 0x1p-69f;
           t = sum4(t);
           if (grp == e) mine = t;
         }
-        // 4-bit codes come with 128 too much: minus 128 sum q against the scale
-        constexpr float over = FMT == KV_U4 ? -128.0f : 0.0f;
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
           const float h = __uint_as_float(__float_as_uint(mine) & 0xFFFF0000u);
-          qs[i] = pair(over * h, h);
+          qs[i] = pair(0.0f, h);
           mine -= h;
+        }
+        if constexpr (FMT == KV_U4) {
+#pragma unroll
+          for (int k = 0; k < F::NC; ++k)
+#pragma unroll
+            for (int i = 1; i < 4; i += 2)
+              q[k][i] = pair(__uint_as_float(q[k][i] << 16) * 0x1p-4f, __uint_as_float(q[k][i] & 0xFFFF0000u) * 0x1p-4f);
         }
       }
     }
@@ -514,22 +518,21 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
       for (int t = 0; t < 2; ++t) {
         f32x4d sum = {};
         if constexpr (CODES) {
-          const u32x2d st = {kst[t], 0u};
-#pragma unroll
-          for (int i = 0; i < 3; ++i) sum = mfma16(st, u32x2d{qs[i], 0u}, sum);
+          sum = mfma16(u32x4d{kst[t], kst[t], kst[t], kst[t]}, qs, sum);  // the three terms at once
+          const u32x2d st = {kst[t], kst[t]};
 #pragma unroll
           for (int e = 0; e < NG; ++e) {
             f32x4d a = {};
 #pragma unroll
             for (int k = e * F::NC / NG; k < (e + 1) * F::NC / NG; ++k)
-              a = mfma16(key_step<FMT, D>(kw[t], k, magic), q[k], a);
+              a = mfma16(key_step<FMT, D>(kw[t], k), q[k], a);
             const f32x4d sc = mfma16(st, u32x2d{pick[e], 0u}, f32x4d{});
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf(sc[i], a[i], sum[i]);
           }
         } else {
 #pragma unroll
-          for (int k = 0; k < F::NC; ++k) sum = mfma16(key_step<FMT, D>(kw[t], k, magic), q[k], sum);
+          for (int k = 0; k < F::NC; ++k) sum = mfma16(key_step<FMT, D>(kw[t], k), q[k], sum);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[4 * t + i] = sum[i];
@@ -609,13 +612,14 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
 #pragma unroll
         for (int k = e * F::NV / NG; k < (e + 1) * F::NV / NG; ++k) {
           if constexpr (CODES) {
-            const u32x4d mid = {MID_TERM, MID_TERM, MID_TERM, MID_TERM};
+            const uint32_t bits = FMT == KV_U8 || sixteenfold(k) ? 0x80808080u : 0x80088008u;  // minus the middle, as the codes
+            const u32x4d mid = {bits, bits, bits, bits};
             acc[k] = mfma16(mid, hi, acc[k]);
             if constexpr (WIDE) acc[k] = mfma16(mid, lo, acc[k]);
           }
           u32x4d a;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) a[i] = value_pair<FMT, D>(vw[2 * i], vw[2 * i + 1], k, magic);
+          for (int i = 0; i < 4; ++i) a[i] = value_pair<FMT, D>(vw[2 * i], vw[2 * i + 1], k);
           acc[k] = mfma16(a, hi, acc[k]);
           if constexpr (WIDE) acc[k] = mfma16(a, lo, acc[k]);
         }
@@ -632,7 +636,7 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
       if constexpr (CODES) off[e] = rest ? 0.0f : sum4(off[e]);
 #pragma unroll
       for (int k = e * F::NV / NG; k < (e + 1) * F::NV / NG; ++k)
-        *reinterpret_cast<f32x4d*>(&so[wave][col][16 * k + 4 * grp]) = CODES ? acc[k] * VBACK + off[e] : acc[k];
+        *reinterpret_cast<f32x4d*>(&so[wave][col][16 * k + 4 * grp]) = CODES ? acc[k] * (sixteenfold(k) ? VBACK / 16 : VBACK) + off[e] : acc[k];
     }
     if (grp == 0) {
       sm[wave][col] = m;

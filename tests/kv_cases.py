@@ -100,9 +100,9 @@ def cos_sin(n, d):
     return np.stack([np.cos(a), np.sin(a)], -1).astype(F32)
 
 
-# A sum over codes adds up code values (counted from 0, 4-bit ones from 128 below) and takes their part of the
-# offset away again: at most this many times the largest value, counting both.
-WIDE = {"bf16": 1.0, "u8": 4.0, "u4": 24.0}
+# A sum over codes adds up code values, counted from 0, and takes their part of the offset away again: at most this
+# many times the largest value, counting both.
+WIDE = {"bf16": 1.0, "u8": 4.0, "u4": 4.0}
 
 
 def attend_bounds(c, q, lens, scale):

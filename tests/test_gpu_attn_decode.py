@@ -52,6 +52,23 @@ def test_lengths(fmt, group, d, n_kv, grp, P):
 
 
 @pytest.mark.parametrize("fmt,group", FORMS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("grp", [4, 12])
+def test_scores_to_fp32(fmt, group, d, grp):
+    """Rows of one position, whose log-sum-exp is the score alone: to 2^-20 normwise.  A score is d / 32 matrix
+    instructions, the scale and offset's product, their joining, the scaling and the exponents' base, at most ten
+    roundings one after the other, of numbers up to WIDE = 4 times its size: 4 sqrt(10 / 3) 2^-24 = 2^-21.1 normwise."""
+    rs = np.random.default_rng(28)
+    n = 100
+    c = filled(rs, [1] * n, 1, d, 16, fmt, group)
+    q = rounded(rs, n, grp, d)
+    _, lse = attend(c, on_device(c), q, [1] * n, d ** -0.5)
+    want = c.attend(q, [1] * n, d ** -0.5)[1]
+    got = lse.cpu().numpy().astype(np.float64)
+    assert np.linalg.norm(got - want) <= 2.0 ** -20 * np.linalg.norm(want)
+
+
+@pytest.mark.parametrize("fmt,group", FORMS)
 def test_holes_and_bad_pages(fmt, group):
     """Pages that are none take no part: first, middle, last, all; whole rows left empty."""
     rs = np.random.default_rng(5)
