@@ -764,7 +764,7 @@ uq_status uniquan_bcq_matmul(int T, int64_t R, int64_t C, int k, int g,
  * A page id outside [0, n_pages) is no page (-1: not allocated, or evicted):
  * nothing is written there and its positions take no part in an attention.
  * Sequences may share pages that are only read.  Two rows of one append must
- * not name the same place: which of them it then holds is not defined.
+ * not name the same place: what it then holds is not defined.
  *
  * Rules shared by the three calls.  d is 64 or 128 (UQ_EUNSUPPORTED
  * otherwise); group is 0 for UQ_KV_BF16, else 32 or d; page_len a power of
@@ -786,7 +786,7 @@ typedef enum { UQ_KV_BF16 = 0, UQ_KV_U8 = 1, UQ_KV_U4 = 2 } uq_kv_format;
  * cache's format.  A row whose position is negative, not below n_cs (with cs)
  * or not below max_pages page_len, or whose sequence is not in [0, n_seq), is
  * padding: nothing is written for it, its q_out row is left as it was.  A row
- * whose page is none gets its q_out row only.
+ * whose page is none gets its q_out row only.  Outputs must not overlap inputs.
  *
  * q [T] rows of H d, k, v [T] rows of H_kv d, in_dtype (UQ_F32 or UQ_BF16),
  * rows ld_q, ld_k, ld_v elements apart (multiples of 8; 0: no gap); q may be
