@@ -166,13 +166,16 @@ __device__ __forceinline__ int blocks_of(int len) { return (len + BLOCK - 1) / B
 struct Share {
   int a, b;
   int s, begin;
+  int total;  // cost of all sequences
 };
+
+__device__ __forceinline__ int parts_of(int total, int want) { return std::min(want, std::max(1, total / MIN_COST)); }
 
 // Every wavefront works it out by itself: its lanes add up runs of the
 // sequences, then the run that holds `a` is searched.  With little in all,
 // only the first shares get something, MIN_COST at least.
 __device__ __forceinline__ Share share_of(const AttnDecodeLaunch& p, int at, int want) {
-  if (want == 1) return Share{0, 0x7FFFFFFF, 0, 0};
+  if (want == 1) return Share{0, 0x7FFFFFFF, 0, 0, 0};
   const int lane = threadIdx.x & 63;
   const int n = int(p.c.n_seq);
   const int per = (n + 63) / 64;
@@ -181,10 +184,11 @@ __device__ __forceinline__ Share share_of(const AttnDecodeLaunch& p, int at, int
   for (int j = lane * per; j < lane * per + per; ++j) mine += cost(j);
   int upto = wave_scan(mine);
   const int total = __builtin_amdgcn_readlane(upto, 63);
-  const int parts = std::min(want, std::max(1, total / MIN_COST));
-  if (at >= parts) return Share{0, 0, 0, 0};
+  const int parts = parts_of(total, want);
+  if (at >= parts) return Share{0, 0, 0, 0, total};
   const int q = total / parts, r = total % parts;
   Share h;
+  h.total = total;
   h.a = at * q + at * r / parts;
   h.b = (at + 1) * q + (at + 1) * r / parts;
   // the run that holds a (it is below total), then the sequence in it, 64 at a time
@@ -204,7 +208,7 @@ __device__ __forceinline__ Share share_of(const AttnDecodeLaunch& p, int at, int
     }
     h.begin = __builtin_amdgcn_readlane(upto, 63);
   }
-  return Share{0, 0, 0, 0};
+  return Share{0, 0, 0, 0, total};
 }
 
 // A share's part of one sequence: blocks [b0, b1); the sequence's first and
@@ -233,12 +237,23 @@ __device__ __forceinline__ bool next_chunk(const AttnDecodeLaunch& p, const Shar
   return false;
 }
 
-// The workspace: the first and the last share of each sequence, then the
-// chunks, that of share i and sequence s at i + s (no two alike: from one chunk
-// to the next either grows), H rows each of (maximum, sum, -, -, D values)
-// against that maximum.
-__device__ __forceinline__ int2* shares_of(const AttnDecodeLaunch& p) { return reinterpret_cast<int2*>(p.ws); }
-__device__ __forceinline__ float* chunks_of(const AttnDecodeLaunch& p) { return p.ws + (p.c.n_seq * 2 + 3) / 4 * 4; }
+// The workspace: notes of the sequences that lie in several shares, one a
+// sequence, or one a share (the sequence that begins in it) where there are
+// fewer shares, so that no more joins are launched than are wanted (4096
+// sequences of 128 positions, 32 heads on 8, in 96 shares: 353 us with one a
+// sequence, 288 with one a share); then two chunks a share, of the sequence that
+// came into it and of the one that goes out, H rows each of (maximum, sum, -, -,
+// D values) against that maximum.
+struct Note {
+  int share, s;  // the first share
+  int last;      // the cost of its last block, -1: the sequence lies in one share
+  int total;     // Share's
+};
+__host__ __device__ __forceinline__ int64_t notes_of(const KvCache& c, int want) { return c.n_seq < want ? c.n_seq : want; }
+__device__ __forceinline__ Note* notes(const AttnDecodeLaunch& p) { return reinterpret_cast<Note*>(p.ws); }
+__device__ __forceinline__ float* chunk(const AttnDecodeLaunch& p, int want, int share, bool opens, int64_t head, int D) {
+  return p.ws + notes_of(p.c, want) * 4 + ((2 * int64_t(share) + opens) * p.H + head) * (D + 4);
+}
 
 // ---------------------------------------------------------------------------
 // one chunk
@@ -367,6 +382,8 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
   const int at = int(unit / c.H_kv), g = int(unit % c.H_kv);
   if (at >= want) return;
   const Share share = share_of(p, at, want);
+  const bool noting = p.ws && g == 0 && rt == 0 && threadIdx.x == 0, by_seq = p.c.n_seq <= want;
+  if (noting && !by_seq) notes(p)[at].last = -1;
   const int grp_heads = p.H / c.H_kv;
   const int h_in = rt * HEADS + (col & (HEADS - 1));  // head within its key/value head's group
   const bool rest = !WIDE && col >= 8;
@@ -448,7 +465,7 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
   load_values();
 
   // A chunk's queries are asked for while the chunk before is joined (65536 sequences of 64 positions 763 us
-  // against 808, 1024 of 128 positions of 8 heads 87 against 92).
+  // against 808).
   u32x4d q[F::NC];
   auto load_queries = [&] {
     const uint16_t* row = p.Q + ch.s * p.ld_q + (int64_t(g) * grp_heads + h_in) * D + 8 * grp;
@@ -462,10 +479,7 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
   while (more) {
     const int64_t s = ch.s;
     const bool opens = ch.opens, closes = ch.closes;
-    if (p.ws && g == 0 && rt == 0 && threadIdx.x == 0) {
-      if (opens) shares_of(p)[s].x = at;
-      if (closes) shares_of(p)[s].y = at;
-    }
+    if (noting && opens && (by_seq || !closes)) notes(p)[by_seq ? s : at] = {at, int(s), closes ? -1 : ch.end - 2, share.total};
 
     // queries (a negative scale's sign put on them), and for codes their sums over each group of channels
     float cl = fabsf(p.scale) * LOG2E_D;  // scores to exponents of 2
@@ -684,7 +698,7 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
         *reinterpret_cast<uint32_t*>(p.O + s * p.ld_o + head * D + cn) = pack_bf16x2(a0 * r, a1 * r);
         if (cn == 0 && p.lse) p.lse[s * p.H + head] = t == 0.0f ? -__builtin_inff() : top + __builtin_amdgcn_logf(t);
       } else {
-        float* part = chunks_of(p) + ((at + s) * p.H + head) * (D + 4);
+        float* part = chunk(p, want, at, opens, head, D);
         *reinterpret_cast<float2*>(part + 4 + cn) = make_float2(a0, a1);
         if (cn == 0) *reinterpret_cast<float2*>(part) = make_float2(top, t);
       }
@@ -696,16 +710,17 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
 // Joins the chunks of a sequence's head: D / 4 lanes a chunk, PAR chunks at a
 // time, four of each in flight.
 template <int D>
-__global__ __launch_bounds__(512) void attn_join_kernel(AttnDecodeLaunch p) {
+__global__ __launch_bounds__(512) void attn_join_kernel(AttnDecodeLaunch p, int want) {
   constexpr int LANES = D / 4, PAR = 512 / LANES;
-  const int s = int(workgroup() / p.H), h = int(workgroup() % p.H);
-  if (s >= p.c.n_seq) return;
-  const int2 in = shares_of(p)[s];
-  const int n = in.y - in.x + 1;
-  if (n <= 1) return;
+  const int64_t at = workgroup() / p.H;
+  const int h = int(workgroup() % p.H);
+  if (at >= notes_of(p.c, want)) return;
+  const Note note = notes(p)[at];
+  if (note.last < 0) return;
+  const int s = note.s;
+  // share i begins at floor(i total / parts): the last one that begins at note.last or before, counted from the first
+  const int n = int(((int64_t(note.last) + 1) * parts_of(note.total, want) - 1) / note.total) - note.share + 1;
   const int lane = threadIdx.x % LANES, row = threadIdx.x / LANES;
-  const float* base = chunks_of(p) + ((int64_t(in.x) + s) * p.H + h) * (D + 4);
-  const int64_t ld = int64_t(p.H) * (D + 4);
   float m = LOWEST, t = 0.0f;
   f32x4d a = {};
   for (int k = row; k < n; k += 4 * PAR) {
@@ -713,9 +728,10 @@ __global__ __launch_bounds__(512) void attn_join_kernel(AttnDecodeLaunch p) {
     f32x4d o[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float* at = base + std::min(k + i * PAR, n - 1) * ld;
-      ml[i] = *reinterpret_cast<const float2*>(at);
-      o[i] = *reinterpret_cast<const f32x4d*>(at + 4 + 4 * lane);
+      const int j = std::min(k + i * PAR, n - 1);
+      const float* part = chunk(p, want, note.share + j, j == 0, h, D);
+      ml[i] = *reinterpret_cast<const float2*>(part);
+      o[i] = *reinterpret_cast<const f32x4d*>(part + 4 + 4 * lane);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -781,7 +797,7 @@ hipError_t launch_form(AttnDecodeLaunch p, hipStream_t st) {
     attn_decode_kernel<FMT, D, NG, false><<<grid, 256, 0, st>>>(p, want, rt);
   if (hipError_t e = hipGetLastError()) return e;
   if (!p.ws) return hipSuccess;
-  attn_join_kernel<D><<<grid_of(p.c.n_seq * p.H), 512, 0, st>>>(p);
+  attn_join_kernel<D><<<grid_of(notes_of(p.c, want) * p.H), 512, 0, st>>>(p, want);
   return hipGetLastError();
 }
 
@@ -798,7 +814,7 @@ hipError_t launch_d(const AttnDecodeLaunch& p, hipStream_t st) {
 size_t attn_decode_ws(int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len) {
   const int64_t want = shares(n_seq, H, H_kv, max_pages, page_len, 4);  // the most of any form
   if (!splits(int(want), max_pages, page_len)) return 0;
-  return size_t(n_seq * 2 + 3) / 4 * 4 + size_t(want + n_seq) * size_t(H) * size_t(d + 4);
+  return size_t(std::min(n_seq, want)) * 4 + 2 * size_t(want) * size_t(H) * size_t(d + 4);
 }
 
 hipError_t launch_attn_decode(const AttnDecodeLaunch& p, hipStream_t st) {
