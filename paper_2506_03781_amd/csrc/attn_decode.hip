@@ -36,9 +36,13 @@
 //
 // Precision.  Scores are fp32 sums of exact products.  A weight p (times the
 // group's scale for codes) enters the second product as two bf16 terms, the
-// truncated value and the truncated rest, so what is lost is below 2^-16 of
-// it: with up to 8 heads the rest stands in the columns 8..15, which costs
-// nothing, above that in a second product.  Every step takes the codes'
+// truncated value and the truncated rest: with up to 8 heads the rest stands in
+// the columns 8..15, which costs nothing, above that in a second product.  The
+// rest is below 2^-7 of p and its truncation takes less than 2^-15 off, 2^-17 on
+// average, so p 2^-17 is added to it first: what the terms miss lies between
+// -2^-17 and 2^-15 - 2^-17 of p and does not add up over a row.  And the rest of
+// a weight is above 0 as the weight is, so that an infinite value stays infinite
+// (0 times it is NaN) down to weights of 2^-116.  Every step takes the codes'
 // middle away again with the same bf16 terms (a product with a constant), and
 // the exact weights carry the middle's value: what truncation takes off the
 // terms then scales values around zero, not their offset, which in a long row
@@ -87,6 +91,7 @@ typedef short s16x4d __attribute__((ext_vector_type(4)));
 
 constexpr float LOG2E_D = 1.44269504088896341f;
 constexpr float LOWEST = -3.402823466e38f;  // the running maximum before any position
+constexpr float MORE = 1.0f + 0x1p-17f;     // a weight's second term is MORE times it, less the first term
 constexpr float SLACK = 8.0f;               // scores may exceed the reference by this (weights up to 2^8)
 constexpr int WAVES = 4;
 constexpr int STEP = 32;                    // positions of a wavefront's step
@@ -390,6 +395,7 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
   const int h_in = rt * HEADS + (col & (HEADS - 1));  // head within its key/value head's group
   const bool rest = !WIDE && col >= 8;
   const uint32_t cut = rest ? 0xFFFF0000u : 0u;
+  const float grown = rest ? MORE : 1.0f;
 
   const uint32_t page_bytes = uint32_t(c.H_kv) * uint32_t(c.page_len) * F::ROW;
   const uint32_t page_stats = uint32_t(c.H_kv) * uint32_t(c.page_len) * NG;
@@ -626,12 +632,14 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
         u32x4d hi, lo;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          auto less = [](float v, uint32_t bits) { return v - __uint_as_float(__float_as_uint(v) & bits); };
+          auto less = [](float v, uint32_t bits, float f) {
+            return __builtin_fmaf(v, f, -__uint_as_float(__float_as_uint(v) & bits));
+          };
           if constexpr (WIDE) {
             hi[i] = pair(z[2 * i], z[2 * i + 1]);
-            lo[i] = pair(less(z[2 * i], 0xFFFF0000u), less(z[2 * i + 1], 0xFFFF0000u));
+            lo[i] = pair(less(z[2 * i], 0xFFFF0000u, MORE), less(z[2 * i + 1], 0xFFFF0000u, MORE));
           } else {
-            hi[i] = pair(less(z[2 * i], cut), less(z[2 * i + 1], cut));
+            hi[i] = pair(less(z[2 * i], cut, grown), less(z[2 * i + 1], cut, grown));
           }
         }
 #pragma unroll
