@@ -827,9 +827,12 @@ uq_status uniquan_kv_read(int64_t n_seq, int H_kv, int d, int64_t L,
  *                                          uniquan_attn_fwd; may be NULL)
  *   O = sum_t 2^(x_t log2 e - row_lse) v_t
  * in fp32 from the stored values, O rounded to bf16 (codes: scales below
- * 2^55; what is below 2^-50 of a value may be lost).  Where no position
- * takes part, or every score is -infinity, O is 0 and row_lse -infinity.  What the cache holds at other
- * positions has no influence, whatever it is.  Long sequences are split over
+ * 2^55; what is below 2^-50 of a value may be lost.  bf16: finite values of any
+ * size where the weights, counted by the largest, sum to less than 2^16, as in
+ * rows of up to 2^16 positions; weights below 2^-90 of the largest may count as
+ * 0, which times an infinite value is NaN).  Where no position takes part, or
+ * every score is -infinity, O is 0 and row_lse -infinity.  What the cache holds
+ * at other positions has no influence, whatever it is.  Long sequences are split over
  * workgroups and joined in a fixed order, so results do not change from run
  * to run; how they are split depends on lens alone.
  *

@@ -42,11 +42,14 @@
 // average, so p 2^-17 is added to it first: what the terms miss lies between
 // -2^-17 and 2^-15 - 2^-17 of p and does not add up over a row.  And the rest of
 // a weight is above 0 as the weight is, so that an infinite value stays infinite
-// (0 times it is NaN) down to weights of 2^-116.  Every step takes the codes'
-// middle away again with the same bf16 terms (a product with a constant), and
-// the exact weights carry the middle's value: what truncation takes off the
-// terms then scales values around zero, not their offset, which in a long row
-// is hundreds of times the output.
+// (0 times it is NaN) down to weights of 2^-92.  Values of a bf16 cache meet
+// weights 2^-24 times their size: of at most 2^-16, so that a row of 2^16 of the
+// largest bf16 numbers stays in fp32's range until it is divided by the weights'
+// sum, while a rounding among the smallest fp32 numbers takes 2^-126 off the
+// output.  Every step takes the codes' middle away again with the same bf16
+// terms (a product with a constant), and the exact weights carry the middle's
+// value: what truncation takes off the terms then scales values around zero,
+// not their offset, which in a long row is hundreds of times the output.
 //
 // Codes as bf16.  A code c enters as c 2^-133: its bits at the foot of a bf16
 // word, which is that number below 128 (subnormal) and above (exponent 1)
@@ -91,6 +94,8 @@ typedef short s16x4d __attribute__((ext_vector_type(4)));
 
 constexpr float LOG2E_D = 1.44269504088896341f;
 constexpr float LOWEST = -3.402823466e38f;  // the running maximum before any position
+constexpr float BF16_DOWN = 0x1p-24f;       // weights of a bf16 cache's values (codes have their own powers of two)
+constexpr float BF16_BACK = 0x1p24f;
 constexpr float MORE = 1.0f + 0x1p-17f;     // a weight's second term is MORE times it, less the first term
 constexpr float SLACK = 8.0f;               // scores may exceed the reference by this (weights up to 2^8)
 constexpr int WAVES = 4;
@@ -626,7 +631,7 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
             }
           } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) z[4 * t + i] = w[4 * t + i];
+            for (int i = 0; i < 4; ++i) z[4 * t + i] = w[4 * t + i] * BF16_DOWN;
           }
         }
         u32x4d hi, lo;
@@ -703,7 +708,7 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
       }
       const int64_t head = int64_t(g) * grp_heads + hh;
       if (opens && closes) {
-        const float r = t == 0.0f ? 0.0f : 1.0f / t;
+        const float r = t == 0.0f ? 0.0f : (CODES ? 1.0f : BF16_BACK) / t;
         *reinterpret_cast<uint32_t*>(p.O + s * p.ld_o + head * D + cn) = pack_bf16x2(a0 * r, a1 * r);
         if (cn == 0 && p.lse) p.lse[s * p.H + head] = t == 0.0f ? -__builtin_inff() : top + __builtin_amdgcn_logf(t);
       } else {
@@ -771,7 +776,7 @@ __global__ __launch_bounds__(512) void attn_join_kernel(AttnDecodeLaunch p, int 
     t += f * st[k];
     a += f * so[k][lane];
   }
-  const float r = t == 0.0f ? 0.0f : 1.0f / t;
+  const float r = t == 0.0f ? 0.0f : (p.c.format == KV_BF16 ? BF16_BACK : 1.0f) / t;
   *reinterpret_cast<uint2*>(p.O + s * p.ld_o + int64_t(h) * D + 4 * lane) =
       make_uint2(pack_bf16x2(a[0] * r, a[1] * r), pack_bf16x2(a[2] * r, a[3] * r));
   if (lane == 0 && p.lse) p.lse[int64_t(s) * p.H + h] = t == 0.0f ? -__builtin_inff() : top + __builtin_amdgcn_logf(t);

@@ -1,6 +1,6 @@
 """uniquan_attn_decode over the whole range of what a cache can hold: infinite
-values, against oracle/kv_cache.py in 64 bits with bars from
-kv_cases.attend_bounds."""
+values, the largest and the smallest ones, against oracle/kv_cache.py in 64
+bits with bars from kv_cases.attend_bounds."""
 import copy
 
 import numpy as np
@@ -75,4 +75,67 @@ def test_infinite_values(d, grp, scale):
         assert np.array_equal(O[s, grp:, ch], np.full(grp, x), equal_nan=True), (s, ch, O[s, grp:, ch])
         O[s, grp:, ch] = ref[s, grp:, ch] = 0
     within(O, ref, tol)
+    within(lse, ref_l, tol_l)
+
+
+BF16_MAX = 0x7F7F
+
+
+def valued(rs, lens, n_kv, d, values):
+    """A bf16 cache with drawn keys of order one and the values that `values` (shape) gives."""
+    c = filled(rs, lens, n_kv, d, 16, "bf16", 0, outlier=False)
+    for s, ln in enumerate(lens):
+        page, r = c.held(s, ln)
+        c.v[page, :, r] = values((len(page), n_kv, d))
+    return c
+
+
+@pytest.mark.parametrize("grp", [1, 6, 12])
+@pytest.mark.parametrize("scale", [0.0, 0.1, -3.0])
+def test_values_up_to_the_largest(grp, scale):
+    """Finite values of any size in rows of up to 2^16 positions: of both signs around the largest bf16 number, and in
+    one channel that number alone, which O then is."""
+    rs = np.random.default_rng(50 + grp)
+    lens = [1, 100, 31, 4000, 257]
+    c = valued(rs, lens, 1, 128, lambda n: rs.integers(0x7F00, BF16_MAX + 1, n).astype(np.uint16)
+               | (rs.integers(0, 2, n) << 15).astype(np.uint16))
+    for s, ln in enumerate(lens):
+        page, r = c.held(s, ln)
+        c.v[page, :, r, 77] = BF16_MAX
+    q = rounded(rs, len(lens), grp, 128)
+    O, lse = attend(c, q, lens, scale)
+    ref, ref_l, tol, tol_l = attend_bounds(c, q, lens, scale)
+    assert np.all(O[..., 77] == KV.from_bf16(BF16_MAX))
+    within(O, ref, tol)
+    within(lse, ref_l, tol_l)
+
+
+def test_values_of_the_largest_in_a_row_of_65536():
+    """All alike and all the largest: the mean is the value."""
+    n, d = 1 << 16, 64
+    pages = n // 1024
+    m = dict(table=torch.arange(pages, dtype=torch.int32, device="cuda").reshape(1, -1), fmt=uq.KV_BF16, page_len=1024,
+             k_cache=torch.zeros(pages, 1, 1024, d, dtype=torch.bfloat16, device="cuda"),
+             v_cache=torch.full((pages, 1, 1024, d), float(KV.from_bf16(BF16_MAX)), dtype=torch.bfloat16, device="cuda"))
+    Q = torch.ones(1, 2 * d, dtype=torch.bfloat16, device="cuda")
+    O = torch.empty_like(Q)
+    uq.uniquan_attn_decode(1, 2, 1, d, Q, torch.tensor([n], dtype=torch.int32, device="cuda"), scale=0.125, O=O,
+                           ws=torch.empty(uq.uniquan_attn_decode_ws(1, 2, 1, d, pages, 1024), device="cuda"), **m)
+    torch.cuda.synchronize()
+    assert bool((O == m["v_cache"][0, 0, 0, 0]).all())
+
+
+@pytest.mark.parametrize("vmag", [2.0 ** -80, 2.0 ** -100, 2.0 ** -112])
+@pytest.mark.parametrize("grp", [3, 12])
+def test_values_near_the_smallest(vmag, grp):
+    """Values near the foot of bf16's range.  Weights enter 2^-24 times in fp32, whose numbers lie 2^-149 apart at the
+    least, so each of a row's n / 8 + 8 roundings of sums (every matrix instruction's and the joins') takes at most
+    2^-150 2^24 off on top of the bars."""
+    rs = np.random.default_rng(60 + grp)
+    lens = [1, 100, 31, 900]
+    c = valued(rs, lens, 1, 128, lambda n: KV.bf16((rs.standard_normal(n) * vmag).astype(F32)))
+    q = rounded(rs, len(lens), grp, 128)
+    O, lse = attend(c, q, lens, 0.09)
+    ref, ref_l, tol, tol_l = attend_bounds(c, q, lens, 0.09)
+    within(O, ref, tol + (np.asarray(lens) / 8 + 8)[:, None, None] * 2.0 ** -126)
     within(lse, ref_l, tol_l)
