@@ -708,8 +708,9 @@ __global__ __launch_bounds__(256, (kResident<FMT, D, NG>)) void attn_decode_kern
       }
       const int64_t head = int64_t(g) * grp_heads + hh;
       if (opens && closes) {
-        const float r = t == 0.0f ? 0.0f : (CODES ? 1.0f : BF16_BACK) / t;
-        *reinterpret_cast<uint32_t*>(p.O + s * p.ld_o + head * D + cn) = pack_bf16x2(a0 * r, a1 * r);
+        const float r = (CODES ? 1.0f : BF16_BACK) / t;
+        // no weight at all: 0, where the values may have made the sums NaN
+        *reinterpret_cast<uint32_t*>(p.O + s * p.ld_o + head * D + cn) = t == 0.0f ? 0u : pack_bf16x2(a0 * r, a1 * r);
         if (cn == 0 && p.lse) p.lse[s * p.H + head] = t == 0.0f ? -__builtin_inff() : top + __builtin_amdgcn_logf(t);
       } else {
         float* part = chunk(p, want, at, opens, head, D);
@@ -776,9 +777,9 @@ __global__ __launch_bounds__(512) void attn_join_kernel(AttnDecodeLaunch p, int 
     t += f * st[k];
     a += f * so[k][lane];
   }
-  const float r = t == 0.0f ? 0.0f : (p.c.format == KV_BF16 ? BF16_BACK : 1.0f) / t;
+  const float r = (p.c.format == KV_BF16 ? BF16_BACK : 1.0f) / t;
   *reinterpret_cast<uint2*>(p.O + s * p.ld_o + int64_t(h) * D + 4 * lane) =
-      make_uint2(pack_bf16x2(a[0] * r, a[1] * r), pack_bf16x2(a[2] * r, a[3] * r));
+      t == 0.0f ? make_uint2(0u, 0u) : make_uint2(pack_bf16x2(a[0] * r, a[1] * r), pack_bf16x2(a[2] * r, a[3] * r));
   if (lane == 0 && p.lse) p.lse[int64_t(s) * p.H + h] = t == 0.0f ? -__builtin_inff() : top + __builtin_amdgcn_logf(t);
 }
 

@@ -139,3 +139,26 @@ def test_values_near_the_smallest(vmag, grp):
     ref, ref_l, tol, tol_l = attend_bounds(c, q, lens, 0.09)
     within(O, ref, tol + (np.asarray(lens) / 8 + 8)[:, None, None] * 2.0 ** -126)
     within(lse, ref_l, tol_l)
+
+
+@pytest.mark.parametrize("grp", [2, 12])
+def test_rows_of_scores_of_minus_infinity(grp):
+    """A row whose every score is -infinity is empty, whatever its values are: NaN, infinite, the largest."""
+    rs = np.random.default_rng(70)
+    lens = [1, 40, 5000, 33, 300]
+    c = filled(rs, lens, 1, 64, 16, "bf16", 0, outlier=False)
+    q = rounded(rs, len(lens), grp, 64)
+    q[..., 5] = 1
+    for s, ln in enumerate(lens[:3]):
+        page, r = c.held(s, ln)
+        c.k[page, :, r, 5] = INF | 0x8000
+        c.v[page, :, r, 0] = 0x7FC0
+        c.v[page[-1], :, r[-1], 1] = INF
+        c.v[page, :, r, 2] = BF16_MAX
+    O, lse = attend(c, q, lens, 0.125)
+    assert np.all(O[:3] == 0) and np.all(lse[:3] == -np.inf)
+    sub = KV.Cache(c.n_pages, 1, 64, 16, "bf16", 0, c.table[3:])
+    sub.k, sub.v = c.k, c.v
+    ref, ref_l, tol, tol_l = attend_bounds(sub, q[3:], lens[3:], 0.125)
+    within(O[3:], ref, tol)
+    within(lse[3:], ref_l, tol_l)
