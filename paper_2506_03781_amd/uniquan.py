@@ -244,8 +244,10 @@ def _check(status: int):
 
 def _stream(stream):
     if stream is None:
-        if torch.cuda.is_initialized():  # 0.3 us; a torch stream object made for its handle takes 2.8
-            return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        # 0.5 us where torch has this call; a torch stream object made for its handle takes 2.7
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is not None and torch.cuda.is_initialized():
+            return raw(torch.cuda.current_device())
         return torch.cuda.current_stream().cuda_stream
     return getattr(stream, "cuda_stream", stream)
 
