@@ -10,6 +10,7 @@ of the expected dtype with at least the number of elements the call touches.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 import re
 
@@ -631,6 +632,22 @@ def _one_device(*tensors):
             raise ValueError(f"tensor on {t.device}, the current device is cuda:{here}")
 
 
+def _whole(t, shape, name):
+    """t as it is, refused where its shape says that its values lie otherwise than in a contiguous tensor of `shape`:
+    as many dimensions must agree (the first may be larger), a flat tensor holds that many values or more, any other
+    exactly that many."""
+    if not isinstance(t, torch.Tensor) or t.dim() < 2:
+        return t
+    got = tuple(t.shape)
+    if len(got) == len(shape):
+        bad = got[1:] != tuple(shape[1:]) or got[0] < shape[0]
+    else:
+        bad = t.numel() != math.prod(shape)
+    if bad:
+        raise ValueError(f"{name} has shape {got}, expected {tuple(shape)}")
+    return t
+
+
 def _ld(t, rows, cols, dtypes, name):
     """Device pointer and row distance of [rows, cols] values: a contiguous tensor of that many, or a
     [rows, cols] view whose rows lie apart (a column slice)."""
@@ -646,7 +663,7 @@ def _ld(t, rows, cols, dtypes, name):
         return t.data_ptr(), t.stride(0)
     if isinstance(t, torch.Tensor) and rows == 1 and tuple(t.shape) == (1, cols):
         t = t[0]
-    return _p(t, rows * cols, dtypes, name), 0
+    return _p(_whole(t, (rows, cols), name), rows * cols, dtypes, name), 0
 
 
 def _kv(Hkv, d, page_len, table, k_cache, v_cache, k_stat, v_stat, fmt, group):
@@ -662,11 +679,15 @@ def _kv(Hkv, d, page_len, table, k_cache, v_cache, k_stat, v_stat, fmt, group):
     page = Hkv * page_len * row
     n_pages = k_cache.numel() // page if isinstance(k_cache, torch.Tensor) else 0
     dt = _B if fmt == KV_BF16 else _U8
+    for t, name in ((k_cache, "k_cache"), (v_cache, "v_cache")):
+        _whole(t, (n_pages, Hkv, page_len, row), name)
     stats = None
     if fmt != KV_BF16 and group > 0:
         stats = n_pages * Hkv * page_len * 2 * (d // group)
         if k_stat is None or v_stat is None:
             raise ValueError("k_stat and v_stat must be given for a cache of codes")
+        for t, name in ((k_stat, "k_stat"), (v_stat, "v_stat")):
+            _whole(t, (n_pages, Hkv, d // group, page_len, 2), name)
     return ((_p(table, None, _I32, "table"), table.shape[0], table.shape[1]),
             (int(fmt), int(group), n_pages, int(page_len)),
             (_p(k_cache, max(1, n_pages) * page, dt, "k_cache"), _p(v_cache, max(1, n_pages) * page, dt, "v_cache"),
@@ -682,13 +703,15 @@ def uniquan_kv_append(T, H, Hkv, d, q, k, v, pos, table, k_cache, v_cache, q_out
         raise TypeError("k and v must be torch.Tensors")
     _one_device(q, k, v, pos, table, k_cache, v_cache, q_out, seq, cs, k_stat, v_stat)
     (pg, n_seq, mp), f, m = _kv(Hkv, d, page_len, table, k_cache, v_cache, k_stat, v_stat, fmt, group)
+    if isinstance(cs, torch.Tensor) and cs.dim() >= 2 and math.prod(cs.shape[1:]) != d:
+        raise ValueError(f"cs has shape {tuple(cs.shape)}, expected [n, {d // 2}, 2]")
     pk, ld_k = _ld(k, T, Hkv * d, _W, "k")
     pv, ld_v = _ld(v, T, Hkv * d, (k.dtype,), "v")
     pq, ld_q = _ld(q, T, H * d, (k.dtype,), "q")
     _check(lib().uniquan_kv_append(
         T, H, Hkv, d, pq, ld_q, pk, ld_k, pv, ld_v, _dt(k), _p(seq, T, _I32, "seq"), _p(pos, T, _I32, "pos"),
         _p(cs, None, _F, "cs"), 0 if cs is None else cs.numel() // d, pg, n_seq, mp, *f, *m,
-        _p(q_out, T * H * d, _B, "q_out"), _stream(stream)))
+        _p(_whole(q_out, (T, H * d), "q_out"), T * H * d, _B, "q_out"), _stream(stream)))
 
 
 def uniquan_kv_read(n_seq, Hkv, d, L, lens, table, k_cache, v_cache, K, V, start=None, fmt=KV_BF16, group=0,
@@ -699,12 +722,13 @@ def uniquan_kv_read(n_seq, Hkv, d, L, lens, table, k_cache, v_cache, K, V, start
     (pg, ns, mp), f, m = _kv(Hkv, d, page_len, table, k_cache, v_cache, k_stat, v_stat, fmt, group)
     if ns != n_seq:
         raise ValueError(f"table has {ns} rows, n_seq is {n_seq}")
-    n = Hkv * n_seq * L * d
+    n, shape = Hkv * n_seq * L * d, (Hkv, n_seq, L, d)
     one = K if K is not None else V
     dt = _W if one is None else (one.dtype,)
     _check(lib().uniquan_kv_read(
         n_seq, Hkv, d, L, _p(start, n_seq, _I32, "start"), _p(lens, n_seq, _I32, "lens"), pg, mp, *f, *m,
-        _p(K, n, dt, "K"), _p(V, n, dt, "V"), UQ_BF16 if one is None else _dt(one), _stream(stream)))
+        _p(_whole(K, shape, "K"), n, dt, "K"), _p(_whole(V, shape, "V"), n, dt, "V"),
+        UQ_BF16 if one is None else _dt(one), _stream(stream)))
 
 
 def uniquan_attn_decode_ws(n_seq, H, Hkv, d, max_pages, page_len) -> int:
