@@ -8,7 +8,8 @@ import pytest
 import torch
 
 import oracle.kv_cache as KV
-from kv_cases import attend_bounds, dev, filled, on_device, rounded
+from attend_bars import attend
+from kv_cases import attend_bounds, filled, rounded
 from paper_2506_03781_amd import uniquan as uq
 
 pytestmark = pytest.mark.gpu
@@ -23,20 +24,6 @@ def _gpu():
     torch.cuda.set_device(0)
     yield
     torch.cuda.synchronize()
-
-
-def attend(c, q, lens, scale):
-    """O [n, H, d] and the log-sum-exp [n, H] in 64 bits, from the device."""
-    n, H, d = q.shape
-    m = on_device(c)
-    O = torch.full((n, H * d), float("nan"), device="cuda", dtype=torch.bfloat16)
-    lse = torch.full((n, H), float("nan"), device="cuda")
-    ws = torch.full((max(1, uq.uniquan_attn_decode_ws(n, H, c.n_kv, d, m["table"].shape[1], c.P)),), float("nan"),
-                    device="cuda")
-    uq.uniquan_attn_decode(n, H, c.n_kv, d, dev(q.reshape(n, H * d)).bfloat16(), dev(np.asarray(lens, np.int32)),
-                           scale=scale, O=O, row_lse=lse, ws=ws, **m)
-    torch.cuda.synchronize()
-    return O.float().cpu().numpy().astype(np.float64).reshape(n, H, d), lse.cpu().numpy().astype(np.float64)
 
 
 def within(got, want, tol, what=""):
