@@ -737,7 +737,11 @@ uq_status uniquan_bcq_matmul(int T, int64_t R, int64_t C, int k, int g,
  * (uniquan_bcq_matmul) a serving loop calls uniquan_kv_append on the rows of
  * the query, key and value products and uniquan_attn_decode on the rotated
  * queries; its O rows are the output product's activations.  For a prompt,
- * uniquan_kv_read gives keys and values back in uniquan_attn_fwd's layout.
+ * uniquan_kv_read gives keys and values back in uniquan_attn_fwd's layout.  That
+ * call takes heads of 128 channels, as many queries as keys and multiples of 32
+ * positions: whole prompts, the last rows padding.  A cache of 64-channel heads,
+ * and a part of a prompt behind positions that are cached already, have the
+ * attention of one token at a time only.
  *
  * Cache.  Positions 0, 1, ... of a sequence lie in pages of page_len
  * positions: position p of sequence s is place p % page_len of page
@@ -757,10 +761,12 @@ uq_status uniquan_bcq_matmul(int T, int64_t R, int64_t C, int k, int g,
  *   lo    = min x rounded down to bf16
  *   scale = (max x - lo) fl(1 / top) rounded up to bf16; 0 if below 2^-126
  *   c     = rint((x - lo) fl(1 / scale)), at most top; 0 where scale is 0
- * so every value comes back to within half a scale.  A group with a
- * non-finite value, or whose max x - lo overflows, gets NaN for scale and lo
- * and comes back as NaN.  (The attention takes a value one of whose groups is
- * NaN as NaN in every channel.)
+ * so, but for the roundings of fp32, every value comes back to within half a
+ * scale, or, where scale is 0, to within max x - lo (below top 2^-126).  A group
+ * with a non-finite value, or whose max x - lo overflows, gets NaN for scale and
+ * lo and comes back as NaN; where max x - lo is 2^127 or more, single values may
+ * come back infinite.  (The attention takes a value one of whose groups is NaN
+ * as NaN in every channel.)
  * A page id outside [0, n_pages) is no page (-1: not allocated, or evicted):
  * nothing is written there and its positions take no part in an attention.
  * Sequences may share pages that are only read.  Two rows of one append must
@@ -826,15 +832,21 @@ uq_status uniquan_kv_read(int64_t n_seq, int H_kv, int d, int64_t L,
  *   row_lse = log2 sum_t 2^(x_t log2 e)   (the base-2 log-sum-exp of
  *                                          uniquan_attn_fwd; may be NULL)
  *   O = sum_t 2^(x_t log2 e - row_lse) v_t
- * in fp32 from the stored values, O rounded to bf16 (codes: scales below
- * 2^55; what is below 2^-50 of a value may be lost.  bf16: finite values of any
- * size where the weights, counted by the largest, sum to less than 2^16, as in
- * rows of up to 2^16 positions; weights below 2^-90 of the largest may count as
- * 0, which times an infinite value is NaN).  Where no position takes part, or
- * every score is -infinity, O is 0 and row_lse -infinity.  What the cache holds
- * at other positions has no influence, whatever it is.  Long sequences are split over
- * workgroups and joined in a fixed order, so results do not change from run
- * to run; how they are split depends on lens alone.
+ * in fp32 from the stored values, except that the weights of v_t are two bf16
+ * terms each (off by at most 2^-15 of a weight, either way); O rounded to bf16.
+ * Where no position takes part, or every score is -infinity, O is 0 and row_lse
+ * -infinity.  What the cache holds at other positions has no influence, whatever
+ * it is.
+ *   bf16 caches: finite values of any size where the weights, counted by the
+ *     largest, sum to less than 2^16, as in rows of up to 2^16 positions; weights
+ *     below 2^-90 of the largest may count as 0, which times an infinite value is
+ *     NaN.
+ *   Codes: scales below 2^55, offsets below 2^60 in size; of O, what is below
+ *     (n + 64) 2^-84 in a row of n positions may be lost; a query with a channel
+ *     that is not finite makes its row NaN.
+ * Long sequences are split over workgroups and joined in a fixed order, so
+ * results do not change from run to run; how they are split depends on the
+ * sizes, the format and group, max_pages and lens.
  *
  * Q [n_seq] rows of H d bf16, ld_q elements apart (a multiple of 8; 0: H d);
  * O [n_seq] rows of H d bf16, ld_o elements apart (a multiple of 4; 0: H d);

@@ -9,8 +9,19 @@ One step of a block on T rows, one per sequence, is
     uniquan_bcq_matmul(O), then the MLP module
 
 and a prompt is appended in the same way, its rows naming their sequences;
-``read`` gives it back in the layout of ``uniquan_attn_fwd``.  All arithmetic
-runs in libuniquan.so; torch only allocates device memory.
+``read`` gives it back in the layout of ``uniquan_attn_fwd``.  That attention
+takes d = 128, as many queries as keys and multiples of 32 positions: a whole
+prompt (padded behind its end), not a part of one behind positions that are
+cached already, nor heads of 64 channels; those are attended one token at a time.
+
+The rotary table cs [n, d / 2, 2] holds (cos, sin) of every position.
+``uniquan_rope_table`` makes its angles in fp32, off by up to p 2^-23 at position
+p; a table for tens of thousands of positions is made in 64 bits:
+
+    a = torch.arange(n, dtype=torch.float64)[:, None] * base ** (-torch.arange(0, d, 2, dtype=torch.float64) / d)
+    cs = torch.stack([a.cos(), a.sin()], -1).float().cuda()
+
+All arithmetic runs in libuniquan.so; torch only allocates device memory.
 """
 from __future__ import annotations
 

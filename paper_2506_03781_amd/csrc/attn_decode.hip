@@ -60,8 +60,9 @@
 // the 128 taken away again: as fast, but scores of short rows were off by up to
 // 6e-6 of their size, now 3e-7.)  The queries of a head are scaled by a power
 // of two to a largest magnitude in [2^120, 2^121) and the scales by 2^64
-// against it, so keys and values up to 2^60 and down to 2^-57 keep full
-// precision.
+// against it.  So scales of keys may reach 2^60 and those of values 2^55 (their
+// weights 2^8), offsets of either 2^60; sums of values stand 2^-69 times their
+// size in fp32, whose roundings are 2^-150 at the least: 2^-81 of the output.
 //
 // Bound and measured (the kernel alone; a sequence split over shares adds the
 // join, 4 to 7 us, a launch and two loads that wait on each other).  bf16 and

@@ -1,6 +1,6 @@
 """uniquan_attn_decode over the whole range of what a cache can hold: infinite
 values, the largest and the smallest ones, against oracle/kv_cache.py in 64
-bits with bars from kv_cases.attend_bounds."""
+bits with bars from kv_cases.attend_bounds and attend_bars."""
 import copy
 
 import numpy as np
@@ -8,8 +8,8 @@ import pytest
 import torch
 
 import oracle.kv_cache as KV
-from attend_bars import attend
-from kv_cases import attend_bounds, filled, rounded
+from attend_bars import attend, bars, broken, store
+from kv_cases import attend_bounds, filled, rounded, tables
 from paper_2506_03781_amd import uniquan as uq
 
 pytestmark = pytest.mark.gpu
@@ -149,3 +149,73 @@ def test_rows_of_scores_of_minus_infinity(grp):
     ref, ref_l, tol, tol_l = attend_bounds(sub, q[3:], lens[3:], 0.125)
     within(O[3:], ref, tol)
     within(lse[3:], ref_l, tol_l)
+
+
+CODES = [("u8", 32), ("u8", 128), ("u4", 32), ("u4", 128)]
+
+
+def coded(rs, lens, fmt, group, kmag, vmag, koff=0.0, voff=0.0):
+    c = filled(rs, [0] * len(lens), 1, 128, 16, fmt, group, table=tables(rs, lens, 16))
+    for s, ln in enumerate(lens):
+        p = np.arange(ln)
+        store(c, True, s, p, ((rs.standard_normal((ln, 1, 128)) + koff) * kmag).astype(F32))
+        store(c, False, s, p, ((rs.standard_normal((ln, 1, 128)) + voff) * vmag).astype(F32))
+    return c
+
+
+@pytest.mark.parametrize("fmt,group", CODES)
+@pytest.mark.parametrize("grp", [3, 12])
+@pytest.mark.parametrize("off", [0.0, 20.0])
+def test_codes_up_to_the_largest(fmt, group, grp, off):
+    """Scales just below 2^55 (a group of normal values spreads over at most seven standard deviations), offsets of
+    twenty standard deviations, below 2^60 for keys; queries that make scores of order one of them."""
+    rs = np.random.default_rng(75)
+    lens = [1, 100, 31, 1500]
+    mag = 2.0 ** 54.9 * KV.TOP[fmt] / 8 / (32 if off and fmt == "u8" else 1)
+    c = coded(rs, lens, fmt, group, mag, mag, off, off)
+    top = max(KV.from_bf16(x[c.table[s, p // 16], :, :, p % 16, 0]).max() for x in (c.k_stat, c.v_stat)
+              for s, ln in enumerate(lens) for p in range(ln))
+    assert 2.0 ** 48 < top < 2.0 ** 55
+    q = KV.from_bf16(KV.bf16((rs.standard_normal((4, grp, 128)) / (mag * (1 + off))).astype(F32)))
+    O, lse = attend(c, q, lens, 0.09)
+    el, norm = broken(O, c, q, lens, 0.09)
+    assert not el.any() and not norm.any()
+
+
+@pytest.mark.parametrize("fmt,group", CODES)
+@pytest.mark.parametrize("grp", [3, 12])
+@pytest.mark.parametrize("mag", [2.0 ** -50, 2.0 ** -60, 2.0 ** -67])
+def test_codes_down_to_the_smallest(fmt, group, grp, mag):
+    """Values enter 2^-69 times their size in fp32, whose numbers lie 2^-149 apart at the least, so each of a row's
+    n / 8 + 8 roundings of sums takes at most 2^-150 2^69 off on top of the bars."""
+    rs = np.random.default_rng(76)
+    lens = [1, 100, 31, 900]
+    c = coded(rs, lens, fmt, group, mag, mag)
+    q = KV.from_bf16(KV.bf16((rs.standard_normal((4, grp, 128)) / mag).astype(F32)))
+    O, lse = attend(c, q, lens, 0.09)
+    want, tol, _ = bars(c, q, lens, 0.09)
+    within(O, want, tol + (np.asarray(lens) / 8 + 8)[:, None, None] * 2.0 ** -81)
+
+
+@pytest.mark.parametrize("fmt,group", [("bf16", 0)] + CODES)
+@pytest.mark.parametrize("grp", [3, 12])
+def test_queries_that_are_not_finite(fmt, group, grp):
+    """A NaN in a query makes its row NaN; for codes an infinity does so too.  Other heads and empty rows are as they
+    would be without it."""
+    rs = np.random.default_rng(77)
+    lens = [1, 100, 0, 700]
+    c = filled(rs, lens, 2, 128, 16, fmt, group)
+    q = rounded(rs, 4, 2 * grp, 128)
+    ref, ref_l, tol, tol_l = attend_bounds(c, q, lens, 0.09)
+    q[:, 0, 7] = np.nan
+    if fmt != "bf16":
+        q[:, grp, 127] = np.inf
+        q[:, grp + 1, 0] = -np.inf
+    O, lse = attend(c, q, lens, 0.09)
+    hit = np.isnan(q).any(-1) | np.isinf(q).any(-1)
+    hit[2] = False
+    assert np.isnan(O[hit]).all() and np.isnan(lse[hit]).all()
+    assert np.all(O[2] == 0) and np.all(lse[2] == -np.inf)
+    hit[2] = True
+    within(O[~hit], ref[~hit], tol[~hit])
+    within(lse[~hit], ref_l[~hit], tol_l[~hit])
