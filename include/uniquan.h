@@ -852,8 +852,9 @@ uq_status uniquan_kv_read(int64_t n_seq, int H_kv, int d, int64_t L,
  * O [n_seq] rows of H d bf16, ld_o elements apart (a multiple of 4; 0: H d);
  * row_lse [n_seq x H] fp32.  The outputs must not overlap Q.  ws [ws_len] fp32
  * workspace of at least uniquan_attn_decode_ws(n_seq, H, H_kv, d, max_pages,
- * page_len) floats (16-byte aligned; 0: may be NULL), of any contents, free to
- * be reused once the call is done; calls that overlap need one each.
+ * page_len) floats (16-byte aligned; 0: may be NULL; 0 also for sizes that the
+ * call refuses), of any contents, free to be reused once the call is done; calls
+ * that overlap need one each.
  * n_seq H <= 2^24, n_seq (max_pages page_len + 256) <= 2^37.
  */
 size_t uniquan_attn_decode_ws(int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len);

@@ -759,24 +759,31 @@ uq_status uniquan_attn_bwd(int64_t batch, int64_t kv_batch, int L, int d, const 
   return hip_status(fn, uq::launch_attn_bwd(q, static_cast<hipStream_t>(stream)));
 }
 
+// Rules of the paged cache's sizes, without its format and arrays.
+static uq_status check_cache_sizes(const char* fn, int H_kv, int d, int64_t n_seq, int64_t max_pages, int page_len) {
+  if (H_kv < 1 || H_kv > 4096) return fail(UQ_EINVAL, "%s: H_kv=%d must be in [1, 4096]", fn, H_kv);
+  if (d < 1) return fail(UQ_EINVAL, "%s: d=%d must be >= 1", fn, d);
+  if (d != 64 && d != 128) return fail(UQ_EUNSUPPORTED, "%s: d=%d, supported 64 and 128", fn, d);
+  if (page_len < 16 || page_len > 1024 || (page_len & (page_len - 1)) != 0)
+    return fail(UQ_EINVAL, "%s: page_len=%d must be a power of two in [16, 1024]", fn, page_len);
+  const int64_t lim = int64_t(1) << 31;
+  if (n_seq < 1 || n_seq >= lim) return fail(UQ_EINVAL, "%s: n_seq=%lld must be in [1, 2^31)", fn, (long long)n_seq);
+  if (max_pages < 1 || max_pages > (lim / 2) / page_len)
+    return fail(UQ_EINVAL, "%s: max_pages=%lld must be >= 1 and max_pages * page_len <= 2^30", fn, (long long)max_pages);
+  return UQ_OK;
+}
+
 // Shape rules shared by the paged cache's entry points; fills *c.
 static uq_status check_cache(const char* fn, uq::KvCache* c, int H_kv, int d, const int32_t* pages, int64_t n_seq,
                              int64_t max_pages, int format, int group, int64_t n_pages, int page_len,
                              const void* k_cache, const void* v_cache, const uint16_t* k_stat,
                              const uint16_t* v_stat) {
-  if (H_kv < 1 || H_kv > 4096) return fail(UQ_EINVAL, "%s: H_kv=%d must be in [1, 4096]", fn, H_kv);
-  if (d < 1) return fail(UQ_EINVAL, "%s: d=%d must be >= 1", fn, d);
-  if (d != 64 && d != 128) return fail(UQ_EUNSUPPORTED, "%s: d=%d, supported 64 and 128", fn, d);
+  if (uq_status st = check_cache_sizes(fn, H_kv, d, n_seq, max_pages, page_len)) return st;
   if (format < UQ_KV_BF16 || format > UQ_KV_U4) return fail(UQ_EINVAL, "%s: bad format %d", fn, format);
   if (format == UQ_KV_BF16 ? group != 0 : (group != 32 && group != d))
     return fail(UQ_EINVAL, "%s: group=%d must be 0 for bf16 and 32 or d=%d for codes", fn, group, d);
-  if (page_len < 16 || page_len > 1024 || (page_len & (page_len - 1)) != 0)
-    return fail(UQ_EINVAL, "%s: page_len=%d must be a power of two in [16, 1024]", fn, page_len);
-  const int64_t lim = int64_t(1) << 31;
-  if (n_pages < 1 || n_pages >= lim) return fail(UQ_EINVAL, "%s: n_pages=%lld must be in [1, 2^31)", fn, (long long)n_pages);
-  if (n_seq < 1 || n_seq >= lim) return fail(UQ_EINVAL, "%s: n_seq=%lld must be in [1, 2^31)", fn, (long long)n_seq);
-  if (max_pages < 1 || max_pages > (lim / 2) / page_len)
-    return fail(UQ_EINVAL, "%s: max_pages=%lld must be >= 1 and max_pages * page_len <= 2^30", fn, (long long)max_pages);
+  if (n_pages < 1 || n_pages >= int64_t(1) << 31)
+    return fail(UQ_EINVAL, "%s: n_pages=%lld must be in [1, 2^31)", fn, (long long)n_pages);
   REQ_PTR(pages, 4); REQ_PTR(k_cache, 16); REQ_PTR(v_cache, 16);
   if (format != UQ_KV_BF16) {
     REQ_PTR(k_stat, 16); REQ_PTR(v_stat, 16);
@@ -854,8 +861,19 @@ uq_status uniquan_kv_read(int64_t n_seq, int H_kv, int d, int64_t L, const int32
   return hip_status(fn, uq::launch_kv_read(p, static_cast<hipStream_t>(stream)));
 }
 
+// Sizes of an attn_decode that check_cache lets through: what its grid and its counts of blocks take.
+static uq_status check_decode(const char* fn, int64_t n_seq, int H, int64_t max_pages, int page_len) {
+  if (n_seq > (int64_t(1) << 24) / H) return fail(UQ_EUNSUPPORTED, "%s: n_seq * H > 2^24", fn);
+  if (n_seq > (int64_t(1) << 37) / (max_pages * page_len + 256))
+    return fail(UQ_EUNSUPPORTED, "%s: n_seq max_pages page_len > 2^37", fn);
+  return UQ_OK;
+}
+
 size_t uniquan_attn_decode_ws(int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len) {
-  if (n_seq < 1 || H_kv < 1 || H < H_kv || d < 1 || max_pages < 1 || page_len < 1) return 0;
+  const char* fn = "uniquan_attn_decode_ws";
+  if (check_cache_sizes(fn, H_kv, d, n_seq, max_pages, page_len) || check_heads(fn, H, H_kv) ||
+      check_decode(fn, n_seq, H, max_pages, page_len))
+    return 0;
   return uq::attn_decode_ws(n_seq, H, H_kv, d, max_pages, page_len);
 }
 
@@ -870,9 +888,7 @@ uq_status uniquan_attn_decode(int64_t n_seq, int H, int H_kv, int d, const uint1
                                  v_cache, k_stat, v_stat))
     return st;
   if (uq_status st = check_heads(fn, H, H_kv)) return st;
-  if (n_seq > (int64_t(1) << 24) / H) return fail(UQ_EUNSUPPORTED, "%s: n_seq * H > 2^24", fn);
-  if (n_seq > (int64_t(1) << 37) / (max_pages * page_len + 256))
-    return fail(UQ_EUNSUPPORTED, "%s: n_seq max_pages page_len > 2^37", fn);
+  if (uq_status st = check_decode(fn, n_seq, H, max_pages, page_len)) return st;
   if (uq_status st = check_ld(fn, "ld_q", &ld_q, int64_t(H) * d, 8)) return st;
   if (uq_status st = check_ld(fn, "ld_o", &ld_o, int64_t(H) * d, 4)) return st;
   REQ_PTR(Q, 16); REQ_PTR(lens, 4); REQ_PTR(O, 8); OPT_PTR(row_lse, 4);
