@@ -626,7 +626,7 @@ def uniquan_attn_bwd(batch, kv_batch, L, d, Q, K, V, O, dO, row_lse, scale, delt
 
 def _one_device(*tensors):
     """Raise unless every tensor given lies on the current device (whose streams the calls run on)."""
-    here = torch.cuda.current_device() if torch.cuda.is_available() else None
+    here = torch.cuda.current_device() if torch.cuda.is_initialized() else None
     for t in tensors:
         if isinstance(t, torch.Tensor) and t.is_cuda and t.device.index != here:
             raise ValueError(f"tensor on {t.device}, the current device is cuda:{here}")
@@ -636,7 +636,7 @@ def _whole(t, shape, name):
     """t as it is, refused where its shape says that its values lie otherwise than in a contiguous tensor of `shape`:
     as many dimensions must agree (the first may be larger), a flat tensor holds that many values or more, any other
     exactly that many."""
-    if not isinstance(t, torch.Tensor) or t.dim() < 2:
+    if not isinstance(t, torch.Tensor) or t.shape == shape or t.dim() < 2:
         return t
     got = tuple(t.shape)
     if len(got) == len(shape):
