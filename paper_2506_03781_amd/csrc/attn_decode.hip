@@ -65,13 +65,13 @@
 // size in fp32, whose roundings are 2^-150 at the least: 2^-81 of the output.
 //
 // Bound and measured (the kernel alone; a sequence split over shares adds the
-// join, 4 to 7 us, a launch and two loads that wait on each other).  bf16 and
+// join, 4 to 8 us, a launch and two loads that wait on each other).  bf16 and
 // 8-bit caches by memory: 64 sequences of up to 16384 positions, 64 heads on 8,
-// 1.96 GB in 337 us, 5.8 TB/s; 48 of up to 8192 at 8 bits 391 MB in 74 us, 5.3
-// TB/s; 4 of 2048, 32 heads, 134 MB in 25.6 us, 5.2 TB/s.  4-bit caches read a
+// 1.96 GB in 337 us, 5.8 TB/s; 48 of up to 8192 at 8 bits 391 MB in 75 us, 5.2
+// TB/s; 4 of 2048, 32 heads, 134 MB in 25.7 us, 5.2 TB/s.  4-bit caches read a
 // quarter of the bytes with the same number of loads: 100001 positions in groups
-// of 32 128 MB in 33.6 us, 3.8 TB/s, vector instructions in 56% of the cycles,
-// matrix ones in 24%.  One sequence of 100 positions 5.6 us: a launch and the
+// of 32 128 MB in 33.4 us, 3.8 TB/s, vector instructions in 57% of the cycles,
+// matrix ones in 24%.  One sequence of 100 positions 5.7 us: a launch and the
 // loads of its length, its page and its rows, one after the other.
 #include <hip/hip_runtime.h>
 #include <stdint.h>

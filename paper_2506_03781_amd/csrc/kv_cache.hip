@@ -4,8 +4,8 @@
 // Both are bound by memory: every kernel moves 16 bytes a lane where the
 // layout lets it and keeps several rows in flight.  Measured: 8192 rows of 32 + 8
 // + 8 heads into an 8-bit cache 185 MB in 36.7 us, 5.0 TB/s; 100002 positions of
-// 8 heads from 4 bits to fp32 947 MB (819 of them written) in 229 us, 4.1 TB/s; one row of
-// 32 heads 2.8 us, a launch and the loads of its position and page.
+// 8 heads from 4 bits to fp32 947 MB (819 of them written) in 230 us, 4.1 TB/s; one row of
+// 32 heads 2.6 us, a launch and the loads of its position and page.
 //
 // Append.  A workgroup takes a row (few rows: a tile of heads of a row).
 // Heads that are stored in channel order (queries, keys, values of a bf16
