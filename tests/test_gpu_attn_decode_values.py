@@ -9,7 +9,7 @@ import torch
 
 import oracle.kv_cache as KV
 from attend_bars import attend, bars, broken, store
-from kv_cases import attend_bounds, filled, rounded, tables
+from kv_cases import attend_bounds, dev, filled, on_device, rounded, tables
 from paper_2506_03781_amd import uniquan as uq
 
 pytestmark = pytest.mark.gpu
@@ -219,3 +219,25 @@ def test_queries_that_are_not_finite(fmt, group, grp):
     hit[2] = True
     within(O[~hit], ref[~hit], tol[~hit])
     within(lse[~hit], ref_l[~hit], tol_l[~hit])
+
+
+def test_rows_behind_the_last_sequence_stay():
+    """O and the log-sum-exp may have more rows than there are sequences; those are left as they were."""
+    rs = np.random.default_rng(78)
+    lens = [300, 0, 17]
+    c = filled(rs, lens, 2, 64, 16, "u8", 32)
+    q = rounded(rs, 5, 8, 64)
+    m = on_device(c)
+    O = torch.full((5, 512), 7.0, device="cuda", dtype=torch.bfloat16)
+    lse = torch.full((5, 8), 7.0, device="cuda")
+    uq.uniquan_attn_decode(3, 8, 2, 64, dev(q.reshape(5, 512)).bfloat16(), dev(np.array(lens + [9, 9], np.int32)),
+                           scale=0.125, O=O, row_lse=lse,
+                           ws=torch.empty(max(1, uq.uniquan_attn_decode_ws(3, 8, 2, 64, m["table"].shape[1], 16)),
+                                          device="cuda"), **m)
+    torch.cuda.synchronize()
+    assert bool((O[3:] == 7).all()) and bool((lse[3:] == 7).all())
+    ref, ref_l, tol, tol_l = attend_bounds(c, q[:3], lens, 0.125)
+    within(O[:3].float().cpu().numpy().reshape(3, 8, 64), ref, tol)
+    got = lse[:3].cpu().numpy().astype(np.float64)
+    assert np.all(got[1] == -np.inf)
+    within(got[[0, 2]], ref_l[[0, 2]], tol_l[[0, 2]])
