@@ -92,3 +92,42 @@ def test_loop_that_advances_itself(fmt):
         other.run()
         for got, w in zip(b.outputs(), want):
             assert np.array_equal(got, w), (fmt, replay)
+
+
+@pytest.mark.parametrize("shared", [False, True])
+def test_two_graphs_and_their_workspaces(shared):
+    """Two captured loops replayed in turn: each with the workspace that attend takes for itself while it is captured,
+    or both with one, which may be used again once a replay is done."""
+    loops, graphs, wants = [], [], []
+    for seed, fmt in ((3, "bf16"), (4, "u4")):
+        eager = Loop(fmt, seed)
+        eager.run()
+        wants.append(eager.outputs())
+        s = Loop(fmt, seed)
+        s.ws = loops[0].ws if shared and loops else s.ws if shared else None
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            s.run()
+        loops.append(s)
+        graphs.append(g)
+    for _ in range(3):
+        for s in loops:
+            s.rewind()
+        for g in graphs:
+            g.replay()
+        for s, want in zip(loops, wants):
+            assert all(np.array_equal(x, y) for x, y in zip(s.outputs(), want))
+
+
+def test_current_stream_other_than_the_default():
+    """Under a stream that torch makes current, attend takes its workspace there."""
+    a, b = Loop("u8", 5), Loop("u8", 5)
+    a.ws = b.ws = None
+    side = torch.cuda.Stream()
+    a.run()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        b.run()
+    for x, y in zip(a.outputs(), b.outputs()):
+        assert np.array_equal(x, y)
