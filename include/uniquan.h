@@ -810,6 +810,33 @@ uq_status uniquan_kv_append(int64_t T, int H, int H_kv, int d,
                             uint16_t* q_out, void* stream);
 
 /*
+ * uniquan_kv_append_axes -- uniquan_kv_append with the positions of the rotation
+ * apart from the places in the cache, and on several axes: pair i of a head
+ * (channels i and i + d/2) of row t is rotated by row rot[t n_axes + axis[i]] of
+ * cs, while the row is stored at place pos[t] of its sequence.  With one axis
+ * this appends a tree of drafted tokens, whose siblings share a position; with
+ * three (time, height, width) the rows of images and videos, axis naming each
+ * pair's, in runs or interleaved.  A pair whose axis is not in [0, n_axes) is not
+ * rotated.  A row is padding where one of its n_axes positions is not in
+ * [0, n_cs) (used or not), its place not in [0, max_pages page_len) or its
+ * sequence not in [0, n_seq).
+ *
+ * rot [T x n_axes], axis [d/2] int32; n_axes in [1, 8]; cs must be given.
+ * Everything else as for uniquan_kv_append; with n_axes 1, axis all 0 and rot
+ * equal to pos the results are that call's, bit for bit.
+ */
+uq_status uniquan_kv_append_axes(int64_t T, int H, int H_kv, int d,
+                                 const void* q, int64_t ld_q, const void* k, int64_t ld_k,
+                                 const void* v, int64_t ld_v, int in_dtype,
+                                 const int32_t* seq, const int32_t* pos,
+                                 const int32_t* rot, int n_axes, const int32_t* axis,
+                                 const float* cs, int64_t n_cs,
+                                 const int32_t* pages, int64_t n_seq, int64_t max_pages,
+                                 int format, int group, int64_t n_pages, int page_len,
+                                 void* k_cache, void* v_cache, uint16_t* k_stat, uint16_t* v_stat,
+                                 uint16_t* q_out, void* stream);
+
+/*
  * uniquan_kv_read -- positions [start[s], start[s] + L) of every sequence
  * (start NULL: 0) back from the cache: K and V [H_kv][n_seq][L][d], the
  * key/value layout of uniquan_attn_fwd (batch h n_seq + s), out_dtype UQ_F32
@@ -866,6 +893,41 @@ uq_status uniquan_attn_decode(int64_t n_seq, int H, int H_kv, int d,
                               const uint16_t* k_stat, const uint16_t* v_stat,
                               float scale, uint16_t* O, int64_t ld_o, float* row_lse,
                               float* ws, size_t ws_len, void* stream);
+
+/*
+ * uniquan_sample -- one token per row of logits x [V], from a given random number:
+ * the end of a serving step.  With t = temperature and M the largest logit,
+ *   w_i = e^((x_i - M) / t), in units of 2^-sh, sh = min(52, 62 - ceil(log2 V))
+ *         (an integer each, rounded to nearest from 64-bit arithmetic);
+ *   order: larger logits first, equal ones by index;
+ *   top_k  the first top_k in order (<= 0 or >= V: all);
+ *   top_p  of those, the ones before which the weights sum to less than top_p
+ *          times the sum over all of them (>= 1: all; <= 0: the first);
+ *   min_p  of those, the ones with w_i >= min_p (<= 0: all; the first always);
+ *   token  the lowest index at which the running sum, by index, of the weights that
+ *          are left exceeds u times their sum (u <= 0: the first with a weight,
+ *          u >= 1: the last); prob its share of that sum.
+ * The sums are exact, so a token is another than in real arithmetic only where u,
+ * top_p, or min_p lie within about V 2^-sh (1e-9 of the sum at V = 131072) of a
+ * border, and results do not depend on how the work is split.  temperature <= 0
+ * or NaN: the first in order, prob 1.  A NaN logit counts as -infinity; tokens at
+ * -infinity are not chosen; a row of nothing else has token -1, prob 0.  Where the
+ * largest logit is +infinity, only those at it have a weight.  NaN for u counts as
+ * 0, for top_p as 1, for min_p as 0.
+ *
+ * logits [T] rows of V x_dtype (UQ_F32 or UQ_BF16), ld elements apart (0: V; any
+ * distance, 16-byte aligned as a whole); u [T] fp32; temperature, top_p, min_p [T]
+ * fp32, top_k [T] int32, each NULL where the step does not apply (temperature: 1);
+ * token [T] int32; prob [T] fp32 or NULL.  1 <= V <= 2^22; T >= 0.  ws [ws_len] fp32
+ * workspace of at least uniquan_sample_ws(T, V) floats (16-byte aligned; 0: may be
+ * NULL), of any contents, free to be reused once the call is done; calls that
+ * overlap need one each.
+ */
+size_t uniquan_sample_ws(int64_t T, int64_t V);
+uq_status uniquan_sample(int64_t T, int64_t V, const void* logits, int64_t ld, int x_dtype,
+                         const float* u, const float* temperature, const int32_t* top_k,
+                         const float* top_p, const float* min_p,
+                         int32_t* token, float* prob, float* ws, size_t ws_len, void* stream);
 
 /*
  * uniquan_init_greedy -- greedy binary-coding start of the appendix

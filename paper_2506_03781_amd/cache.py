@@ -56,12 +56,19 @@ class KVCache:
     def _form(self):
         return dict(fmt=self.fmt, group=self.group, page_len=self.page_len, k_stat=self.k_stat, v_stat=self.v_stat)
 
-    def append(self, k, v, pos, q=None, q_out=None, seq=None, cs=None, stream=None):
+    def append(self, k, v, pos, q=None, q_out=None, seq=None, cs=None, stream=None, rot=None, axis=None):
         """Rows k, v [T, n_kv d] at positions pos [T] of sequences seq [T] (None: row t of sequence t); q [T, H d]
-        to q_out; q and k rotated by cs where given."""
+        to q_out; q and k rotated by cs where given: at pos, or, with rot [T, n_axes] and axis [d / 2], pair i at
+        rot[t, axis[i]] (drafted tokens whose place is not their position, images and videos)."""
         H = self.n_kv if q is None else q.shape[1] // self.d
-        uq.uniquan_kv_append(k.shape[0], H, self.n_kv, self.d, q, k, v, pos, self.table, self.k, self.v, q_out, seq=seq,
-                             cs=cs, stream=stream, **self._form())
+        rows = (k.shape[0], H, self.n_kv, self.d, q, k, v, pos)
+        if (rot is None) != (axis is None):
+            raise ValueError("rot and axis must be given together")
+        if rot is None:
+            uq.uniquan_kv_append(*rows, self.table, self.k, self.v, q_out, seq=seq, cs=cs, stream=stream, **self._form())
+        else:
+            uq.uniquan_kv_append_axes(*rows, rot, axis, cs, self.table, self.k, self.v, q_out, seq=seq, stream=stream,
+                                      **self._form())
 
     def read(self, lens, L, K, V, start=None, stream=None):
         """Positions start[s] .. + L of every sequence into K, V [n_kv, n_seq, L, d] (fp32 or bf16)."""

@@ -811,12 +811,13 @@ static uq_status check_heads(const char* fn, int H, int H_kv) {
   return UQ_OK;
 }
 
-uq_status uniquan_kv_append(int64_t T, int H, int H_kv, int d, const void* q, int64_t ld_q, const void* k, int64_t ld_k,
-                            const void* v, int64_t ld_v, int in_dtype, const int32_t* seq, const int32_t* pos,
-                            const float* cs, int64_t n_cs, const int32_t* pages, int64_t n_seq, int64_t max_pages,
-                            int format, int group, int64_t n_pages, int page_len, void* k_cache, void* v_cache,
-                            uint16_t* k_stat, uint16_t* v_stat, uint16_t* q_out, void* stream) {
-  const char* fn = "uniquan_kv_append";
+// The appending calls; rot, axis, n_axes: uniquan_kv_append_axes (axes), NULL and 0 without.
+static uq_status kv_append(const char* fn, bool axes, int64_t T, int H, int H_kv, int d, const void* q, int64_t ld_q,
+                           const void* k, int64_t ld_k, const void* v, int64_t ld_v, int in_dtype, const int32_t* seq,
+                           const int32_t* pos, const int32_t* rot, int n_axes, const int32_t* axis, const float* cs,
+                           int64_t n_cs, const int32_t* pages, int64_t n_seq, int64_t max_pages, int format, int group,
+                           int64_t n_pages, int page_len, void* k_cache, void* v_cache, uint16_t* k_stat,
+                           uint16_t* v_stat, uint16_t* q_out, void* stream) {
   uq::KvAppendLaunch p{};
   if (uq_status st = check_cache(fn, &p.c, H_kv, d, pages, n_seq, max_pages, format, group, n_pages, page_len, k_cache,
                                  v_cache, k_stat, v_stat))
@@ -826,20 +827,46 @@ uq_status uniquan_kv_append(int64_t T, int H, int H_kv, int d, const void* q, in
   if (!is_dtype(in_dtype)) return fail(UQ_EINVAL, "%s: bad dtype", fn);
   if ((q == nullptr) != (q_out == nullptr)) return fail(UQ_EINVAL, "%s: q and q_out must be given together", fn);
   if (q == nullptr && H != H_kv) return fail(UQ_EINVAL, "%s: H=%d must be H_kv=%d without q", fn, H, H_kv);
-  if (cs != nullptr && n_cs < 1) return fail(UQ_EINVAL, "%s: n_cs=%lld must be >= 1", fn, (long long)n_cs);
+  if ((axes || cs != nullptr) && n_cs < 1) return fail(UQ_EINVAL, "%s: n_cs=%lld must be >= 1", fn, (long long)n_cs);
+  if (axes && (n_axes < 1 || n_axes > 8)) return fail(UQ_EINVAL, "%s: n_axes=%d must be in [1, 8]", fn, n_axes);
   if (uq_status st = check_ld(fn, "ld_q", &ld_q, int64_t(H) * d, 8)) return st;
   if (uq_status st = check_ld(fn, "ld_k", &ld_k, int64_t(H_kv) * d, 8)) return st;
   if (uq_status st = check_ld(fn, "ld_v", &ld_v, int64_t(H_kv) * d, 8)) return st;
   if (T > (int64_t(1) << 28) / (int64_t(H) + 2 * H_kv)) return fail(UQ_EUNSUPPORTED, "%s: T (H + 2 H_kv) > 2^28", fn);
   if (T == 0) return UQ_OK;
   OPT_PTR(q, 16); REQ_PTR(k, 16); REQ_PTR(v, 16); OPT_PTR(seq, 4); REQ_PTR(pos, 4); OPT_PTR(cs, 16); OPT_PTR(q_out, 16);
+  if (axes) {
+    REQ_PTR(rot, 4); REQ_PTR(axis, 4); REQ_PTR(cs, 16);
+  }
   p.T = T; p.H = H;
   p.q = q; p.k = k; p.v = v;
   p.ld_q = ld_q; p.ld_k = ld_k; p.ld_v = ld_v;
   p.in_dtype = in_dtype;
   p.seq = seq; p.pos = pos; p.cs = cs; p.n_cs = n_cs;
   p.q_out = q_out;
+  p.rot = rot; p.axis = axis; p.n_axes = n_axes;
   return hip_status(fn, uq::launch_kv_append(p, static_cast<hipStream_t>(stream)));
+}
+
+uq_status uniquan_kv_append(int64_t T, int H, int H_kv, int d, const void* q, int64_t ld_q, const void* k, int64_t ld_k,
+                            const void* v, int64_t ld_v, int in_dtype, const int32_t* seq, const int32_t* pos,
+                            const float* cs, int64_t n_cs, const int32_t* pages, int64_t n_seq, int64_t max_pages,
+                            int format, int group, int64_t n_pages, int page_len, void* k_cache, void* v_cache,
+                            uint16_t* k_stat, uint16_t* v_stat, uint16_t* q_out, void* stream) {
+  return kv_append("uniquan_kv_append", false, T, H, H_kv, d, q, ld_q, k, ld_k, v, ld_v, in_dtype, seq, pos, nullptr, 0,
+                   nullptr, cs, n_cs, pages, n_seq, max_pages, format, group, n_pages, page_len, k_cache, v_cache, k_stat,
+                   v_stat, q_out, stream);
+}
+
+uq_status uniquan_kv_append_axes(int64_t T, int H, int H_kv, int d, const void* q, int64_t ld_q, const void* k,
+                                 int64_t ld_k, const void* v, int64_t ld_v, int in_dtype, const int32_t* seq,
+                                 const int32_t* pos, const int32_t* rot, int n_axes, const int32_t* axis,
+                                 const float* cs, int64_t n_cs, const int32_t* pages, int64_t n_seq, int64_t max_pages,
+                                 int format, int group, int64_t n_pages, int page_len, void* k_cache, void* v_cache,
+                                 uint16_t* k_stat, uint16_t* v_stat, uint16_t* q_out, void* stream) {
+  return kv_append("uniquan_kv_append_axes", true, T, H, H_kv, d, q, ld_q, k, ld_k, v, ld_v, in_dtype, seq, pos, rot,
+                   n_axes, axis, cs, n_cs, pages, n_seq, max_pages, format, group, n_pages, page_len, k_cache, v_cache,
+                   k_stat, v_stat, q_out, stream);
 }
 
 uq_status uniquan_kv_read(int64_t n_seq, int H_kv, int d, int64_t L, const int32_t* start, const int32_t* lens,
@@ -898,6 +925,38 @@ uq_status uniquan_attn_decode(int64_t n_seq, int H, int H_kv, int d, const uint1
   p.H = H; p.Q = Q; p.ld_q = ld_q; p.lens = lens; p.scale = scale;
   p.O = O; p.ld_o = ld_o; p.lse = row_lse; p.ws = ws;
   return hip_status(fn, uq::launch_attn_decode(p, static_cast<hipStream_t>(stream)));
+}
+
+static uq_status check_sample(const char* fn, int64_t T, int64_t V) {
+  if (T < 0 || T >= int64_t(1) << 31) return fail(UQ_EINVAL, "%s: T=%lld must be in [0, 2^31)", fn, (long long)T);
+  if (V < 1) return fail(UQ_EINVAL, "%s: V=%lld must be >= 1", fn, (long long)V);
+  if (V > int64_t(1) << 22) return fail(UQ_EUNSUPPORTED, "%s: V=%lld > 2^22", fn, (long long)V);
+  return UQ_OK;
+}
+
+size_t uniquan_sample_ws(int64_t T, int64_t V) {
+  return check_sample("uniquan_sample_ws", T, V) ? 0 : uq::sample_ws(T, V);
+}
+
+uq_status uniquan_sample(int64_t T, int64_t V, const void* logits, int64_t ld, int x_dtype, const float* u,
+                         const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p,
+                         int32_t* token, float* prob, float* ws, size_t ws_len, void* stream) {
+  const char* fn = "uniquan_sample";
+  if (uq_status st = check_sample(fn, T, V)) return st;
+  if (!is_dtype(x_dtype)) return fail(UQ_EINVAL, "%s: bad dtype", fn);
+  if (uq_status st = check_ld(fn, "ld", &ld, V, 1)) return st;
+  const size_t need = uq::sample_ws(T, V);
+  if (ws_len < need) return fail(UQ_EINVAL, "%s: ws_len=%zu < %zu", fn, ws_len, need);
+  if (T == 0) return UQ_OK;
+  if (need > 0) REQ_PTR(ws, 16);
+  REQ_PTR(logits, 16); REQ_PTR(u, 4); REQ_PTR(token, 4); OPT_PTR(prob, 4);
+  OPT_PTR(temperature, 4); OPT_PTR(top_k, 4); OPT_PTR(top_p, 4); OPT_PTR(min_p, 4);
+  uq::SampleLaunch p{};
+  p.T = T; p.V = int(V);
+  p.x = logits; p.ld = ld; p.x_dtype = x_dtype;
+  p.u = u; p.temperature = temperature; p.top_k = top_k; p.top_p = top_p; p.min_p = min_p;
+  p.token = token; p.prob = prob; p.ws = ws;
+  return hip_status(fn, uq::launch_sample(p, static_cast<hipStream_t>(stream)));
 }
 
 double uniquan_probe_mfma_flops(int iters) {

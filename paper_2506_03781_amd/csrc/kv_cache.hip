@@ -97,12 +97,20 @@ struct Row {
   int pos, page;
 };
 // False: padding.
+template <bool AXES>
 __device__ __forceinline__ bool row_of(const KvAppendLaunch& p, int64_t t, Row& r) {
   const KvCache& c = p.c;
   r.pos = p.pos[t];
   r.seq = p.seq ? p.seq[t] : t;
-  if (r.pos < 0 || r.pos >= c.max_pages << c.log_page || (p.cs && r.pos >= p.n_cs) || r.seq < 0 || r.seq >= c.n_seq)
+  if (r.pos < 0 || r.pos >= c.max_pages << c.log_page || (!AXES && p.cs && r.pos >= p.n_cs) || r.seq < 0 ||
+      r.seq >= c.n_seq)
     return false;
+  if constexpr (AXES) {
+    for (int a = 0; a < p.n_axes; ++a) {
+      const int at = p.rot[t * p.n_axes + a];
+      if (at < 0 || at >= p.n_cs) return false;
+    }
+  }
   r.page = kv_page(c, r.seq, r.pos);
   return true;
 }
@@ -124,7 +132,8 @@ __device__ __forceinline__ void store_run(uint8_t* row, int r, const float (&x)[
   }
 }
 
-template <int D, int FMT, bool F32>
+// AXES: pair i is rotated at position rot[t][axis[i]], which is not the row's place.
+template <int D, int FMT, bool F32, bool AXES>
 __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendLaunch p) {
   constexpr int LANES = D / 16, SLOTS = 256 / LANES;  // of a head in channel order, heads of a tile
   constexpr int DT = F32 ? DType::F32 : DType::BF16;
@@ -134,7 +143,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendLaunch p) {
   const KvCache& c = p.c;
   const int64_t t = workgroup();
   Row r;
-  if (t >= p.T || !row_of(p, t, r)) return;
+  if (t >= p.T || !row_of<AXES>(p, t, r)) return;
   const int place = r.pos & (c.page_len - 1);
   const int64_t ph0 = int64_t(r.page) * c.H_kv;
   const int n_q = p.q ? p.H : 0;
@@ -142,7 +151,29 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendLaunch p) {
   const int tiles = (plain + SLOTS - 1) / SLOTS, vtiles = CODES ? (c.H_kv + 15) / 16 : 0;
   const int lane = threadIdx.x % LANES;
   float co[8], si[8];
-  if (p.cs && int(blockIdx.z) < tiles) {
+  uint32_t still = 0;  // AXES: pairs that are not rotated
+  if constexpr (AXES) {
+    if (int(blockIdx.z) < tiles) {
+      const int32_t* axis = p.axis + 8 * lane;
+      const int32_t* rot = p.rot + t * p.n_axes;
+      const float2* cs = reinterpret_cast<const float2*>(p.cs) + 8 * lane;
+      int a[8], at[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) a[i] = axis[i];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const bool is = a[i] >= 0 && a[i] < p.n_axes;
+        still |= is ? 0u : 1u << i;
+        at[i] = rot[is ? a[i] : 0];
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float2 v = cs[int64_t(at[i]) * (D / 2) + i];
+        co[i] = v.x;
+        si[i] = v.y;
+      }
+    }
+  } else if (p.cs && int(blockIdx.z) < tiles) {
     const float4* cs = reinterpret_cast<const float4*>(p.cs + int64_t(r.pos) * D + 16 * lane);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -168,6 +199,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(KvAppendLaunch p) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float x1 = a[i], x2 = b[i];
+        if (AXES && (still >> i & 1)) continue;
         a[i] = x1 * co[i] - x2 * si[i];
         b[i] = x2 * co[i] + x1 * si[i];
       }
@@ -411,7 +443,10 @@ void append_form(const KvAppendLaunch& p, hipStream_t st) {
   // against 15.9, 4096 29.6 against 32.4).
   dim3 grid = grid_of(p.T);
   grid.z = p.T < 1536 ? unsigned(tiles) : 1u;
-  kv_append_kernel<D, FMT, F32><<<grid, 256, 0, st>>>(p);
+  if (p.rot)
+    kv_append_kernel<D, FMT, F32, true><<<grid, 256, 0, st>>>(p);
+  else
+    kv_append_kernel<D, FMT, F32, false><<<grid, 256, 0, st>>>(p);
 }
 template <int D>
 void append_d(const KvAppendLaunch& p, hipStream_t st) {

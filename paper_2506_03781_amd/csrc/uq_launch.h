@@ -216,6 +216,8 @@ struct KvAppendLaunch {
   const int32_t* seq; const int32_t* pos;
   const float* cs; int64_t n_cs;
   uint16_t* q_out;
+  const int32_t* rot; const int32_t* axis;  // NULL: pos is the position of the rotation
+  int n_axes;
 };
 struct KvReadLaunch {
   KvCache c;
@@ -234,6 +236,34 @@ struct AttnDecodeLaunch {
   float* lse;
   float* ws;
 };
+struct AttnExtendLaunch {
+  KvCache c;
+  int64_t T;
+  int H;
+  const uint16_t* Q; int64_t ld_q;
+  const int32_t* row_start; const int32_t* lens;
+  const uint64_t* mask; int words;  // NULL: rows see what lies before them
+  const int32_t* pos;               // NULL: base + j
+  int window, sinks;                // window 0: none
+  float scale;
+  uint16_t* O; int64_t ld_o;
+  float* lse;
+  float* ws;
+};
+struct SampleLaunch {
+  int64_t T;
+  int V;
+  const void* x; int64_t ld; int x_dtype;
+  const float* u;
+  const float* temperature; const int32_t* top_k; const float* top_p; const float* min_p;
+  int32_t* token; float* prob;
+  void* ws;
+  int sh;  // weights count in 2^-sh
+};
+hipError_t launch_attn_extend(const AttnExtendLaunch& p, hipStream_t st);
+size_t attn_extend_ws(int64_t T, int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len);
+hipError_t launch_sample(SampleLaunch p, hipStream_t st);
+size_t sample_ws(int64_t T, int64_t V);
 hipError_t launch_kv_append(const KvAppendLaunch& p, hipStream_t st);
 hipError_t launch_kv_read(const KvReadLaunch& p, hipStream_t st);
 hipError_t launch_attn_decode(const AttnDecodeLaunch& p, hipStream_t st);

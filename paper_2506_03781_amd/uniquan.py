@@ -90,11 +90,15 @@ _SIGS = {
                           _vp, _vp], _i32),
     "uniquan_kv_append": ([_i64, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _vp, _vp, _i64, _vp, _i64,
                            _i64, _i32, _i32, _i64, _i32, _vp, _vp, _vp, _vp, _vp, _vp], _i32),
+    "uniquan_kv_append_axes": ([_i64, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _vp, _vp, _i32, _vp,
+                                _vp, _i64, _vp, _i64, _i64, _i32, _i32, _i64, _i32, _vp, _vp, _vp, _vp, _vp, _vp], _i32),
     "uniquan_kv_read": ([_i64, _i32, _i32, _i64, _vp, _vp, _vp, _i64, _i32, _i32, _i64, _i32, _vp, _vp, _vp, _vp, _vp,
                          _vp, _i32, _vp], _i32),
     "uniquan_attn_decode_ws": ([_i64, _i32, _i32, _i32, _i64, _i32], ctypes.c_size_t),
     "uniquan_attn_decode": ([_i64, _i32, _i32, _i32, _vp, _i64, _vp, _vp, _i64, _i32, _i32, _i64, _i32, _vp, _vp, _vp,
                              _vp, _f32, _vp, _i64, _vp, _vp, ctypes.c_size_t, _vp], _i32),
+    "uniquan_sample_ws": ([_i64, _i64], ctypes.c_size_t),
+    "uniquan_sample": ([_i64, _i64, _vp, _i64, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp], _i32),
     "uniquan_probe_mfma_flops": ([_i32], ctypes.c_double),
     "uniquan_probe_stream": ([_i32, _i64, _vp, _vp, _vp, _i32, _vp], _i32),
     "uniquan_probe_mfma": ([_i32, _vp, _vp], _i32),
@@ -694,6 +698,17 @@ def _kv(Hkv, d, page_len, table, k_cache, v_cache, k_stat, v_stat, fmt, group):
              _p(k_stat, stats, _B, "k_stat"), _p(v_stat, stats, _B, "v_stat")))
 
 
+def _append_args(T, H, Hkv, d, q, k, v, table, k_cache, v_cache, cs, fmt, group, page_len, k_stat, v_stat):
+    """What the appending calls share, checked: the rows' arguments, then the cache's."""
+    (pg, n_seq, mp), f, m = _kv(Hkv, d, page_len, table, k_cache, v_cache, k_stat, v_stat, fmt, group)
+    if isinstance(cs, torch.Tensor) and cs.dim() >= 2 and math.prod(cs.shape[1:]) != d:
+        raise ValueError(f"cs has shape {tuple(cs.shape)}, expected [n, {d // 2}, 2]")
+    pk, ld_k = _ld(k, T, Hkv * d, _W, "k")
+    pv, ld_v = _ld(v, T, Hkv * d, (k.dtype,), "v")
+    pq, ld_q = _ld(q, T, H * d, (k.dtype,), "q")
+    return (T, H, Hkv, d, pq, ld_q, pk, ld_k, pv, ld_v, _dt(k)), (pg, n_seq, mp, *f, *m)
+
+
 def uniquan_kv_append(T, H, Hkv, d, q, k, v, pos, table, k_cache, v_cache, q_out=None, seq=None, cs=None, fmt=KV_BF16,
                       group=0, page_len=64, k_stat=None, v_stat=None, stream=None):
     """Rows q [T, H d], k, v [T, Hkv d] (fp32 or bf16; column slices allowed) at positions pos [T] of sequences
@@ -702,15 +717,27 @@ def uniquan_kv_append(T, H, Hkv, d, q, k, v, pos, table, k_cache, v_cache, q_out
     if not isinstance(k, torch.Tensor) or not isinstance(v, torch.Tensor):
         raise TypeError("k and v must be torch.Tensors")
     _one_device(q, k, v, pos, table, k_cache, v_cache, q_out, seq, cs, k_stat, v_stat)
-    (pg, n_seq, mp), f, m = _kv(Hkv, d, page_len, table, k_cache, v_cache, k_stat, v_stat, fmt, group)
-    if isinstance(cs, torch.Tensor) and cs.dim() >= 2 and math.prod(cs.shape[1:]) != d:
-        raise ValueError(f"cs has shape {tuple(cs.shape)}, expected [n, {d // 2}, 2]")
-    pk, ld_k = _ld(k, T, Hkv * d, _W, "k")
-    pv, ld_v = _ld(v, T, Hkv * d, (k.dtype,), "v")
-    pq, ld_q = _ld(q, T, H * d, (k.dtype,), "q")
+    rows, cache = _append_args(T, H, Hkv, d, q, k, v, table, k_cache, v_cache, cs, fmt, group, page_len, k_stat, v_stat)
     _check(lib().uniquan_kv_append(
-        T, H, Hkv, d, pq, ld_q, pk, ld_k, pv, ld_v, _dt(k), _p(seq, T, _I32, "seq"), _p(pos, T, _I32, "pos"),
-        _p(cs, None, _F, "cs"), 0 if cs is None else cs.numel() // d, pg, n_seq, mp, *f, *m,
+        *rows, _p(seq, T, _I32, "seq"), _p(pos, T, _I32, "pos"), _p(cs, None, _F, "cs"), 0 if cs is None else cs.numel() // d,
+        *cache, _p(_whole(q_out, (T, H * d), "q_out"), T * H * d, _B, "q_out"), _stream(stream)))
+
+
+def uniquan_kv_append_axes(T, H, Hkv, d, q, k, v, pos, rot, axis, cs, table, k_cache, v_cache, q_out=None, seq=None,
+                           fmt=KV_BF16, group=0, page_len=64, k_stat=None, v_stat=None, stream=None):
+    """uniquan_kv_append with the rotation's positions rot [T, n_axes] apart from the places pos [T]: pair i of row t
+    by row rot[t, axis[i]] of cs, axis [d/2] (outside [0, n_axes): not rotated)."""
+    if not isinstance(k, torch.Tensor) or not isinstance(v, torch.Tensor):
+        raise TypeError("k and v must be torch.Tensors")
+    if not isinstance(cs, torch.Tensor):
+        raise TypeError("cs must be a torch.Tensor")
+    if not isinstance(rot, torch.Tensor) or rot.dim() != 2 or rot.shape[0] != T:
+        raise ValueError(f"rot must be a [{T}, n_axes] tensor")
+    _one_device(q, k, v, pos, rot, axis, cs, table, k_cache, v_cache, q_out, seq, k_stat, v_stat)
+    rows, cache = _append_args(T, H, Hkv, d, q, k, v, table, k_cache, v_cache, cs, fmt, group, page_len, k_stat, v_stat)
+    _check(lib().uniquan_kv_append_axes(
+        *rows, _p(seq, T, _I32, "seq"), _p(pos, T, _I32, "pos"), _p(rot, rot.numel(), _I32, "rot"), rot.shape[1],
+        _p(_whole(axis, (d // 2,), "axis"), d // 2, _I32, "axis"), _p(cs, None, _F, "cs"), cs.numel() // d, *cache,
         _p(_whole(q_out, (T, H * d), "q_out"), T * H * d, _B, "q_out"), _stream(stream)))
 
 
@@ -750,6 +777,30 @@ def uniquan_attn_decode(n_seq, H, Hkv, d, Q, lens, table, k_cache, v_cache, scal
         n_seq, H, Hkv, d, pq, ld_q, _p(lens, n_seq, _I32, "lens"), pg, mp, *f, *m, float(scale), po, ld_o,
         _p(row_lse, n_seq * H, _F, "row_lse"), _p(ws, None, _F, "ws"), 0 if ws is None else ws.numel(),
         _stream(stream)))
+
+
+def uniquan_sample_ws(T, V) -> int:
+    return int(lib().uniquan_sample_ws(T, V))
+
+
+def uniquan_sample(T, V, logits, u, token, prob=None, temperature=None, top_k=None, top_p=None, min_p=None, ws=None,
+                   stream=None):
+    """token [T] (int32) and prob [T]: one token per row of logits [T, V] (fp32 or bf16; a column slice allowed) by
+    the random numbers u [T] and the rows' temperature, top_k (int32), top_p, min_p [T], each None where it does not
+    apply (see the header).  ws: fp32 workspace of uniquan_sample_ws floats."""
+    _one_device(logits, u, token, prob, temperature, top_k, top_p, min_p, ws)
+    if not isinstance(logits, torch.Tensor):
+        raise TypeError("logits must be a torch.Tensor")
+    px, ld = _ld(logits, T, V, _W, "logits")
+    need = uniquan_sample_ws(T, V)
+
+    def row(t, dtypes, name):
+        return _p(_whole(t, (T,), name), T, dtypes, name)
+
+    _check(lib().uniquan_sample(
+        T, V, px, ld, _dt(logits), row(u, _F, "u"), row(temperature, _F, "temperature"), row(top_k, _I32, "top_k"),
+        row(top_p, _F, "top_p"), row(min_p, _F, "min_p"), row(token, _I32, "token"), row(prob, _F, "prob"),
+        _p(ws, need, _F, "ws"), 0 if ws is None else ws.numel(), _stream(stream)))
 
 
 def uniquan_transpose_bf16_batched(batch, R, C, x, out, stream=None):
