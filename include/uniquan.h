@@ -643,6 +643,27 @@ uq_status uniquan_attn_bwd(int64_t batch, int64_t kv_batch, int L, int d,
                            int tok_seqs, int group, const float* cs, void* stream);
 
 /*
+ * uniquan_attn_window_fwd / uniquan_attn_window_bwd -- uniquan_attn_fwd / _bwd with a
+ * sliding window and a few first positions always in sight: query i sees the keys
+ * j <= i with i - j < window or j < sinks, and only the tiles that hold one of them
+ * are walked.  Formulas, layouts and outputs as there, but that P enters dS before
+ * it is rounded: dS = bf16(2^(c S - row_lse) (dP - delta)).  window >= 1, sinks >= 0
+ * (window >= L: the causal attention); any L >= 1 (up to 2^22, batch ceil(L / 128) at
+ * most 2^22); scale positive and finite.  Q, K, V, dO have to be finite: a key outside
+ * a query's sight has weight 0, not no part.
+ */
+uq_status uniquan_attn_window_fwd(int64_t batch, int64_t kv_batch, int L, int d,
+                                  const uint16_t* Q, const uint16_t* K, const uint16_t* V,
+                                  float scale, int window, int sinks, uint16_t* O, float* row_lse,
+                                  int tok_seqs, int group, void* stream);
+uq_status uniquan_attn_window_bwd(int64_t batch, int64_t kv_batch, int L, int d,
+                                  const uint16_t* Q, const uint16_t* K, const uint16_t* V,
+                                  const uint16_t* O, const uint16_t* dO, const float* row_lse,
+                                  float scale, int window, int sinks, float* delta,
+                                  void* dQ, void* dK, void* dV,
+                                  int tok_seqs, int group, const float* cs, void* stream);
+
+/*
  * uniquan_transpose_bf16_batched -- out_b = in_b^T for batch matrices
  * [R, C] stored back to back (bf16; in and out 8-byte aligned).
  */

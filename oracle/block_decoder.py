@@ -92,18 +92,22 @@ def merge_heads(x):
     return np.asarray(x, F64).transpose(0, 2, 1, 3).reshape(n * L, H * d)
 
 
-def causal_softmax(S):
-    """Row softmax of S [..., L, L] over keys j <= i."""
+def causal_softmax(S, window=0, sinks=0):
+    """Row softmax of S [..., L, L] over keys j <= i, with a window only those
+    with i - j < window or j < sinks."""
     S = np.asarray(S, F64)
     L = S.shape[-1]
     mask = np.triu(np.ones((L, L), dtype=bool), 1)
+    if window:
+        gap = np.arange(L)[:, None] - np.arange(L)
+        mask |= (gap >= window) & (np.arange(L) >= sinks)
     Sm = np.where(mask, -np.inf, S)
     Sm = Sm - np.max(Sm, axis=-1, keepdims=True)
     e = np.exp(Sm)
     return e / np.sum(e, axis=-1, keepdims=True)
 
 
-def decoder_forward(X, W, g1, g2, n_seq, H, store=_ident, n_kv=None):
+def decoder_forward(X, W, g1, g2, n_seq, H, store=_ident, n_kv=None, window=0, sinks=0):
     """All intermediates of the block on input X [T, C] with weights
     W = dict(q, o [C, C], k, v [n_kv d, C], g, u [I, C], d [C, I])
     (n_kv key/value heads, H by default)."""
@@ -121,7 +125,7 @@ def decoder_forward(X, W, g1, g2, n_seq, H, store=_ident, n_kv=None):
     Vh = store(split_heads(Z1 @ Wf["v"].T, n_seq, n_kv))
     Kx, Vx = np.repeat(Kh, grp, axis=1), np.repeat(Vh, grp, axis=1)   # head h reads key/value head h // grp
     S = Qh @ np.swapaxes(Kx, -1, -2) / np.sqrt(d)
-    P = store(causal_softmax(S))
+    P = store(causal_softmax(S, window, sinks))
     O = store(merge_heads(P @ Vx))
     A = O @ Wf["o"].T
     R = X + A
@@ -135,11 +139,11 @@ def decoder_forward(X, W, g1, g2, n_seq, H, store=_ident, n_kv=None):
                 H=Hm, Y=Y, ang=ang, n_kv=n_kv)
 
 
-def decoder_step(Xhat, Y_ref, W, g1, g2, n_seq, H, store=_ident, n_kv=None):
+def decoder_step(Xhat, Y_ref, W, g1, g2, n_seq, H, store=_ident, n_kv=None, window=0, sinks=0):
     """Loss ||Y(Xhat; W) - Y_ref||_F^2 and its gradient for each of the seven
     matrices (Algorithm 1's backpropagation; the input and the norm weights
     are not trained)."""
-    f = decoder_forward(Xhat, W, g1, g2, n_seq, H, store, n_kv)
+    f = decoder_forward(Xhat, W, g1, g2, n_seq, H, store, n_kv, window, sinks)
     grp = H // f["n_kv"]
     Wf = {n: np.asarray(w, F64) for n, w in W.items()}
     T, C = f["R"].shape

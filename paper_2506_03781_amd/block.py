@@ -145,6 +145,8 @@ class DecoderBlock:
     two halves of stacked [2I, C] arrays (their values kept), so that the
     backpropagation reads and writes both in one product each; with
     grouped-query attention, the W_hat and G arrays of k and v likewise.
+    With window > 0 the attention is that of a sliding window (token i sees
+    j <= i with i - j < window or j < sinks; any L then).
 
     ``prepare(X)`` computes the full-precision block's output on the
     full-precision input X (the target); ``set_input(Xhat)`` gives the
@@ -158,12 +160,14 @@ class DecoderBlock:
 
     NAMES = ("q", "k", "v", "o", "g", "u", "d")
 
-    def __init__(self, mats: dict, g1, g2, T, n_seq, H, n_kv=None, device="cuda"):
+    def __init__(self, mats: dict, g1, g2, T, n_seq, H, n_kv=None, device="cuda", window=0, sinks=0):
         q, gm = mats["q"], mats["g"]
         C, I = q.C, gm.R
         n_kv = H if n_kv is None else n_kv
         assert C % H == 0 and T % n_seq == 0 and H % n_kv == 0
-        assert C // H == 128 and (T // n_seq) % 32 == 0, "the fused attention takes d = 128 and L % 32 == 0"
+        assert C // H == 128 and (T // n_seq) % 32 == 0 or window, "the fused attention takes d = 128 and L % 32 == 0"
+        assert C // H == 128 and T % 32 == 0, "the weights' gradients take multiples of 32 tokens"
+        self.window, self.sinks = window, sinks
         self.mats, self.T, self.C, self.I, self.H, self.n_seq = mats, T, C, I, H, n_seq
         # backward: independent products in pairs on two streams.  Off: on the 7B
         # block the concurrent products slow each other down (11.5 against
@@ -255,8 +259,12 @@ class DecoderBlock:
             self._project_heads(W["v"], Hkv, self.Vh, 1, False, self.Vb)
         # causal attention with the score tiles on chip (query batch g Bkv + c uses key/value batch c)
         # (O written token-major: the merge of the heads is in the kernel's store)
-        uq.uniquan_attn_fwd(B, Bkv, L, d, self.Qh, self.Kh, self.Vh, sc, self.O, self.lse,
-                            tok_seqs=self.n_seq, group=grp)
+        how = dict(tok_seqs=self.n_seq, group=grp)
+        if self.window:
+            uq.uniquan_attn_window_fwd(B, Bkv, L, d, self.Qh, self.Kh, self.Vh, sc, self.window, self.sinks, self.O,
+                                       self.lse, **how)
+        else:
+            uq.uniquan_attn_fwd(B, Bkv, L, d, self.Qh, self.Kh, self.Vh, sc, self.O, self.lse, **how)
         # R = X + O W_o^T in the product's store, then the second norm of R
         uq.uniquan_gemm_nt_residual(T, C, C, self.O, W["o"], X, self.R)
         uq.uniquan_add_rmsnorm(T, C, self.R, None, self.g2, None, self.Z2, self.r2)
@@ -380,12 +388,14 @@ class DecoderBlock:
         Hkv, Ckv, Bkv, grp = self.Hkv, self.Ckv, self.Bkv, self.grp
         # O and dO token-major; dQ (and dK, dV with one query head per key/value
         # head) written token-major and inverse-rotated by the kernels' stores
-        if grp == 1:
-            uq.uniquan_attn_bwd(B, Bkv, L, d, self.Qh, self.Kh, self.Vh, self.O, self.dO, self.lse, sc, self.delta,
-                                self.dQ, self.dK, self.dV, tok_seqs=self.n_seq, group=grp, cs=self.rope_cs)
+        back = (self.Qh, self.Kh, self.Vh, self.O, self.dO, self.lse, sc)
+        outs = (self.delta, self.dQ, *((self.dK, self.dV) if grp == 1 else (self.dKp, self.dVp)))
+        how = dict(tok_seqs=self.n_seq, group=grp, cs=self.rope_cs)
+        if self.window:
+            uq.uniquan_attn_window_bwd(B, Bkv, L, d, *back, self.window, self.sinks, *outs, **how)
         else:
-            uq.uniquan_attn_bwd(B, Bkv, L, d, self.Qh, self.Kh, self.Vh, self.O, self.dO, self.lse, sc, self.delta,
-                                self.dQ, self.dKp, self.dVp, tok_seqs=self.n_seq, group=grp, cs=self.rope_cs)
+            uq.uniquan_attn_bwd(B, Bkv, L, d, *back, *outs, **how)
+        if grp > 1:
             uq.uniquan_rope_merge(T, Hkv, d, L, self.dKp, self.dK, rotate=True, nsum=grp, ld_out=2 * Ckv)
             uq.uniquan_rope_merge(T, Hkv, d, L, self.dVp, self.dV, rotate=False, nsum=grp, ld_out=2 * Ckv)
         uq.uniquan_gemm(C, C, T, self.dQ, 1, self.Z1, 1, m["q"].G)
@@ -447,11 +457,16 @@ class DecoderBlock:
         """GEMM flops of one step: the seven projections forward and their
         weight gradients, the input gradients through the MLP and the output
         projection, and the attention products forward and backward (the
-        causal half of each [L, L] product that is never computed is not
-        counted)."""
+        causal half of each [L, L] product that is never computed, and what a
+        window hides, is not counted)."""
         T, C, I, L, d, B = self.T, self.C, self.I, self.L, self.d, self.B
         lin = 2.0 * T * C * C * 2 + 2.0 * T * self.Ckv * C * 2 + 2.0 * T * C * I * 3
-        attn = 2.0 * B * (L * (L + 1) / 2) * d
+        pairs = L * (L + 1) / 2
+        if self.window and self.window < L:
+            w, more = self.window, L - self.window  # rows that see their whole window, and sinks before it
+            k = min(self.sinks, more)
+            pairs = w * (w + 1) / 2 + w * more + k * (k + 1) / 2 + k * (more - k)
+        attn = 2.0 * B * pairs * d
         return 2 * lin + 3 * (2.0 * T * C * I) + 2.0 * T * C * C + 6 * attn
 
     def output(self):

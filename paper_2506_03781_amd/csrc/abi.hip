@@ -694,14 +694,25 @@ uq_status uniquan_sgd(int64_t n, float* theta, const float* grad, float lr, void
   return hip_status(fn, uq::launch_sgd(n, theta, grad, lr, static_cast<hipStream_t>(stream)));
 }
 
-static uq_status check_attn(const char* fn, int64_t batch, int64_t kv_batch, int L, int d) {
+// win: uniquan_attn_window_fwd / _bwd.
+static uq_status check_attn(const char* fn, int64_t batch, int64_t kv_batch, int L, int d, bool win, float scale,
+                            int window, int sinks) {
   if (batch < 1 || kv_batch < 1 || batch % kv_batch != 0)
     return fail(UQ_EINVAL, "%s: batch=%lld must be a positive multiple of kv_batch=%lld", fn, (long long)batch,
                 (long long)kv_batch);
   if (batch > 65535) return fail(UQ_EUNSUPPORTED, "%s: batch=%lld > 65535", fn, (long long)batch);
   if (d != 128) return fail(UQ_EUNSUPPORTED, "%s: d=%d, supported 128", fn, d);
-  if (L < 32 || L % 32 != 0) return fail(UQ_EUNSUPPORTED, "%s: L=%d must be a positive multiple of 32", fn, L);
-  if (int64_t(L) * L >= (int64_t(1) << 31)) return fail(UQ_EUNSUPPORTED, "%s: L=%d too large", fn, L);
+  if (!win) {
+    if (L < 32 || L % 32 != 0) return fail(UQ_EUNSUPPORTED, "%s: L=%d must be a positive multiple of 32", fn, L);
+    if (int64_t(L) * L >= (int64_t(1) << 31)) return fail(UQ_EUNSUPPORTED, "%s: L=%d too large", fn, L);
+    return UQ_OK;
+  }
+  if (L < 1) return fail(UQ_EINVAL, "%s: L=%d must be >= 1", fn, L);
+  if (L > (1 << 22) || (L + 127) / 128 * batch > (int64_t(1) << 22))
+    return fail(UQ_EUNSUPPORTED, "%s: L=%d > 2^22 or batch ceil(L / 128) > 2^22", fn, L);
+  if (window < 1) return fail(UQ_EINVAL, "%s: window=%d must be >= 1", fn, window);
+  if (sinks < 0) return fail(UQ_EINVAL, "%s: sinks=%d must be >= 0", fn, sinks);
+  if (!(scale > 0.0f) || scale > 3.4e38f) return fail(UQ_EINVAL, "%s: scale=%g must be positive and finite", fn, scale);
   return UQ_OK;
 }
 
@@ -715,26 +726,25 @@ static uq_status check_tok(const char* fn, int64_t batch, int64_t kv_batch, int 
   return UQ_OK;
 }
 
-uq_status uniquan_attn_fwd(int64_t batch, int64_t kv_batch, int L, int d, const uint16_t* Q, const uint16_t* K,
-                           const uint16_t* V, float scale, uint16_t* O, float* row_lse, int tok_seqs, int group,
-                           void* stream) {
-  const char* fn = "uniquan_attn_fwd";
-  if (uq_status st = check_attn(fn, batch, kv_batch, L, d)) return st;
+static uq_status attn_fwd(const char* fn, bool win, int64_t batch, int64_t kv_batch, int L, int d, const uint16_t* Q,
+                          const uint16_t* K, const uint16_t* V, float scale, int window, int sinks, uint16_t* O,
+                          float* row_lse, int tok_seqs, int group, void* stream) {
+  if (uq_status st = check_attn(fn, batch, kv_batch, L, d, win, scale, window, sinks)) return st;
   if (uq_status st = check_tok(fn, batch, kv_batch, tok_seqs, group)) return st;
   REQ_PTR(Q, 16); REQ_PTR(K, 16); REQ_PTR(V, 16); REQ_PTR(O, 16); REQ_PTR(row_lse, 16);
   uq::AttnLaunch q{};
   q.batch = batch; q.kv_batch = kv_batch; q.L = L; q.scale = scale;
   q.Q = Q; q.K = K; q.V = V; q.O_out = O; q.lse = row_lse;
   q.tok_seqs = tok_seqs; q.group = group;
+  q.window = window; q.sinks = sinks;
   return hip_status(fn, uq::launch_attn_fwd(q, static_cast<hipStream_t>(stream)));
 }
 
-uq_status uniquan_attn_bwd(int64_t batch, int64_t kv_batch, int L, int d, const uint16_t* Q, const uint16_t* K,
-                           const uint16_t* V, const uint16_t* O, const uint16_t* dO, const float* row_lse, float scale,
-                           float* delta, void* dQ, void* dK, void* dV, int tok_seqs, int group, const float* cs,
-                           void* stream) {
-  const char* fn = "uniquan_attn_bwd";
-  if (uq_status st = check_attn(fn, batch, kv_batch, L, d)) return st;
+static uq_status attn_bwd(const char* fn, bool win, int64_t batch, int64_t kv_batch, int L, int d, const uint16_t* Q,
+                          const uint16_t* K, const uint16_t* V, const uint16_t* O, const uint16_t* dO,
+                          const float* row_lse, float scale, int window, int sinks, float* delta, void* dQ, void* dK,
+                          void* dV, int tok_seqs, int group, const float* cs, void* stream) {
+  if (uq_status st = check_attn(fn, batch, kv_batch, L, d, win, scale, window, sinks)) return st;
   if (uq_status st = check_tok(fn, batch, kv_batch, tok_seqs, group)) return st;
   REQ_PTR(Q, 16); REQ_PTR(K, 16); REQ_PTR(V, 16); REQ_PTR(O, 16);
   REQ_PTR(dO, 16); REQ_PTR(row_lse, 16); REQ_PTR(delta, 16);
@@ -744,6 +754,7 @@ uq_status uniquan_attn_bwd(int64_t batch, int64_t kv_batch, int L, int d, const 
   q.batch = batch; q.kv_batch = kv_batch; q.L = L; q.scale = scale;
   q.Q = Q; q.K = K; q.V = V; q.O = O; q.dO = dO;
   q.tok_seqs = tok_seqs; q.group = group; q.cs = cs;
+  q.window = window; q.sinks = sinks;
   const bool bf_kv = tok_seqs > 0 && kv_batch == batch;  // token-major bf16 dK, dV
   if (tok_seqs > 0) q.dQ_tok = static_cast<uint16_t*>(dQ);
   if (bf_kv) {
@@ -757,6 +768,36 @@ uq_status uniquan_attn_bwd(int64_t batch, int64_t kv_batch, int L, int d, const 
     q.dV = static_cast<float*>(dV);
   }
   return hip_status(fn, uq::launch_attn_bwd(q, static_cast<hipStream_t>(stream)));
+}
+
+uq_status uniquan_attn_fwd(int64_t batch, int64_t kv_batch, int L, int d, const uint16_t* Q, const uint16_t* K,
+                           const uint16_t* V, float scale, uint16_t* O, float* row_lse, int tok_seqs, int group,
+                           void* stream) {
+  return attn_fwd("uniquan_attn_fwd", false, batch, kv_batch, L, d, Q, K, V, scale, 0, 0, O, row_lse, tok_seqs, group,
+                  stream);
+}
+
+uq_status uniquan_attn_window_fwd(int64_t batch, int64_t kv_batch, int L, int d, const uint16_t* Q, const uint16_t* K,
+                                  const uint16_t* V, float scale, int window, int sinks, uint16_t* O, float* row_lse,
+                                  int tok_seqs, int group, void* stream) {
+  return attn_fwd("uniquan_attn_window_fwd", true, batch, kv_batch, L, d, Q, K, V, scale, window, sinks, O, row_lse,
+                  tok_seqs, group, stream);
+}
+
+uq_status uniquan_attn_bwd(int64_t batch, int64_t kv_batch, int L, int d, const uint16_t* Q, const uint16_t* K,
+                           const uint16_t* V, const uint16_t* O, const uint16_t* dO, const float* row_lse, float scale,
+                           float* delta, void* dQ, void* dK, void* dV, int tok_seqs, int group, const float* cs,
+                           void* stream) {
+  return attn_bwd("uniquan_attn_bwd", false, batch, kv_batch, L, d, Q, K, V, O, dO, row_lse, scale, 0, 0, delta, dQ, dK,
+                  dV, tok_seqs, group, cs, stream);
+}
+
+uq_status uniquan_attn_window_bwd(int64_t batch, int64_t kv_batch, int L, int d, const uint16_t* Q, const uint16_t* K,
+                                  const uint16_t* V, const uint16_t* O, const uint16_t* dO, const float* row_lse,
+                                  float scale, int window, int sinks, float* delta, void* dQ, void* dK, void* dV,
+                                  int tok_seqs, int group, const float* cs, void* stream) {
+  return attn_bwd("uniquan_attn_window_bwd", true, batch, kv_batch, L, d, Q, K, V, O, dO, row_lse, scale, window, sinks,
+                  delta, dQ, dK, dV, tok_seqs, group, cs, stream);
 }
 
 // Rules of the paged cache's sizes, without its format and arrays.

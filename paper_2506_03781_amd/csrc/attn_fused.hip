@@ -259,6 +259,8 @@ struct AttnArgs {
   uint16_t* dQ_tok;     // bf16 [n_seq L, heads D]
   uint16_t* dK_tok;     // bf16, when kv_batch == batch (else dK, dV per query head)
   uint16_t* dV_tok;
+  // WIN kernels: query i sees the keys j <= i with i - j < window or j < sinks
+  int window, sinks;    // both at most L
 };
 
 // Element offset of row l of query batch b in the token-major layout.
@@ -274,6 +276,42 @@ template <int PW>
 __device__ __forceinline__ void copy_tile(const uint16_t* base, const uint32_t (&off)[PW], u32x4a* tile, int wave) {
 #pragma unroll
   for (int q = 0; q < PW; ++q) copy16(base, off[q], tile + (wave * PW + q) * 64);
+}
+
+// Windows (WIN).  Any L: the rows of the last tile that lie behind L are copies
+// of row L - 1, which no query before them sees and whose own results are not
+// stored.  P enters dS before its rounding to bf16 (one rounding less in dQ and
+// dK: relative errors 2.4e-3 in place of 2.9e-3, the outputs' own rounding among
+// them).
+template <bool WIN, int PW>
+__device__ __forceinline__ void copy_rows(const uint16_t* base, const uint32_t (&off)[PW], u32x4a* tile, int wave, int lane,
+                                          int ld, int rows) {
+  if constexpr (WIN) {
+    if (rows < NB) {
+#pragma unroll
+      for (int q = 0; q < PW; ++q) {
+        const int s = (wave * PW + q) * 64 + lane;
+        const int over = max(0, perm32(s >> 4) - (rows - 1));
+        copy16(base, off[q] - uint32_t(over) * uint32_t(ld) * 2u, tile + (wave * PW + q) * 64);
+      }
+      return;
+    }
+  }
+  copy_tile<PW>(base, off, tile, wave);
+}
+
+// The key tiles that a run of queries [q0, q1) sees: those with sinks, then those of the window.
+struct KeyWalk {
+  int n_sink, shift, n;  // tile of step i: i below n_sink, else i + shift
+  __device__ __forceinline__ int tile(int i) const { return i < n_sink ? i : i + shift; }
+};
+__device__ __forceinline__ int first_tile(int q0, int window) { return max(0, q0 - window + 1) / NB; }
+__device__ __forceinline__ KeyWalk key_walk(int q0, int n_tiles, int window, int sinks) {
+  KeyWalk w;
+  w.n_sink = min((sinks + NB - 1) / NB, n_tiles);
+  w.shift = max(0, first_tile(q0, window) - w.n_sink);
+  w.n = n_tiles - w.shift;
+  return w;
 }
 
 // Split walks (KS = 2): a workgroup has KS groups of NW waves that own the same
@@ -319,7 +357,7 @@ __device__ __forceinline__ void add_groups(f32x16a (&acc)[4], float* smem, int w
 // fragments go from LDS straight into their MFMAs rather than into arrays
 // held across the tile: 156 registers, so three waves share a SIMD and one
 // wave's exponentials overlap another's products (two waves per SIMD at 243).
-template <int NW, int S, bool TOK, int KS>
+template <int NW, int S, bool TOK, int KS, bool WIN = false>
 __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(KS == 1 ? 3 : 2))) void attn_fwd_kernel(AttnArgs a) {
   constexpr int QB = NW * NB;
   constexpr int PW = 8 / NW;  // copy blocks per wave and tile
@@ -336,11 +374,23 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(KS
   const int q0 = qb * QB + wave * NB;
   const bool active = q0 < L;
   const int qi = q0 + (lane & 31);  // this lane's query
-  const int n_tiles = min(L, qb * QB + QB) / NB;
+  const int n_tiles = (min(L, qb * QB + QB) + (WIN ? NB - 1 : 0)) / NB;
   const int my_tiles = active ? q0 / NB + 1 : 0;
+  const KeyWalk walk = WIN ? key_walk(qb * QB, n_tiles, a.window, a.sinks) : KeyWalk{0, 0, n_tiles};
   // step i of the walk: tile i KS + ks (past the end the last tile is copied, unused)
-  const int n_steps = (n_tiles + KS - 1) / KS;
-  auto tile_at = [&](int i) { return int64_t(KS == 1 ? i : min(i * KS + ks, n_tiles - 1)); };
+  const int n_steps = (walk.n + KS - 1) / KS;
+  auto tile_at = [&](int i) {
+    const int j = KS == 1 ? i : min(i * KS + ks, walk.n - 1);
+    return int64_t(WIN ? walk.tile(j) : j);
+  };
+  // whether this wave's queries see anything of tile t, and whether they do not see all of it
+  auto sees = [&](int i, int t) {
+    return t < my_tiles && (!WIN || ((KS == 1 || i * KS + ks < walk.n) && (t * NB < a.sinks || t >= first_tile(q0, a.window))));
+  };
+  auto cut = [&](int t) {
+    return t == my_tiles - 1 || (WIN && q0 + NB - 1 - t * NB >= a.window && (t + 1) * NB > a.sinks);
+  };
+  auto hidden = [&](int j) { return j > qi || (WIN && qi - j >= a.window && j >= a.sinks); };
   auto stage_at = [&](int i) { return smem + ((i % S) * KS + ks) * STAGE; };
   const uint16_t* Kb = a.K + bk * int64_t(L) * D;
   const uint16_t* Vb = a.V + bk * int64_t(L) * D;
@@ -358,24 +408,24 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(KS
   float m = -INFINITY, l = 0.0f;
 #pragma unroll
   for (int t = 0; t < S - 1; ++t)
-    if (t < n_steps) copy_tile<PW>(Kb + tile_at(t) * NB * D, ro, stage_at(t), wave);
+    if (t < n_steps) copy_rows<WIN, PW>(Kb + tile_at(t) * NB * D, ro, stage_at(t), wave, lane, D, L - int(tile_at(t)) * NB);
   for (int i = 0; i < n_steps; ++i) {
     wait_tiles<PW>(min(S - 2, n_steps - 1 - i));
     lds_wait_barrier();
     if (i + S - 1 < n_steps) {
       const int u = i + S - 1;
-      copy_tile<PW>(Kb + tile_at(u) * NB * D, ro, stage_at(u), wave);
+      copy_rows<WIN, PW>(Kb + tile_at(u) * NB * D, ro, stage_at(u), wave, lane, D, L - int(tile_at(u)) * NB);
     }
-    const int t = i * KS + ks;
-    if (t >= my_tiles) continue;
+    const int t = WIN ? int(tile_at(i)) : i * KS + ks;
+    if (!sees(i, t)) continue;
     const u32x4a* tk = stage_at(i);
     f32x16a s = zero16();
 #pragma unroll
     for (int j = 0; j < 8; ++j) s = mfma(row_frag(tk, j, lane), qf[j], s);
-    if (t == my_tiles - 1) {
+    if (cut(t)) {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        if (t * NB + slot_row(r, lane) > qi) s[r] = -INFINITY;
+        if (hidden(t * NB + slot_row(r, lane))) s[r] = -INFINITY;
     }
     float mx = s[0];
 #pragma unroll
@@ -417,19 +467,19 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(KS
 #pragma unroll
   for (int t = 0; t < S - 1; ++t)
     if (t < n_steps) {
-      copy_tile<PW>(Kb + tile_at(t) * NB * D, ro, stage_at(t), wave);
-      copy_tile<PW>(Vb + tile_at(t) * NB * D, ro, stage_at(t) + TILE16, wave);
+      copy_rows<WIN, PW>(Kb + tile_at(t) * NB * D, ro, stage_at(t), wave, lane, D, L - int(tile_at(t)) * NB);
+      copy_rows<WIN, PW>(Vb + tile_at(t) * NB * D, ro, stage_at(t) + TILE16, wave, lane, D, L - int(tile_at(t)) * NB);
     }
   for (int i = 0; i < n_steps; ++i) {
     wait_tiles<2 * PW>(min(S - 2, n_steps - 1 - i));
     lds_wait_barrier();
     if (i + S - 1 < n_steps) {
       const int u = i + S - 1;
-      copy_tile<PW>(Kb + tile_at(u) * NB * D, ro, stage_at(u), wave);
-      copy_tile<PW>(Vb + tile_at(u) * NB * D, ro, stage_at(u) + TILE16, wave);
+      copy_rows<WIN, PW>(Kb + tile_at(u) * NB * D, ro, stage_at(u), wave, lane, D, L - int(tile_at(u)) * NB);
+      copy_rows<WIN, PW>(Vb + tile_at(u) * NB * D, ro, stage_at(u) + TILE16, wave, lane, D, L - int(tile_at(u)) * NB);
     }
-    const int t = i * KS + ks;
-    if (t >= my_tiles) continue;
+    const int t = WIN ? int(tile_at(i)) : i * KS + ks;
+    if (!sees(i, t)) continue;
     const u32x4a* tk = stage_at(i);
     const u32x4a* tv = tk + TILE16;
     f32x16a s = zero16();
@@ -438,10 +488,10 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(KS
     float p[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) p[r] = exp2a(fmaf(s[r], c, -lse));
-    if (t == my_tiles - 1) {
+    if (cut(t)) {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        if (t * NB + slot_row(r, lane) > qi) p[r] = 0.0f;
+        if (hidden(t * NB + slot_row(r, lane))) p[r] = 0.0f;
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -455,7 +505,7 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(KS
     add_groups<NW>(o, reinterpret_cast<float*>(smem), wave, ks, lane);
     if (ks != 0) return;
   }
-  if (!active) return;
+  if (!active || (WIN && qi >= L)) return;
   uint16_t* orow = a.O_out + (TOK ? tok_off(a, b, qi) : (b * L + qi) * int64_t(D));
 #pragma unroll
   for (int db = 0; db < 4; ++db)
@@ -478,7 +528,7 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(KS
 // Backward for the queries: delta = dO . O per row, then per key tile
 // S -> P (from lse), dP = dO V^T, dS = bf16(P (dP - delta)), dQ += dS K;
 // dQ * scale stored in fp32, delta stored for the key kernel.
-template <int NW, int S, bool TOK, int KS>
+template <int NW, int S, bool TOK, int KS, bool WIN = false>
 __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_bwd_dq_kernel(AttnArgs a) {
   constexpr int QB = NW * NB;
   constexpr int PW = 8 / NW;
@@ -496,11 +546,23 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(2,
   const bool active = q0 < L;
   const int qi = q0 + (lane & 31);
   const int qc = min(qi, L - 1);
-  const int n_tiles = min(L, qb * QB + QB) / NB;
+  const int n_tiles = (min(L, qb * QB + QB) + (WIN ? NB - 1 : 0)) / NB;
   const int my_tiles = active ? q0 / NB + 1 : 0;
+  const KeyWalk walk = WIN ? key_walk(qb * QB, n_tiles, a.window, a.sinks) : KeyWalk{0, 0, n_tiles};
   // step i of the walk, as in the forward
-  const int n_steps = (n_tiles + KS - 1) / KS;
-  auto tile_at = [&](int i) { return int64_t(KS == 1 ? i : min(i * KS + ks, n_tiles - 1)); };
+  const int n_steps = (walk.n + KS - 1) / KS;
+  auto tile_at = [&](int i) {
+    const int j = KS == 1 ? i : min(i * KS + ks, walk.n - 1);
+    return int64_t(WIN ? walk.tile(j) : j);
+  };
+  // whether this wave's queries see anything of tile t, and whether they do not see all of it
+  auto sees = [&](int i, int t) {
+    return t < my_tiles && (!WIN || ((KS == 1 || i * KS + ks < walk.n) && (t * NB < a.sinks || t >= first_tile(q0, a.window))));
+  };
+  auto cut = [&](int t) {
+    return t == my_tiles - 1 || (WIN && q0 + NB - 1 - t * NB >= a.window && (t + 1) * NB > a.sinks);
+  };
+  auto hidden = [&](int j) { return j > qi || (WIN && qi - j >= a.window && j >= a.sinks); };
   auto stage_at = [&](int i) { return smem + ((i % S) * KS + ks) * STAGE; };
   const uint16_t* Kb = a.K + bk * int64_t(L) * D;
   const uint16_t* Vb = a.V + bk * int64_t(L) * D;
@@ -531,19 +593,19 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
   for (int t = 0; t < S - 1; ++t)
     if (t < n_steps) {
-      copy_tile<PW>(Kb + tile_at(t) * NB * D, ro, stage_at(t), wave);
-      copy_tile<PW>(Vb + tile_at(t) * NB * D, ro, stage_at(t) + TILE16, wave);
+      copy_rows<WIN, PW>(Kb + tile_at(t) * NB * D, ro, stage_at(t), wave, lane, D, L - int(tile_at(t)) * NB);
+      copy_rows<WIN, PW>(Vb + tile_at(t) * NB * D, ro, stage_at(t) + TILE16, wave, lane, D, L - int(tile_at(t)) * NB);
     }
   for (int it = 0; it < n_steps; ++it) {
     wait_tiles<2 * PW>(min(S - 2, n_steps - 1 - it));
     lds_wait_barrier();
     if (it + S - 1 < n_steps) {
       const int u = it + S - 1;
-      copy_tile<PW>(Kb + tile_at(u) * NB * D, ro, stage_at(u), wave);
-      copy_tile<PW>(Vb + tile_at(u) * NB * D, ro, stage_at(u) + TILE16, wave);
+      copy_rows<WIN, PW>(Kb + tile_at(u) * NB * D, ro, stage_at(u), wave, lane, D, L - int(tile_at(u)) * NB);
+      copy_rows<WIN, PW>(Vb + tile_at(u) * NB * D, ro, stage_at(u) + TILE16, wave, lane, D, L - int(tile_at(u)) * NB);
     }
-    const int t = it * KS + ks;
-    if (t >= my_tiles) continue;
+    const int t = WIN ? int(tile_at(it)) : it * KS + ks;
+    if (!sees(it, t)) continue;
     const u32x4a* tk = stage_at(it);
     bf16x8a f[8];
 #pragma unroll
@@ -559,11 +621,14 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(2,
     for (int i = 0; i < 8; ++i) f[i] = col_frag(tk, i & 3, i >> 2, lane);
     // dS in place of dP
 #pragma unroll
-    for (int r = 0; r < 16; ++r) dp[r] = bf16_round(exp2a(fmaf(s[r], c, -lse))) * (dp[r] - dl);
-    if (t == my_tiles - 1) {
+    for (int r = 0; r < 16; ++r) {
+      const float p = exp2a(fmaf(s[r], c, -lse));
+      dp[r] = (WIN ? p : bf16_round(p)) * (dp[r] - dl);
+    }
+    if (cut(t)) {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        if (t * NB + slot_row(r, lane) > qi) dp[r] = 0.0f;
+        if (hidden(t * NB + slot_row(r, lane))) dp[r] = 0.0f;
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -579,7 +644,7 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(2,
     add_groups<NW>(dq, reinterpret_cast<float*>(smem), wave, ks, lane);
     if (ks != 0) return;
   }
-  if (!active) return;
+  if (!active || (WIN && qi >= L)) return;
   if (lane < 32) a.delta[b * L + qi] = dl;
   if constexpr (TOK) store_bf16_row<true>(a.dQ_tok + tok_off(a, b, qi), dq, a.scale, a.cs, qi, lane);
   else store_f32_rows(a.dQ + (b * L + qi) * int64_t(D), dq, a.scale, lane);
@@ -594,12 +659,12 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(2,
 // 1 KB slot of the stage (lanes 0-7 lse, 8-15 delta, the rest repeat them).
 // To hold two workgroups of 256 registers per lane on a SIMD, the last NPARK
 // of the wave's V fragments are kept in LDS and read back for each tile.
-template <int NW, int S, bool TOK, int KS>
+template <int NW, int S, bool TOK, int KS, bool WIN = false>
 __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void attn_bwd_dkv_kernel(AttnArgs a) {
   constexpr int KB = NW * NB;
   constexpr int PW = 8 / NW;
   constexpr int STAGE = 2 * TILE16 + 64;  // Q, dO tiles, row terms
-  constexpr int NPARK = 3;
+  constexpr int NPARK = WIN ? 5 : 3;
   __shared__ u32x4a smem[S * KS * STAGE + NW * KS * NPARK * 64];
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6));
@@ -608,21 +673,37 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(2,
   int kb;
   int64_t b;
   block_of((L + KB - 1) / KB, a.batch, kb, b);
+  if constexpr (WIN) kb = (L + KB - 1) / KB - 1 - kb;  // the sinks, which most queries see, first
   const int64_t bk = b % a.kv_batch;
   const int k0 = kb * KB + wave * NB;
   const bool active = k0 < L;
   const int kj = k0 + (lane & 31);  // this lane's key
   const int kc = min(kj, L - 1);
   const int first = kb * KB / NB;   // first query tile of the workgroup
-  const int n_tiles = L / NB;
+  // query tiles up to the last that sees one of the keys [k, k1)
+  auto last_tile = [&](int k, int k1) {
+    return !WIN ? L / NB : (k < a.sinks ? L + NB - 1 : min(L, min(k1, L) - 1 + a.window) + NB - 1) / NB;
+  };
+  const int n_tiles = last_tile(kb * KB, kb * KB + KB);
   const int my_first = active ? k0 / NB : n_tiles;
+  const int my_last = WIN && active ? last_tile(k0, k0 + NB) : n_tiles;
   const float c = a.scale * LOG2E;
   const uint16_t* Qb = a.Q + b * int64_t(L) * D;
   // dO tile t starts at dOb + t NB ldo (token-major rows: a stride of heads D)
   const int ldo = TOK ? a.heads * D : D;
   const uint16_t* dOb = a.dO + (TOK ? tok_off(a, b, 0) : b * int64_t(L) * D);
   // row terms: lane (l % 16) copies 4 floats of lse (l % 16 < 8) or delta
-  const float* rt_src = ((lane & 15) < 8 ? a.lse : a.delta) + b * L + 4 * (lane & 7);
+  // (WIN: lane l one float of lse (l < 32) or delta, of any alignment)
+  const float* rt_src = WIN ? (lane < 32 ? a.lse : a.delta) + b * L
+                            : ((lane & 15) < 8 ? a.lse : a.delta) + b * L + 4 * (lane & 7);
+  auto copy_terms = [&](int t, u32x4a* dst) {
+    if constexpr (WIN) {
+      const float* at = rt_src + min(t * NB + (lane & 31), L - 1);
+      __builtin_amdgcn_global_load_lds((glb_void_a*)at, (lds_void_a*)dst, 4, 0, 0);
+    } else {
+      copy16(rt_src + t * NB, 0, dst);
+    }
+  };
   uint32_t ro[PW], rod[PW];
 #pragma unroll
   for (int q = 0; q < PW; ++q) {
@@ -651,9 +732,9 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(2,
     if (i < nt) {
       const int t = tile_at(i);
       u32x4a* st = stage_at(i);
-      copy_tile<PW>(Qb + int64_t(t) * NB * D, ro, st, wave);
-      copy_tile<PW>(dOb + int64_t(t) * NB * ldo, rod, st + TILE16, wave);
-      if (wave == 0) copy16(rt_src + t * NB, 0, st + 2 * TILE16);
+      copy_rows<WIN, PW>(Qb + int64_t(t) * NB * D, ro, st, wave, lane, D, L - t * NB);
+      copy_rows<WIN, PW>(dOb + int64_t(t) * NB * ldo, rod, st + TILE16, wave, lane, ldo, L - t * NB);
+      if (wave == 0) copy_terms(t, st + 2 * TILE16);
     }
   for (int i = 0; i < nt; ++i) {
     if (wave == 0) wait_tiles<2 * PW + 1>(min(S - 2, nt - 1 - i));
@@ -662,12 +743,12 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(2,
     if (i + S - 1 < nt) {
       const int t = tile_at(i + S - 1);
       u32x4a* st = stage_at(i + S - 1);
-      copy_tile<PW>(Qb + int64_t(t) * NB * D, ro, st, wave);
-      copy_tile<PW>(dOb + int64_t(t) * NB * ldo, rod, st + TILE16, wave);
-      if (wave == 0) copy16(rt_src + t * NB, 0, st + 2 * TILE16);
+      copy_rows<WIN, PW>(Qb + int64_t(t) * NB * D, ro, st, wave, lane, D, L - t * NB);
+      copy_rows<WIN, PW>(dOb + int64_t(t) * NB * ldo, rod, st + TILE16, wave, lane, ldo, L - t * NB);
+      if (wave == 0) copy_terms(t, st + 2 * TILE16);
     }
     const int t = first + i * KS + ks;
-    if (t < my_first || (KS > 1 && t >= n_tiles)) continue;
+    if (t < my_first || (KS > 1 && t >= n_tiles) || (WIN && t >= my_last)) continue;
     const u32x4a* st = stage_at(i);
     const float* rt = reinterpret_cast<const float*>(st + 2 * TILE16);  // lse[32], delta[32]
     f32x16a s = zero16(), dp = zero16();
@@ -689,18 +770,21 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(2,
 #pragma unroll
       for (int i8 = 0; i8 < 8; ++i8) {
         const int r = 8 * h + i8;
-        const float pv = bf16_round(exp2a(fmaf(s[r], c, -ls[i8])));
+        const float e = exp2a(fmaf(s[r], c, -ls[i8]));
+        const float pv = bf16_round(e);
         s[r] = pv;
-        dp[r] = pv * (dp[r] - de[i8]);
+        dp[r] = (WIN ? e : pv) * (dp[r] - de[i8]);
       }
     }
-    if (t == my_first) {
+    if (t == my_first || (WIN && ((t * NB + NB - 1 - k0 >= a.window && k0 + NB > a.sinks) || t * NB + NB > L))) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (kj > t * NB + slot_row(r, lane)) {
+      for (int r = 0; r < 16; ++r) {
+        const int i = t * NB + slot_row(r, lane);
+        if (kj > i || (WIN && ((i - kj >= a.window && kj >= a.sinks) || i >= L))) {
           s[r] = 0.0f;
           dp[r] = 0.0f;
         }
+      }
     }
     // the transpose-read addresses are recomputed for each tile (an opaque
     // copy of the lane index keeps them from being held across the loop)
@@ -728,7 +812,7 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(2,
     add_groups<NW>(dv, reinterpret_cast<float*>(smem), wave, ks, lane);
     if (ks != 0) return;
   }
-  if (!active) return;
+  if (!active || (WIN && kj >= L)) return;
   if (TOK && a.kv_batch == a.batch) {
     const int64_t o = tok_off(a, b, kj);
     store_bf16_row<true>(a.dK_tok + o, dk, a.scale, a.cs, kj, lane);
@@ -783,12 +867,29 @@ void launch(Kern kern, int64_t blocks, int ks, const AttnArgs& a, hipStream_t st
 }
 }  // namespace
 
+// The kernel's instance for token-major operands, split walks and windows.
+#define UQ_ATTN_FORM(kernel)                                                                            \
+  [](bool tok, bool split, bool win) {                                                                  \
+    if (win)                                                                                            \
+      return split ? (tok ? kernel<NW, S, true, 2, true> : kernel<NW, S, false, 2, true>)               \
+                   : (tok ? kernel<NW, S, true, 1, true> : kernel<NW, S, false, 1, true>);              \
+    return split ? (tok ? kernel<NW, S, true, 2> : kernel<NW, S, false, 2>)                             \
+                 : (tok ? kernel<NW, S, true, 1> : kernel<NW, S, false, 1>);                            \
+  }
+
 static void set_tok(AttnArgs& a, const AttnLaunch& q) {
   a.n_seq = q.tok_seqs > 0 ? q.tok_seqs : 1;
   a.heads = int(q.batch / a.n_seq);
   a.grp = q.group > 0 ? q.group : 1;
   a.cs = q.cs;
   a.dQ_tok = q.dQ_tok; a.dK_tok = q.dK_tok; a.dV_tok = q.dV_tok;
+  a.window = std::min(q.window, q.L); a.sinks = std::min(q.sinks, q.L);
+}
+
+// Whether a call's walks are split, split_walk's rule for windows: all rows but the sinks' walk alike.
+static bool splits(const AttnLaunch& q, int nblk) {
+  if (q.window <= 0) return split_walk(nblk, q.batch, q.L);
+  return nblk * q.batch <= 256 && std::min(q.L, std::min(q.window, q.L) + NW * NB) >= 512;
 }
 
 hipError_t launch_attn_fwd(const AttnLaunch& q, hipStream_t st) {
@@ -797,10 +898,8 @@ hipError_t launch_attn_fwd(const AttnLaunch& q, hipStream_t st) {
   a.Q = q.Q; a.K = q.K; a.V = q.V; a.O_out = q.O_out; a.lse = q.lse;
   set_tok(a, q);
   const int nblk = (q.L + NW * NB - 1) / (NW * NB);
-  const int64_t blocks = nblk * q.batch;
-  const bool tok = q.tok_seqs > 0;
-  if (split_walk(nblk, q.batch, q.L)) launch(tok ? attn_fwd_kernel<NW, S, true, 2> : attn_fwd_kernel<NW, S, false, 2>, blocks, 2, a, st);
-  else launch(tok ? attn_fwd_kernel<NW, S, true, 1> : attn_fwd_kernel<NW, S, false, 1>, blocks, 1, a, st);
+  const bool split = splits(q, nblk);
+  launch(UQ_ATTN_FORM(attn_fwd_kernel)(q.tok_seqs > 0, split, q.window > 0), nblk * q.batch, split ? 2 : 1, a, st);
   return hipGetLastError();
 }
 
@@ -810,16 +909,15 @@ hipError_t launch_attn_bwd(const AttnLaunch& q, hipStream_t st) {
   a.Q = q.Q; a.K = q.K; a.V = q.V; a.O = q.O; a.dO = q.dO;
   a.lse = q.lse; a.delta = q.delta; a.dQ = q.dQ; a.dK = q.dK; a.dV = q.dV;
   set_tok(a, q);
-  const bool tok = q.tok_seqs > 0;
+  const bool tok = q.tok_seqs > 0, win = q.window > 0;
   const int nblk = (q.L + NW * NB - 1) / (NW * NB);
   const int64_t blocks = nblk * q.batch;
-  const bool split = split_walk(nblk, q.batch, q.L);
-  if (split) launch(tok ? attn_bwd_dq_kernel<NW, S, true, 2> : attn_bwd_dq_kernel<NW, S, false, 2>, blocks, 2, a, st);
-  else launch(tok ? attn_bwd_dq_kernel<NW, S, true, 1> : attn_bwd_dq_kernel<NW, S, false, 1>, blocks, 1, a, st);
+  const bool split = splits(q, nblk);
+  const int ks = split ? 2 : 1;
+  launch(UQ_ATTN_FORM(attn_bwd_dq_kernel)(tok, split, win), blocks, ks, a, st);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (split) launch(tok ? attn_bwd_dkv_kernel<NW, S, true, 2> : attn_bwd_dkv_kernel<NW, S, false, 2>, blocks, 2, a, st);
-  else launch(tok ? attn_bwd_dkv_kernel<NW, S, true, 1> : attn_bwd_dkv_kernel<NW, S, false, 1>, blocks, 1, a, st);
+  launch(UQ_ATTN_FORM(attn_bwd_dkv_kernel)(tok, split, win), blocks, ks, a, st);
   return hipGetLastError();
 }
 

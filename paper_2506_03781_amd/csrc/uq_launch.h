@@ -190,6 +190,7 @@ struct AttnLaunch {
   int tok_seqs, group;
   const float* cs;
   uint16_t* dQ_tok; uint16_t* dK_tok; uint16_t* dV_tok;
+  int window, sinks;  // window 0: none
 };
 hipError_t launch_attn_fwd(const AttnLaunch& p, hipStream_t st);
 hipError_t launch_attn_bwd(const AttnLaunch& p, hipStream_t st);

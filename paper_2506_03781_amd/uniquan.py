@@ -88,6 +88,9 @@ _SIGS = {
     "uniquan_attn_fwd": ([_i64, _i64, _i32, _i32, _vp, _vp, _vp, _f32, _vp, _vp, _i32, _i32, _vp], _i32),
     "uniquan_attn_bwd": ([_i64, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _f32, _vp, _vp, _vp, _vp, _i32, _i32,
                           _vp, _vp], _i32),
+    "uniquan_attn_window_fwd": ([_i64, _i64, _i32, _i32, _vp, _vp, _vp, _f32, _i32, _i32, _vp, _vp, _i32, _i32, _vp], _i32),
+    "uniquan_attn_window_bwd": ([_i64, _i64, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _f32, _i32, _i32, _vp, _vp, _vp,
+                                 _vp, _i32, _i32, _vp, _vp], _i32),
     "uniquan_kv_append": ([_i64, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _vp, _vp, _i64, _vp, _i64,
                            _i64, _i32, _i32, _i64, _i32, _vp, _vp, _vp, _vp, _vp, _vp], _i32),
     "uniquan_kv_append_axes": ([_i64, _i32, _i32, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _vp, _vp, _vp, _i32, _vp,
@@ -626,6 +629,31 @@ def uniquan_attn_bwd(batch, kv_batch, L, d, Q, K, V, O, dO, row_lse, scale, delt
                                   _p(delta, nr, _F, "delta"), _p(dQ, nq, tq, "dQ"), _p(dK, nq, tkv, "dK"),
                                   _p(dV, nq, tkv, "dV"), int(tok_seqs), int(group),
                                   _p(cs, L * d, _F, "cs") if tok_seqs else None, _stream(stream)))
+
+
+def uniquan_attn_window_fwd(batch, kv_batch, L, d, Q, K, V, scale, window, sinks, O, row_lse, tok_seqs=0, group=1,
+                            stream=None):
+    """uniquan_attn_fwd with a sliding window: query i sees the keys j <= i with i - j < window or j < sinks; any L."""
+    _one_device(Q, K, V, O, row_lse)
+    nq, nk = batch * L * d, kv_batch * L * d
+    _check(lib().uniquan_attn_window_fwd(batch, kv_batch, L, d, _p(Q, nq, _B, "Q"), _p(K, nk, _B, "K"), _p(V, nk, _B, "V"),
+                                         float(scale), int(window), int(sinks), _p(O, nq, _B, "O"),
+                                         _p(row_lse, batch * L, _F, "row_lse"), int(tok_seqs), int(group),
+                                         _stream(stream)))
+
+
+def uniquan_attn_window_bwd(batch, kv_batch, L, d, Q, K, V, O, dO, row_lse, scale, window, sinks, delta, dQ, dK, dV,
+                            tok_seqs=0, group=1, cs=None, stream=None):
+    """Backward of uniquan_attn_window_fwd; gradients laid out as uniquan_attn_bwd's."""
+    _one_device(Q, K, V, O, dO, row_lse, delta, dQ, dK, dV, cs)
+    nq, nk, nr = batch * L * d, kv_batch * L * d, batch * L
+    tq = _B if tok_seqs else _F
+    tkv = _B if tok_seqs and kv_batch == batch else _F
+    _check(lib().uniquan_attn_window_bwd(
+        batch, kv_batch, L, d, _p(Q, nq, _B, "Q"), _p(K, nk, _B, "K"), _p(V, nk, _B, "V"), _p(O, nq, _B, "O"),
+        _p(dO, nq, _B, "dO"), _p(row_lse, nr, _F, "row_lse"), float(scale), int(window), int(sinks),
+        _p(delta, nr, _F, "delta"), _p(dQ, nq, tq, "dQ"), _p(dK, nq, tkv, "dK"), _p(dV, nq, tkv, "dV"), int(tok_seqs),
+        int(group), _p(cs, L * d, _F, "cs") if tok_seqs else None, _stream(stream)))
 
 
 def _one_device(*tensors):
