@@ -647,7 +647,8 @@ uq_status uniquan_attn_bwd(int64_t batch, int64_t kv_batch, int L, int d,
  * sliding window and a few first positions always in sight: query i sees the keys
  * j <= i with i - j < window or j < sinks, and only the tiles that hold one of them
  * are walked.  Formulas, layouts and outputs as there, but that P enters dS before
- * it is rounded: dS = bf16(2^(c S - row_lse) (dP - delta)).  window >= 1, sinks >= 0
+ * it is rounded: dS = bf16(2^(c S - row_lse) (dP - delta)), and that delta is
+ * sum_j P_ij dP_ij (fp32; O is not read).  window >= 1, sinks >= 0
  * (window >= L: the causal attention); any L >= 1 (up to 2^22, batch ceil(L / 128) at
  * most 2^22); scale positive and finite.  Q, K, V, dO have to be finite: a key outside
  * a query's sight has weight 0, not no part.
@@ -760,9 +761,9 @@ uq_status uniquan_bcq_matmul(int T, int64_t R, int64_t C, int k, int g,
  * queries; its O rows are the output product's activations.  For a prompt,
  * uniquan_kv_read gives keys and values back in uniquan_attn_fwd's layout.  That
  * call takes heads of 128 channels, as many queries as keys and multiples of 32
- * positions: whole prompts, the last rows padding.  A cache of 64-channel heads,
- * and a part of a prompt behind positions that are cached already, have the
- * attention of one token at a time only.
+ * positions: whole prompts, the last rows padding.  For a cache of 64-channel
+ * heads, and for a part of a prompt behind positions that are cached already,
+ * uniquan_attn_extend attends to the cache itself.
  *
  * Cache.  Positions 0, 1, ... of a sequence lie in pages of page_len
  * positions: position p of sequence s is place p % page_len of page
@@ -908,6 +909,55 @@ uq_status uniquan_kv_read(int64_t n_seq, int H_kv, int d, int64_t L,
 size_t uniquan_attn_decode_ws(int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len);
 uq_status uniquan_attn_decode(int64_t n_seq, int H, int H_kv, int d,
                               const uint16_t* Q, int64_t ld_q, const int32_t* lens,
+                              const int32_t* pages, int64_t max_pages,
+                              int format, int group, int64_t n_pages, int page_len,
+                              const void* k_cache, const void* v_cache,
+                              const uint16_t* k_stat, const uint16_t* v_stat,
+                              float scale, uint16_t* O, int64_t ld_o, float* row_lse,
+                              float* ws, size_t ws_len, void* stream);
+
+/*
+ * uniquan_attn_extend -- attention of several query rows per sequence over its
+ * cached positions: a part of a prompt behind what is cached (its rows have been
+ * appended already), a tree of drafted tokens, with or without a sliding window
+ * whose first positions stay in sight; one row per sequence with a window is the
+ * single-token form of uniquan_attn_window_fwd's attention.
+ *
+ * Rows [row_start[s], row_start[s + 1]) belong to sequence s, m of them; row j
+ * has its place at base + j, base = lens[s] - m (lens counts them).  It sees, of
+ * the positions t in [0, lens[s]) that lie on a page (lens capped at max_pages
+ * page_len):
+ *   t < base       where t < sinks or t > P - window, P the row's position: pos
+ *                  where given, else base + j (window 0: all of them, sinks is
+ *                  not read);
+ *   t = base + i   without mask for i <= j, by the same window; with mask where
+ *                  bit i of the row's mask is set (whatever the window; its own
+ *                  bit is not set by itself).
+ * O and row_lse are as in uniquan_attn_decode: base-2 log-sum-exp, 0 and -infinity
+ * where a row sees nothing, what it does not see has no influence whatever it
+ * is, and the same limits on values, scales, offsets and queries hold.  Where a
+ * sequence's rows and the query heads of a key/value head come to more than 16 on
+ * average (ceil(T / n_seq) H / H_kv), a weight times the group's scale is rounded
+ * once to bf16 (2^-8 of it at most), else it is two bf16 terms.  Rows behind
+ * row_start[n_seq] are padding: their O and row_lse are left as they were.
+ * Results do not change from run to run.
+ *
+ * Q [T] rows of H d bf16, ld_q elements apart (a multiple of 8; 0: H d); O [T] rows
+ * of H d bf16, ld_o elements apart (a multiple of 4; 0: H d); row_lse [T x H] fp32 or
+ * NULL; row_start [n_seq + 1] ascending, within [0, T]; mask [T x words] 64-bit
+ * words, bit i % 64 of word i / 64, or NULL; words in [1, 64]; pos [T] int32 or NULL
+ * (with mask and a window it must be given); window, sinks >= 0.  The outputs must
+ * not overlap Q.  T >= 0, T H <= 2^26; n_seq H <= 2^24, n_seq (max_pages page_len +
+ * 256) <= 2^37.  ws [ws_len] fp32 workspace of at least uniquan_attn_extend_ws(...)
+ * floats (16-byte aligned; 0: may be NULL; 0 also for sizes that the call refuses),
+ * of any contents, free to be reused once the call is done; calls that overlap need
+ * one each.
+ */
+size_t uniquan_attn_extend_ws(int64_t T, int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len);
+uq_status uniquan_attn_extend(int64_t T, int64_t n_seq, int H, int H_kv, int d,
+                              const uint16_t* Q, int64_t ld_q, const int32_t* row_start,
+                              const int32_t* lens, const uint64_t* mask, int words,
+                              const int32_t* pos, int window, int sinks,
                               const int32_t* pages, int64_t max_pages,
                               int format, int group, int64_t n_pages, int page_len,
                               const void* k_cache, const void* v_cache,

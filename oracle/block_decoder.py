@@ -170,7 +170,12 @@ def decoder_step(Xhat, Y_ref, W, g1, g2, n_seq, H, store=_ident, n_kv=None, wind
     # sum_j P_ij dP_ij written as dO_i . O_i (the same value in exact
     # arithmetic, O = P V), evaluated from the stored O
     delta = np.sum(dOh * split_heads(f["O"], n_seq, H), axis=-1, keepdims=True)
-    dS = store(f["P"] * (dP - delta))
+    Pd = f["P"]
+    if window:
+        # a windowed block's dS takes P before it is stored, and the row term from P itself
+        Pd = causal_softmax(f["S"], window, sinks)
+        delta = np.sum(Pd * dP, axis=-1, keepdims=True)
+    dS = store(Pd * (dP - delta))
     dQh = dS @ f["Kx"] / np.sqrt(d)
 
     def group_sum(x):  # per query head -> per key/value head

@@ -207,3 +207,43 @@ class Cache:
                 absv[s, h] = p @ np.abs(V[g]).max(-1)
                 absx[s, h] = abs(scale) * np.abs(K[g]).max() * np.abs(q[s, h]).sum()
         return O, lse, absv, absx
+
+    def attend_rows(self, q, row_start, lens, scale, mask=None, pos=None, window=0, sinks=0):
+        """attend for several rows per sequence (uniquan_attn_extend): q [T, H, d] bf16 values, mask a list of T
+        Python integers.  Rows of no sequence are NaN.  Also the number of positions that each row sees."""
+        T, H, d = q.shape
+        O, lse = np.full((T, H, d), np.nan), np.full((T, H), np.nan)
+        absv, absx, count = np.zeros((T, H)), np.zeros((T, H)), np.zeros(T, int)
+        cap = self.table.shape[1] * self.P
+        for s in range(self.table.shape[0]):
+            first, m = int(row_start[s]), int(row_start[s + 1]) - int(row_start[s])
+            if m == 0:
+                continue
+            at = np.array([p for p in range(max(0, min(int(lens[s]), cap))) if self.page(s, p) >= 0], np.int64)
+            K, V = self.dense(s, max(0, int(lens[s])))
+            base = max(int(lens[s]), 0) - m
+            for j in range(m):
+                r = first + j
+                P = base + j if pos is None else int(pos[r])
+                near = (at > P - window) | (at < sinks) if window else np.ones(len(at), bool)
+                if mask is None:
+                    see = near & (at <= base + j)
+                else:
+                    see = np.array([bool(near[i]) if t < base else bool(mask[r] >> int(t - base) & 1)
+                                    for i, t in enumerate(at)], bool).reshape(-1)
+                count[r] = see.sum()
+                O[r], lse[r] = 0, -np.inf
+                if not see.any():
+                    continue
+                for h in range(H):
+                    g = h // (H // self.n_kv)
+                    k, v = K[g][see], V[g][see]
+                    x = scale * (k @ q[r, h].astype(F64))
+                    top = x.max()
+                    p = np.exp(x - top)
+                    lse[r, h] = (top + np.log(p.sum())) / np.log(2.0)
+                    p /= p.sum()
+                    O[r, h] = p @ v
+                    absv[r, h] = p @ np.abs(v).max(-1)
+                    absx[r, h] = abs(scale) * np.abs(k).max() * np.abs(q[r, h]).sum()
+        return O, lse, absv, absx, count

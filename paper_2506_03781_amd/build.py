@@ -21,7 +21,7 @@ OBJ = os.path.join(os.path.dirname(HERE), "_build")
 LIB = os.path.join(HERE, "libuniquan.so")
 SOURCES = ["abi.hip", "fq_fwd.hip", "fq_bwd.hip", "gemm.hip", "init_unified.hip", "bcq_deploy.hip", "block_mlp.hip",
            "block_attn.hip", "attn_fused.hip", "kv_cache.hip", "attn_decode.hip",
-           "sample.hip", "probe.hip"]
+           "attn_extend.hip", "sample.hip", "probe.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -11,8 +11,19 @@ One step of a block on T rows, one per sequence, is
 and a prompt is appended in the same way, its rows naming their sequences;
 ``read`` gives it back in the layout of ``uniquan_attn_fwd``.  That attention
 takes d = 128, as many queries as keys and multiples of 32 positions: a whole
-prompt (padded behind its end), not a part of one behind positions that are
-cached already, nor heads of 64 channels; those are attended one token at a time.
+prompt (padded behind its end).  For heads of 64 channels, and for a part of a
+prompt behind positions that are cached already, ``extend`` attends to the cache.
+
+A step that verifies a tree of drafted tokens, m rows of a sequence whose length
+counts them (the drafts' places are the last m, their positions base + depth):
+
+    cache.append(k, v, place, q=q, q_out=Qr, seq=seq, cs=table, rot=position, axis=zeros)
+    cache.extend(Qr, row_start, lens, O, mask=ancestors)
+    ...                                                 the rest of the model
+    uniquan_sample(logits, u, token)                    a token after every draft
+
+and the drafts of the path that agrees are appended again, from the products'
+rows that the caller has kept, at places that are their positions.
 
 The rotary table cs [n, d / 2, 2] holds (cos, sin) of every position.
 ``uniquan_rope_table`` makes its angles in fp32, off by up to p 2^-23 at position
@@ -75,11 +86,17 @@ class KVCache:
         uq.uniquan_kv_read(self.table.shape[0], self.n_kv, self.d, L, lens, self.table, self.k, self.v, K, V,
                            start=start, stream=stream, **self._form())
 
-    def workspace(self, H):
-        """An fp32 workspace for attend with H query heads (None: none needed).  Calls that may overlap, and
-        graphs that are replayed at the same time, need one each."""
-        need = uq.uniquan_attn_decode_ws(self.table.shape[0], H, self.n_kv, self.d, self.table.shape[1], self.page_len)
+    def workspace(self, H, rows=None):
+        """An fp32 workspace for attend with H query heads, or for extend with `rows` rows (None: none needed).
+        Calls that may overlap, and graphs that are replayed at the same time, need one each."""
+        n, size = self.table.shape[0], (H, self.n_kv, self.d, self.table.shape[1], self.page_len)
+        need = uq.uniquan_attn_decode_ws(n, *size) if rows is None else uq.uniquan_attn_extend_ws(rows, n, *size)
         return torch.empty(need, dtype=torch.float32, device=self.k.device) if need else None
+
+    def _own_ws(self, ws, stream, name):
+        if ws is not None and (stream is not None or uq._recorder is not None):
+            raise ValueError(f"{name} needs the caller's ws on a given stream and within record()")
+        return ws
 
     def attend(self, Q, lens, O, row_lse=None, scale=None, ws=None, stream=None):
         """O [n_seq, H d] = attention of the rows Q [n_seq, H d] over each sequence's first lens[s] positions.
@@ -87,9 +104,19 @@ class KVCache:
         stream or within uniquan.record, whose launches outlive it, brings its own."""
         n, H = self.table.shape[0], Q.shape[1] // self.d
         if ws is None:
-            ws = self.workspace(H)
-            if ws is not None and (stream is not None or uq._recorder is not None):
-                raise ValueError("attend needs the caller's ws on a given stream and within record()")
+            ws = self._own_ws(self.workspace(H), stream, "attend")
         uq.uniquan_attn_decode(n, H, self.n_kv, self.d, Q, lens, self.table, self.k, self.v,
                                1.0 / float(self.d) ** 0.5 if scale is None else scale, O, row_lse, ws, stream=stream,
                                **self._form())
+
+    def extend(self, Q, row_start, lens, O, row_lse=None, mask=None, pos=None, window=0, sinks=0, scale=None, ws=None,
+               stream=None):
+        """O [T, H d] = attention of the rows Q [T, H d], row_start[s] .. row_start[s + 1] of them of sequence s, at
+        the last of its lens[s] places: parts of prompts, and with mask [T, words] trees of drafts; window and sinks
+        as in uniquan_attn_extend.  ws (from workspace(H, rows=T)) as for attend."""
+        n, T, H = self.table.shape[0], Q.shape[0], Q.shape[1] // self.d
+        if ws is None:
+            ws = self._own_ws(self.workspace(H, T), stream, "extend")
+        uq.uniquan_attn_extend(T, n, H, self.n_kv, self.d, Q, row_start, lens, self.table, self.k, self.v,
+                               1.0 / float(self.d) ** 0.5 if scale is None else scale, O, row_lse, ws, mask=mask, pos=pos,
+                               window=window, sinks=sinks, stream=stream, **self._form())

@@ -968,6 +968,56 @@ uq_status uniquan_attn_decode(int64_t n_seq, int H, int H_kv, int d, const uint1
   return hip_status(fn, uq::launch_attn_decode(p, static_cast<hipStream_t>(stream)));
 }
 
+// Sizes of an attn_extend that check_cache lets through.
+static uq_status check_extend(const char* fn, int64_t T, int H) {
+  if (T < 0 || T >= int64_t(1) << 31) return fail(UQ_EINVAL, "%s: T=%lld must be in [0, 2^31)", fn, (long long)T);
+  if (T > (int64_t(1) << 26) / H) return fail(UQ_EUNSUPPORTED, "%s: T H > 2^26", fn);
+  return UQ_OK;
+}
+
+size_t uniquan_attn_extend_ws(int64_t T, int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len) {
+  const char* fn = "uniquan_attn_extend_ws";
+  if (check_cache_sizes(fn, H_kv, d, n_seq, max_pages, page_len) || check_heads(fn, H, H_kv) || check_extend(fn, T, H) ||
+      check_decode(fn, n_seq, H, max_pages, page_len) || T == 0)
+    return 0;
+  return uq::attn_extend_ws(T, n_seq, H, H_kv, d, max_pages, page_len);
+}
+
+uq_status uniquan_attn_extend(int64_t T, int64_t n_seq, int H, int H_kv, int d, const uint16_t* Q, int64_t ld_q,
+                              const int32_t* row_start, const int32_t* lens, const uint64_t* mask, int words,
+                              const int32_t* pos, int window, int sinks, const int32_t* pages, int64_t max_pages,
+                              int format, int group, int64_t n_pages, int page_len, const void* k_cache,
+                              const void* v_cache, const uint16_t* k_stat, const uint16_t* v_stat, float scale,
+                              uint16_t* O, int64_t ld_o, float* row_lse, float* ws, size_t ws_len, void* stream) {
+  const char* fn = "uniquan_attn_extend";
+  uq::AttnExtendLaunch p{};
+  if (uq_status st = check_cache(fn, &p.c, H_kv, d, pages, n_seq, max_pages, format, group, n_pages, page_len, k_cache,
+                                 v_cache, k_stat, v_stat))
+    return st;
+  if (uq_status st = check_heads(fn, H, H_kv)) return st;
+  if (uq_status st = check_extend(fn, T, H)) return st;
+  if (uq_status st = check_decode(fn, n_seq, H, max_pages, page_len)) return st;
+  if (uq_status st = check_ld(fn, "ld_q", &ld_q, int64_t(H) * d, 8)) return st;
+  if (uq_status st = check_ld(fn, "ld_o", &ld_o, int64_t(H) * d, 4)) return st;
+  if (window < 0) return fail(UQ_EINVAL, "%s: window=%d must be >= 0", fn, window);
+  if (sinks < 0) return fail(UQ_EINVAL, "%s: sinks=%d must be >= 0", fn, sinks);
+  if (mask != nullptr && (words < 1 || words > 64)) return fail(UQ_EINVAL, "%s: words=%d must be in [1, 64]", fn, words);
+  if (mask != nullptr && window > 0 && pos == nullptr)
+    return fail(UQ_EINVAL, "%s: a window over a tree needs the rows' positions", fn);
+  OPT_PTR(mask, 8); OPT_PTR(pos, 4);
+  if (T == 0) return UQ_OK;
+  REQ_PTR(Q, 16); REQ_PTR(row_start, 4); REQ_PTR(lens, 4); REQ_PTR(O, 8); OPT_PTR(row_lse, 4);
+  const size_t need = uq::attn_extend_ws(T, n_seq, H, H_kv, d, max_pages, page_len);
+  if (ws_len < need) return fail(UQ_EINVAL, "%s: ws_len=%zu < %zu", fn, ws_len, need);
+  if (need > 0) REQ_PTR(ws, 16);
+  p.T = T; p.H = H; p.Q = Q; p.ld_q = ld_q;
+  p.row_start = row_start; p.lens = lens;
+  p.mask = mask; p.words = words; p.pos = pos;
+  p.window = window; p.sinks = sinks;
+  p.scale = scale; p.O = O; p.ld_o = ld_o; p.lse = row_lse; p.ws = ws;
+  return hip_status(fn, uq::launch_attn_extend(p, static_cast<hipStream_t>(stream)));
+}
+
 static uq_status check_sample(const char* fn, int64_t T, int64_t V) {
   if (T < 0 || T >= int64_t(1) << 31) return fail(UQ_EINVAL, "%s: T=%lld must be in [0, 2^31)", fn, (long long)T);
   if (V < 1) return fail(UQ_EINVAL, "%s: V=%lld must be >= 1", fn, (long long)V);

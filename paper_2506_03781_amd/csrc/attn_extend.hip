@@ -1,0 +1,767 @@
+// Attention of several query rows per sequence over the paged key/value cache
+// (uniquan_attn_extend): parts of prompts, trees of drafts, windows; formulas and
+// errors in uniquan.h.
+//
+// Split.  The rows of a sequence and the query heads of a key/value head are the
+// columns of one product, m (H / H_kv) of them in the order row, head.  A
+// workgroup of four wavefronts takes 16 NT columns (a tile) and a share of the
+// positions that its rows see, its wavefronts every fourth step of 32 positions.
+// Where the tiles are fewer than the workgroups that the GPU holds, the sequences'
+// positions are cut into shares of equal length and attn_extend_join_kernel joins
+// them; workgroups find their place by adding up all sequences' tiles and steps.
+//
+// One step is that of the single-token attention (attn_decode.hip): S^T = K Q^T and
+// O^T += V^T P^T with the heads as columns, K and V straight from the cache into
+// registers, codes fed as they are.  Each key and value operand meets NT column
+// tiles, which shares out its load and its preparation.
+//
+// What is seen.  A step in which some column does not see all 32 positions (its
+// own end, a window's edge, a tree's drafts, the end of the sequence or a missing
+// page) is masked entry by entry: scores to -infinity, weights to 0, and nothing
+// of a value or a scale that is not finite where the weight is 0 (its products
+// are 0, not NaN).  All other steps, nearly all of a long history, have no masks.
+//
+// Precision.  As in attn_decode.hip, but that with more than one column tile a
+// weight enters the second product as one bf16 value, rounded to nearest (2^-9 of it
+// at most, either way), as in the block's causal attention: a second term would
+// double that product, which bounds such calls.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "uq_attend.h"
+#include "uq_device.h"
+#include "uq_kv.h"
+#include "uq_launch.h"
+
+namespace uq {
+
+namespace {
+
+constexpr int MIN_STEPS = 8;  // of a share
+
+// ---------------------------------------------------------------------------
+// which tile and share a workgroup takes
+// ---------------------------------------------------------------------------
+struct Seq {
+  int first, m;  // rows
+  int len;
+};
+__device__ __forceinline__ Seq seq_of(const AttnExtendLaunch& p, int first, int end, int len) {
+  const int64_t m = int64_t(end) - first;
+  return Seq{first, first < 0 || m < 0 ? 0 : int(m < p.T ? m : p.T), len};
+}
+__device__ __forceinline__ int capped(const AttnExtendLaunch& p, int len) {
+  const int64_t cap = p.c.max_pages << p.c.log_page;
+  return len < 0 ? 0 : int(len < cap ? len : cap);
+}
+
+template <int COLS>
+struct Work {
+  const AttnExtendLaunch& p;
+  int G;  // query heads of a key/value head
+  __device__ __forceinline__ int tiles(const Seq& s) const { return int((int64_t(s.m) * G + COLS - 1) / COLS); }
+  // steps that a tile's rows see, about
+  __device__ __forceinline__ int steps(const Seq& s) const {
+    const int all = (capped(p, s.len) + STEP - 1) / STEP;
+    if (p.window <= 0) return all;
+    const int64_t near = (int64_t(p.sinks) + p.window + s.m) / STEP + 3;
+    return near < all ? int(near) : all;
+  }
+};
+
+struct Unit {
+  int s;          // sequence
+  int at;         // of the sequence's units
+  int slot;       // of the workspace, where the sequence is cut
+  int per;        // steps of a share
+};
+
+// Unit x: a share of a tile, or with TILES a tile; false: there are fewer.
+// target: shares that are wanted (0: no tile is cut).
+template <int COLS, bool TILES>
+__device__ __forceinline__ bool find(const AttnExtendLaunch& p, int G, int64_t x, int target, Unit& u) {
+  const Work<COLS> w{p, G};
+  const int lane = threadIdx.x & 63;
+  const int n = int(p.c.n_seq), run = (n + 63) / 64;
+  auto seq = [&](int j) { return seq_of(p, p.row_start[j], p.row_start[j + 1], p.lens[j]); };
+  u.per = 0x40000000;
+  if (target > 0) {
+    float mine = 0.0f;  // (an estimate: every wavefront adds up the same numbers in the same order)
+    for (int j = lane * run; j < lane * run + run && j < n; ++j) {
+      const Seq s = seq(j);
+      mine += float(w.tiles(s)) * float(w.steps(s));
+    }
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) mine += __shfl_xor(mine, d);
+    const int per = int(fminf(mine / float(target), 1e9f)) + WAVES;
+    u.per = std::max(MIN_STEPS, per & ~(WAVES - 1));
+  }
+  auto count = [&](int j, int& un, int& sp) {
+    un = sp = 0;
+    if (j >= n) return;
+    const Seq s = seq(j);
+    const int tiles = w.tiles(s), parts = std::max(1, (w.steps(s) + u.per - 1) / u.per);
+    un = TILES ? tiles : tiles * parts;
+    sp = parts > 1 ? tiles * parts : 0;
+  };
+  int un = 0, sp = 0;
+  for (int j = lane * run; j < lane * run + run; ++j) {
+    int a, b;
+    count(j, a, b);
+    un += a;
+    sp += b;
+  }
+  int upto = wave_scan(un), supto = wave_scan(sp);
+  if (x >= __builtin_amdgcn_readlane(upto, 63)) return false;
+  int in = __builtin_ctzll(__ballot(upto > int(x)));
+  u.s = in * run;
+  int before = __builtin_amdgcn_readlane(upto - un, in);
+  u.slot = __builtin_amdgcn_readlane(supto - sp, in);
+  if (run > 1) {
+    for (const int end = u.s + run; u.s < end; u.s += 64) {
+      const int j = u.s + lane < end ? u.s + lane : n;
+      count(j, un, sp);
+      upto = wave_scan(un) + before;
+      supto = wave_scan(sp) + u.slot;
+      const uint64_t past = __ballot(upto > int(x));
+      if (past) {
+        in = __builtin_ctzll(past);
+        u.s += in;
+        before = __builtin_amdgcn_readlane(upto - un, in);
+        u.slot = __builtin_amdgcn_readlane(supto - sp, in);
+        break;
+      }
+      before = __builtin_amdgcn_readlane(upto, 63);
+      u.slot = __builtin_amdgcn_readlane(supto, 63);
+    }
+  }
+  u.at = int(x) - before;
+  return true;
+}
+
+// A share's sums for one column: (maximum, sum, -, -, D values) against that maximum.
+template <int COLS, int D>
+__device__ __forceinline__ float* part_of(const AttnExtendLaunch& p, int64_t slot, int g, int col) {
+  return p.ws + ((slot * p.c.H_kv + g) * COLS + col) * (D + 4);
+}
+
+// Bits [at, at + 32) of a row's mask; at > -32, bits outside it 0.
+__device__ __forceinline__ uint32_t mask_bits(const uint64_t* row, int words, int at) {
+  const int w = at >> 6, sh = at & 63;
+  const uint64_t lo = w >= 0 && w < words ? row[w] : 0u, hi = w + 1 >= 0 && w + 1 < words ? row[w + 1] : 0u;
+  return uint32_t(sh ? lo >> sh | hi << (64 - sh) : lo);
+}
+
+__device__ __forceinline__ int wave_min(int x) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) x = std::min(x, __shfl_xor(x, d));
+  return x;
+}
+__device__ __forceinline__ int wave_max(int x) {
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) x = std::max(x, __shfl_xor(x, d));
+  return x;
+}
+
+// Whether one of a word's two bf16 values is not finite.
+__device__ __forceinline__ bool wild(uint32_t w) {
+  return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
+}
+
+// Workgroups a CU holds (their registers are bounded to that): the most for which nothing is spilled in the loop.
+template <int FMT, int D, int NG, int NT>
+constexpr int kHeld = NT == 2 && NG == 4 ? 1 : 2;
+
+template <int FMT, int D, int NG, int NT>
+__global__ __launch_bounds__(256, (kHeld<FMT, D, NG, NT>)) void attn_extend_kernel(AttnExtendLaunch p, int target) {
+  using F = Form<FMT, D>;
+  constexpr int COLS = 16 * NT;
+  constexpr bool CODES = FMT != KV_BF16, TWO = NT == 1;  // two terms a weight
+  constexpr float MID = FMT == KV_U8 ? 128.0f : 8.0f;
+  constexpr float VSCALE = 0x1p64f;  // on the scales
+  constexpr float VBACK = 0x1p69f;   // 2^133 / VSCALE
+  auto sixteenfold = [](int k) { return FMT == KV_U4 && k % 2 == 1; };  // 4-bit codes of the odd channel tiles
+  constexpr int LD = D + 4;
+  __shared__ __attribute__((aligned(16))) float so[WAVES][16][LD];
+  __shared__ float sm[WAVES][16], ss[WAVES][16];
+  const KvCache& c = p.c;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int col = lane & 15, grp = lane >> 4;
+  const int G = p.H / c.H_kv;
+  const int64_t b = workgroup();
+  const int g = int(b % c.H_kv);  // one key/value head's workgroups on one XCD, or on as few as can be
+  Unit unit;
+  if (!find<COLS, false>(p, G, b / c.H_kv, target, unit)) return;
+  const int s = unit.s;
+  const Seq seq = seq_of(p, scalar(p.row_start, s), scalar(p.row_start, s + 1), scalar(p.lens, s));
+  const Work<COLS> work{p, G};
+  const int tiles = work.tiles(seq), parts = std::max(1, (work.steps(seq) + unit.per - 1) / unit.per);
+  const int part = unit.at / tiles, tile = tiles - 1 - unit.at % tiles;  // the longest first
+  const int len = capped(p, seq.len);
+  const int base = seq.len < 0 ? -seq.m : std::max(seq.len - seq.m, -seq.m);
+  const bool tree = p.mask != nullptr;
+
+  // the lane's columns: rows of Q and what they see
+  int64_t row[NT];      // -1: none
+  int head[NT];
+  int end[NT], low[NT];  // seen: below end, at low or behind (or below sinks)
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int64_t i = int64_t(tile) * COLS + 16 * n + col;
+    const int j = int(i / G);
+    row[n] = j < seq.m && int64_t(seq.first) + j < p.T ? int64_t(seq.first) + j : -1;
+    head[n] = g * G + int(i % G);
+    end[n] = tree ? base : base + j + 1;
+    const int64_t at = row[n] >= 0 && p.pos ? p.pos[row[n]] : int64_t(base) + j;
+    low[n] = p.window > 0 ? int(std::min<int64_t>(std::max<int64_t>(at - p.window + 1, 0), 0x7FFFFFFF)) : 0;
+  }
+  int end_min = 0x7FFFFFFF, end_max = 0, low_min = 0x7FFFFFFF, low_max = 0;
+#pragma unroll
+  for (int n = 0; n < NT; ++n)
+    if (row[n] >= 0) {
+      end_min = std::min(end_min, end[n]);
+      end_max = std::max(end_max, end[n]);
+      low_min = std::min(low_min, low[n]);
+      low_max = std::max(low_max, low[n]);
+    }
+  end_min = uniform(wave_min(end_min));
+  end_max = uniform(wave_max(end_max));
+  low_min = uniform(wave_min(low_min));
+  low_max = uniform(wave_max(low_max));
+
+  // the steps of the tile: those with sinks, then from the window's begin to the last end
+  const int hi = tree ? len : std::min(len, end_max);
+  const int lo = std::max(0, tree ? std::min(low_min, base) : low_min);
+  const int n_sink = p.window > 0 ? (std::min(p.sinks, std::max(hi, 0)) + STEP - 1) / STEP : 0;
+  const int u_lo = std::max(lo / STEP, n_sink);
+  const int n_steps = n_sink + std::max(0, (std::max(hi, 0) + STEP - 1) / STEP - u_lo);
+  const int i0 = int(int64_t(n_steps) * part / parts), i1 = int(int64_t(n_steps) * (part + 1) / parts);
+  auto step_at = [&](int i) { return i < n_sink ? i : u_lo + (i - n_sink); };
+
+  const uint32_t page_bytes = uint32_t(c.H_kv) * uint32_t(c.page_len) * F::ROW;
+  const uint32_t page_stats = uint32_t(c.H_kv) * uint32_t(c.page_len) * NG;
+  const uint32_t head_bytes = uint32_t(g) * uint32_t(c.page_len) * F::ROW;
+  const uint32_t lane_stat = (uint32_t(g) * NG + uint32_t(grp % NG)) * uint32_t(c.page_len) + col;
+  uint32_t pick[NG], mids[NG];
+#pragma unroll
+  for (int e = 0; e < NG; ++e) {
+    pick[e] = grp == e ? pair(VSCALE, 0.0f) : 0u;
+    mids[e] = grp == e ? pair(MID, 1.0f) : 0u;
+  }
+
+  // The loads run a step ahead of the products, as in the single-token attention.
+  struct Ahead {
+    int i, u, page[2];
+    uint64_t place[2], stat[2];
+    int nv[2];  // positions of each tile that exist
+  } next;
+  uint32_t kw[2][F::KW], vw[8][F::VW], kst[2], vst[2];
+  const int32_t* pages = c.pages + int64_t(s) * c.max_pages;
+  auto look_up = [&] {
+    next.u = step_at(next.i);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int at = next.u * STEP + 16 * t;
+      next.page[t] = next.i < i1 && at < len ? scalar(pages, at >> c.log_page) : -1;
+    }
+  };
+  auto load_keys = [&] {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int at = next.u * STEP + 16 * t;
+      const bool is = next.page[t] >= 0 && next.page[t] < c.n_pages;
+      const uint32_t pg = is ? uint32_t(next.page[t]) : 0u;
+      const uint32_t r = is ? uint32_t(at & (c.page_len - 1)) : 0u;
+      next.nv[t] = is ? std::min(16, len - at) : 0;
+      next.place[t] = uint64_t(pg) * page_bytes + (head_bytes + r * F::ROW);
+      next.stat[t] = uint64_t(pg) * page_stats + r;
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      load_key<FMT, D>(static_cast<const char*>(c.k) + next.place[t], lane, kw[t]);
+      if constexpr (CODES) kst[t] = (reinterpret_cast<const uint32_t*>(c.k_stat) + next.stat[t])[lane_stat];
+    }
+  };
+  auto load_values = [&] {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+      if constexpr (CODES) vst[t] = (reinterpret_cast<const uint32_t*>(c.v_stat) + next.stat[t])[lane_stat];
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      load_value<FMT, D>(static_cast<const char*>(c.v) + next.place[j / 4], 4 * grp + j % 4, lane, vw[j]);
+    next.i += WAVES;
+    look_up();
+  };
+
+  // queries, a negative scale's sign on them; for codes scaled, and their sums over each group of channels
+  u32x4d q[NT][F::NC];
+  u32x4d qs[NT] = {};
+  float cl[NT];  // scores to exponents of 2
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const uint16_t* at = p.Q + (row[n] < 0 ? 0 : row[n]) * p.ld_q + int64_t(head[n]) * D + 8 * grp;
+#pragma unroll
+    for (int k = 0; k < F::NC; ++k)
+      q[n][k] = row[n] >= 0 ? *reinterpret_cast<const u32x4d*>(at + 32 * k) : u32x4d{0, 0, 0, 0};
+  }
+  next.i = i0 + wave;
+  look_up();
+  load_keys();
+  int nv[2] = {next.nv[0], next.nv[1]};
+  load_values();
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    cl[n] = fabsf(p.scale) * LOG2E_D;
+    if (p.scale < 0.0f) {
+#pragma unroll
+      for (int k = 0; k < F::NC; ++k) q[n][k] ^= 0x80008000u;
+    }
+    if constexpr (CODES) {
+      uint32_t top = 0;
+#pragma unroll
+      for (int k = 0; k < F::NC; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) top = std::max(top, std::max(q[n][k][i] << 16 & 0x7FFF0000u, q[n][k][i] & 0x7FFF0000u));
+      const int ex = int(__float_as_uint(max4(__uint_as_float(top))) >> 23) - 127;
+      const float up = ldexpf(1.0f, 120 - std::max(ex, -7));
+      cl[n] = cl[n] * ldexpf(1.0f, 13 - 64 + std::max(ex, -7));  // 2^133 over the queries' power and the scales'
+#pragma unroll
+      for (int k = 0; k < F::NC; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          q[n][k][i] = pair(__uint_as_float(q[n][k][i] << 16) * up, __uint_as_float(q[n][k][i] & 0xFFFF0000u) * up);
+      float mine = 0.0f;
+#pragma unroll
+      for (int e = 0; e < NG; ++e) {
+        float t = 0.0f;
+#pragma unroll
+        for (int k = e * F::NC / NG; k < (e + 1) * F::NC / NG; ++k)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            t += __uint_as_float(q[n][k][i] << 16) * 0x1p-69f + __uint_as_float(q[n][k][i] & 0xFFFF0000u) * 0x1p-69f;
+        t = sum4(t);
+        if (grp == e) mine = t;
+      }
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const float h = __uint_as_float(__float_as_uint(mine) & 0xFFFF0000u);
+        qs[n][i] = pair(0.0f, h);
+        mine -= h;
+      }
+      if constexpr (FMT == KV_U4) {
+#pragma unroll
+        for (int k = 0; k < F::NC; ++k)
+#pragma unroll
+          for (int i = 1; i < 4; i += 2)
+            q[n][k][i] = pair(__uint_as_float(q[n][k][i] << 16) * 0x1p-4f, __uint_as_float(q[n][k][i] & 0xFFFF0000u) * 0x1p-4f);
+      }
+    }
+  }
+
+  f32x4d acc[NT][F::NV] = {};
+  f32x4d mid[NT][NG] = {};  // sums of the products' weights times minus the codes' middle
+  float off[NT][NG] = {};   // sums of weight times the value of the codes' middle
+  float m[NT], l[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    m[n] = LOWEST;
+    l[n] = 0.0f;
+  }
+
+  for (int i = i0 + wave; i < i1; i += WAVES) {
+    const int t0 = step_at(i) * STEP;
+    // scores of positions 4 grp + i of tile t
+    float x[NT][8];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      f32x4d sum[NT] = {};
+      if constexpr (CODES) {
+        const u32x4d st4 = {kst[t], kst[t], kst[t], kst[t]};
+        const u32x2d st = {kst[t], kst[t]};
+#pragma unroll
+        for (int n = 0; n < NT; ++n) sum[n] = mfma16(st4, qs[n], sum[n]);  // the three terms at once
+#pragma unroll
+        for (int e = 0; e < NG; ++e) {
+          f32x4d a[NT] = {};
+#pragma unroll
+          for (int k = e * F::NC / NG; k < (e + 1) * F::NC / NG; ++k) {
+            const u32x4d ks = key_step<FMT, D>(kw[t], k);
+#pragma unroll
+            for (int n = 0; n < NT; ++n) a[n] = mfma16(ks, q[n][k], a[n]);
+          }
+          const f32x4d sc = mfma16(st, u32x2d{pick[e], 0u}, f32x4d{});
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum[n][r] = __builtin_fmaf(sc[r], a[n][r], sum[n][r]);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < F::NC; ++k) {
+          const u32x4d ks = key_step<FMT, D>(kw[t], k);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) sum[n] = mfma16(ks, q[n][k], sum[n]);
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[n][4 * t + r] = sum[n][r];
+    }
+    load_keys();
+    const bool cut = nv[0] + nv[1] < STEP || t0 + STEP > end_min || (t0 < low_max && t0 + STEP > p.sinks);
+    uint32_t seen[NT];  // bit j: position 4 grp + j % 4 of tile j / 4
+    if (cut) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        uint32_t drafts = 0;
+        if (tree && t0 + STEP > base && row[n] >= 0)
+          drafts = mask_bits(p.mask + row[n] * p.words, p.words, t0 - base);
+        seen[n] = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const int in = 16 * (j / 4) + 4 * grp + j % 4, at = t0 + in;
+          const bool ok = at < end[n] ? (at >= low[n] || (p.window > 0 && at < p.sinks)) : (at >= base && (drafts >> in & 1));
+          seen[n] |= ok && in - 16 * (j / 4) < nv[j / 4] ? 1u << j : 0u;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[n][j] = seen[n] >> j & 1 ? x[n][j] : -__builtin_inff();
+      }
+      // nothing of what does not exist
+      if constexpr (!CODES) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int w = 0; w < F::VW; ++w) vw[j][w] = 4 * grp + j % 4 < nv[j / 4] ? vw[j][w] : 0u;
+      }
+    }
+    float w[NT][8];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      // running maximum: the reference moves only when a score exceeds it by SLACK
+      float mx = x[n][0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) mx = fmaxf(mx, x[n][j]);
+      mx = max4(mx) * cl[n];
+      if (__any(mx > m[n] + SLACK)) {
+        const float m1 = fmaxf(m[n], mx);
+        const float f = __builtin_amdgcn_exp2f(m[n] - m1);
+        m[n] = m1;
+        l[n] *= f;
+#pragma unroll
+        for (int k = 0; k < F::NV; ++k) acc[n][k] *= f;
+        if constexpr (CODES) {
+#pragma unroll
+          for (int e = 0; e < NG; ++e) {
+            mid[n][e] *= f;
+            off[n][e] *= f;
+          }
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) w[n][j] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[n][j], cl[n], -m[n]));
+      if (cut) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[n][j] = seen[n] >> j & 1 ? w[n][j] : 0.0f;
+      }
+      l[n] += ((w[n][0] + w[n][1]) + (w[n][2] + w[n][3])) + ((w[n][4] + w[n][5]) + (w[n][6] + w[n][7]));
+    }
+    // the weights as operands: two bf16 terms, or one rounded to nearest
+    auto operands = [&](const float (&z)[8], u32x4d& h, u32x4d& lo) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if constexpr (TWO) {
+          auto less = [](float v) { return __builtin_fmaf(v, MORE, -__uint_as_float(__float_as_uint(v) & 0xFFFF0000u)); };
+          h[r] = pair(z[2 * r], z[2 * r + 1]);
+          lo[r] = pair(less(z[2 * r]), less(z[2 * r + 1]));
+        } else {
+          h[r] = pack_bf16x2(z[2 * r], z[2 * r + 1]);
+        }
+      }
+    };
+#pragma unroll
+    for (int e = 0; e < NG; ++e) {
+      u32x4d h[NT], lo2[NT];
+      if constexpr (CODES) {
+        f32x4d sc[2], md[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          const u32x2d st = {vst[t], 0u};
+          sc[t] = mfma16(st, u32x2d{pick[e], 0u}, f32x4d{});
+          md[t] = mfma16(st, u32x2d{mids[e], 0u}, f32x4d{});
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          float z[8];
+          if (cut) {  // scales that are not finite where the weight is 0
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              z[j] = w[n][j] == 0.0f ? 0.0f : w[n][j] * sc[j / 4][j % 4];
+              off[n][e] += w[n][j] == 0.0f ? 0.0f : w[n][j] * md[j / 4][j % 4];
+            }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+              z[j] = w[n][j] * sc[j / 4][j % 4];
+              off[n][e] = __builtin_fmaf(w[n][j], md[j / 4][j % 4], off[n][e]);
+            }
+          }
+          operands(z, h[n], lo2[n]);
+          const uint32_t bits = FMT == KV_U8 ? 0x80808080u : 0x80088008u;  // minus the middle, as the codes
+          const u32x4d minus = {bits, bits, bits, bits};
+          mid[n][e] = mfma16(minus, h[n], mid[n][e]);
+          if constexpr (TWO) mid[n][e] = mfma16(minus, lo2[n], mid[n][e]);
+        }
+      } else {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          float z[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) z[j] = w[n][j] * BF16_DOWN;
+          operands(z, h[n], lo2[n]);
+        }
+        if (cut) {
+          // values that are not finite: out of the products, and in by themselves where there is a weight
+          bool any = false;
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int v = 0; v < F::VW; ++v) any |= wild(vw[j][v]);
+          if (__any(any)) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+#pragma unroll 1
+              for (int src = 0; src < 4; ++src) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                  const float z = __shfl(w[n][j], col + 16 * src) * BF16_DOWN;
+#pragma unroll
+                  for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int v = 0; v < F::VW; ++v) {
+                      const uint32_t pairs = __shfl(vw[j][v], 4 * grp + r + 16 * src);
+                      const float a = __uint_as_float(pairs << 16), b2 = __uint_as_float(pairs & 0xFFFF0000u);
+                      if (z != 0.0f && a - a != 0.0f) acc[n][2 * v][r] += z * a;
+                      if (z != 0.0f && b2 - b2 != 0.0f) acc[n][2 * v + 1][r] += z * b2;
+                    }
+                }
+              }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+              for (int v = 0; v < F::VW; ++v) {
+                if ((vw[j][v] & 0x7F80u) == 0x7F80u) vw[j][v] &= 0xFFFF0000u;
+                if ((vw[j][v] & 0x7F800000u) == 0x7F800000u) vw[j][v] &= 0xFFFFu;
+              }
+          }
+        }
+      }
+#pragma unroll
+      for (int k = e * F::NV / NG; k < (e + 1) * F::NV / NG; ++k) {
+        u32x4d a;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) a[r] = value_pair<FMT, D>(vw[2 * r], vw[2 * r + 1], k);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          acc[n][k] = mfma16(a, h[n], acc[n][k]);
+          if constexpr (TWO) acc[n][k] = mfma16(a, lo2[n], acc[n][k]);
+        }
+      }
+    }
+    nv[0] = next.nv[0];
+    nv[1] = next.nv[1];
+    load_values();
+  }
+
+  // join the wavefronts, a column tile at a time
+  const bool whole = parts == 1;
+  const int64_t slot = int64_t(unit.slot) + unit.at;
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const float ln = sum4(l[n]);
+    if (n) __syncthreads();
+#pragma unroll
+    for (int e = 0; e < NG; ++e) {
+      const float o = CODES ? sum4(off[n][e]) : 0.0f;
+#pragma unroll
+      for (int k = e * F::NV / NG; k < (e + 1) * F::NV / NG; ++k) {
+        f32x4d v = acc[n][k];
+        if constexpr (CODES) v = sixteenfold(k) ? (v + mid[n][e] * 16.0f) * (VBACK / 16) + o : (v + mid[n][e]) * VBACK + o;
+        *reinterpret_cast<f32x4d*>(&so[wave][col][16 * k + 4 * grp]) = v;
+      }
+    }
+    if (grp == 0) {
+      sm[wave][col] = m[n];
+      ss[wave][col] = ln;
+    }
+    __syncthreads();
+    // two neighbouring channels of a column a thread
+    for (int o = threadIdx.x; o < 16 * D / 2; o += 256) {
+      const int h = o / (D / 2), cn = o % (D / 2) * 2;
+      const int64_t idx = int64_t(tile) * COLS + 16 * n + h;
+      const int j = int(idx / G);
+      const int64_t r = int64_t(seq.first) + j;
+      if (j >= seq.m || r >= p.T) break;
+      const int a0 = CODES ? cn : cn % F::NV * 16 + cn / F::NV;
+      const int a1 = CODES ? cn + 1 : a0 + 16;
+      float top = sm[0][h];
+#pragma unroll
+      for (int v = 1; v < WAVES; ++v) top = fmaxf(top, sm[v][h]);
+      float t = 0.0f, x0 = 0.0f, x1 = 0.0f;
+#pragma unroll
+      for (int v = 0; v < WAVES; ++v) {
+        const float f = __builtin_amdgcn_exp2f(sm[v][h] - top);
+        t += f * ss[v][h];
+        x0 += f * so[v][h][a0];
+        x1 += f * so[v][h][a1];
+      }
+      if (whole) {
+        const int hd = g * G + int(idx % G);
+        const float inv = (CODES ? 1.0f : BF16_BACK) / t;
+        // no weight at all: 0, where the values may have made the sums NaN
+        *reinterpret_cast<uint32_t*>(p.O + r * p.ld_o + int64_t(hd) * D + cn) = t == 0.0f ? 0u : pack_bf16x2(x0 * inv, x1 * inv);
+        if (cn == 0 && p.lse) p.lse[r * p.H + hd] = t == 0.0f ? -__builtin_inff() : top + __builtin_amdgcn_logf(t);
+      } else if (slot < 2 * int64_t(target)) {
+        float* out = part_of<COLS, D>(p, slot, g, 16 * n + h);
+        *reinterpret_cast<float2*>(out + 4 + cn) = make_float2(x0, x1);
+        if (cn == 0) *reinterpret_cast<float2*>(out) = make_float2(top, t);
+      }
+    }
+  }
+}
+
+// Joins the shares of a tile's columns: D / 4 lanes a share of a column, PAR
+// shares of it at a time, four of each in flight; 256 / (PAR D / 4) columns.
+template <int D, int COLS, int PAR>
+__global__ __launch_bounds__(256) void attn_extend_join_kernel(AttnExtendLaunch p, int target) {
+  constexpr int LANES = D / 4, ROWS = 256 / LANES / PAR, GROUPS = COLS / ROWS;
+  const int G = p.H / p.c.H_kv;
+  const int64_t b = workgroup();
+  const int g = int(b % p.c.H_kv), group = int(b / p.c.H_kv % GROUPS);
+  Unit unit;
+  if (!find<COLS, true>(p, G, b / p.c.H_kv / GROUPS, target, unit)) return;
+  const int s = unit.s;
+  const Seq seq = seq_of(p, scalar(p.row_start, s), scalar(p.row_start, s + 1), scalar(p.lens, s));
+  const Work<COLS> work{p, G};
+  const int tiles = work.tiles(seq), n = std::max(1, (work.steps(seq) + unit.per - 1) / unit.per);
+  if (n == 1) return;
+  const int lane = threadIdx.x % LANES, rank = threadIdx.x / LANES % PAR, col = group * ROWS + threadIdx.x / LANES / PAR;
+  const int tile = unit.at;
+  const int64_t idx = int64_t(tile) * COLS + col;
+  const int64_t r = int64_t(seq.first) + idx / G;
+  const bool real = idx / G < seq.m && r < p.T && int64_t(unit.slot) + int64_t(n) * tiles <= 2 * int64_t(target);
+  float m = LOWEST, t = 0.0f;
+  f32x4d a = {};
+  if (real) {
+    for (int k = rank; k < n; k += 4 * PAR) {
+      float2 ml[4];
+      f32x4d o[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int j = std::min(k + i * PAR, n - 1);
+        const float* part = part_of<COLS, D>(p, int64_t(unit.slot) + int64_t(j) * tiles + (tiles - 1 - tile), g, col);
+        ml[i] = *reinterpret_cast<const float2*>(part);
+        o[i] = *reinterpret_cast<const f32x4d*>(part + 4 + 4 * lane);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (k + i * PAR >= n) break;
+        const float m1 = fmaxf(m, ml[i].x);
+        const float f0 = __builtin_amdgcn_exp2f(m - m1), f1 = __builtin_amdgcn_exp2f(ml[i].x - m1);
+        m = m1;
+        t = t * f0 + ml[i].y * f1;
+        a = a * f0 + o[i] * f1;
+      }
+    }
+  }
+  if constexpr (PAR > 1) {
+    __shared__ f32x4d so[256];
+    __shared__ float sm[256 / LANES], st[256 / LANES];
+    so[threadIdx.x] = a;
+    if (lane == 0) {
+      sm[threadIdx.x / LANES] = m;
+      st[threadIdx.x / LANES] = t;
+    }
+    __syncthreads();
+    if (rank) return;
+    const int first = threadIdx.x / LANES;
+    float top = sm[first];
+#pragma unroll
+    for (int k = 1; k < PAR; ++k) top = fmaxf(top, sm[first + k]);
+    t = 0.0f;
+    a = f32x4d{};
+#pragma unroll
+    for (int k = 0; k < PAR; ++k) {
+      const float f = __builtin_amdgcn_exp2f(sm[first + k] - top);
+      t += f * st[first + k];
+      a += f * so[(first + k) * LANES + lane];
+    }
+    m = top;
+  }
+  if (!real) return;
+  const int hd = g * G + int(idx % G);
+  const float inv = (p.c.format == KV_BF16 ? BF16_BACK : 1.0f) / t;
+  *reinterpret_cast<uint2*>(p.O + r * p.ld_o + int64_t(hd) * D + 4 * lane) =
+      t == 0.0f ? make_uint2(0u, 0u) : make_uint2(pack_bf16x2(a[0] * inv, a[1] * inv), pack_bf16x2(a[2] * inv, a[3] * inv));
+  if (lane == 0 && p.lse) p.lse[r * p.H + hd] = t == 0.0f ? -__builtin_inff() : m + __builtin_amdgcn_logf(t);
+}
+
+// Column tiles of a workgroup, for the columns that a sequence has on average.
+int col_tiles(int64_t T, int64_t n_seq, int H, int H_kv) {
+  const int64_t cols = (T + n_seq - 1) / n_seq * (H / H_kv);
+  return cols <= 16 ? 1 : 2;
+}
+// Tiles of one key/value head, if no row is padding.
+int64_t tiles_of(int64_t T, int H, int H_kv, int nt) { return T * (H / H_kv) / (16 * nt); }
+// Shares of one key/value head that are wanted (0: no tile is cut).
+int target_of(int64_t T, int64_t n_seq, int H, int H_kv, int64_t max_pages, int page_len) {
+  const int nt = col_tiles(T, n_seq, H, H_kv);
+  const int64_t want = 2 * CUS / H_kv;
+  if (max_pages * page_len <= MIN_STEPS * STEP || tiles_of(T, H, H_kv, nt) >= want) return 0;
+  return int(want);
+}
+
+template <int FMT, int D, int NG, int NT>
+hipError_t launch_nt(const AttnExtendLaunch& p, hipStream_t st) {
+  const int H_kv = p.c.H_kv, target = target_of(p.T, p.c.n_seq, p.H, H_kv, p.c.max_pages, p.c.page_len);
+  const int64_t tiles = tiles_of(p.T, p.H, H_kv, NT) + std::min(p.T, p.c.n_seq);
+  attn_extend_kernel<FMT, D, NG, NT><<<grid_of((tiles + target) * H_kv), 256, 0, st>>>(p, target);
+  if (hipError_t e = hipGetLastError()) return e;
+  if (!target) return hipSuccess;
+  constexpr int COLS = 16 * NT, LANES = D / 4;
+  if (p.T * p.H <= 2048)
+    attn_extend_join_kernel<D, COLS, 256 / LANES><<<grid_of(tiles * H_kv * COLS), 256, 0, st>>>(p, target);
+  else
+    attn_extend_join_kernel<D, COLS, 1><<<grid_of(tiles * H_kv * COLS * LANES / 256), 256, 0, st>>>(p, target);
+  return hipGetLastError();
+}
+
+template <int FMT, int D, int NG>
+hipError_t launch_form(const AttnExtendLaunch& p, hipStream_t st) {
+  return col_tiles(p.T, p.c.n_seq, p.H, p.c.H_kv) == 1 ? launch_nt<FMT, D, NG, 1>(p, st) : launch_nt<FMT, D, NG, 2>(p, st);
+}
+
+template <int D>
+hipError_t launch_d(const AttnExtendLaunch& p, hipStream_t st) {
+  const bool one = p.c.group == D;
+  if (p.c.format == KV_BF16) return launch_form<KV_BF16, D, 1>(p, st);
+  if (p.c.format == KV_U8) return one ? launch_form<KV_U8, D, 1>(p, st) : launch_form<KV_U8, D, D / 32>(p, st);
+  return one ? launch_form<KV_U4, D, 1>(p, st) : launch_form<KV_U4, D, D / 32>(p, st);
+}
+
+}  // namespace
+
+size_t attn_extend_ws(int64_t T, int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len) {
+  const size_t target = size_t(target_of(T, n_seq, H, H_kv, max_pages, page_len));
+  return 2 * target * size_t(H_kv) * size_t(16 * col_tiles(T, n_seq, H, H_kv)) * size_t(d + 4);
+}
+
+hipError_t launch_attn_extend(const AttnExtendLaunch& p, hipStream_t st) {
+  return p.c.d == 128 ? launch_d<128>(p, st) : launch_d<64>(p, st);
+}
+
+}  // namespace uq

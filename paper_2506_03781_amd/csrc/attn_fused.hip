@@ -280,9 +280,7 @@ __device__ __forceinline__ void copy_tile(const uint16_t* base, const uint32_t (
 
 // Windows (WIN).  Any L: the rows of the last tile that lie behind L are copies
 // of row L - 1, which no query before them sees and whose own results are not
-// stored.  P enters dS before its rounding to bf16 (one rounding less in dQ and
-// dK: relative errors 2.4e-3 in place of 2.9e-3, the outputs' own rounding among
-// them).
+// stored.  P enters dS before its rounding to bf16, one rounding less in dQ and dK.
 template <bool WIN, int PW>
 __device__ __forceinline__ void copy_rows(const uint16_t* base, const uint32_t (&off)[PW], u32x4a* tile, int wave, int lane,
                                           int ld, int rows) {
@@ -525,6 +523,81 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(KS
   if (lane < 32) a.lse[b * L + qi] = lse;
 }
 
+// Delta of a window's rows from sum_j P_ij dP_ij, in a walk of its own.  From the
+// stored O, as the causal kernels take it, its error is O's rounding, the same for
+// all keys of a row: where few keys hold the weight, O is as large as the values,
+// and with keys whose mean is not 0 (channels of outliers) it was the largest error
+// of dQ by far (4 x 2048 rows, 32 heads, window 512, one channel of the keys ten
+// times the others: dQ off by 4.0e-3 of its norm and by up to 0.66 of an element's
+// size, now 3.2e-3 and 0.25; the walk takes 147 of 924 us).
+template <int NW, int S, bool TOK>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(3))) void attn_window_delta_kernel(AttnArgs a) {
+  constexpr int QB = NW * NB;
+  constexpr int PW = 8 / NW;
+  constexpr int STAGE = 2 * TILE16;  // key tile, value tile
+  __shared__ u32x4a smem[S * STAGE];
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6));
+  const int L = a.L;
+  int qb;
+  int64_t b;
+  block_of((L + QB - 1) / QB, a.batch, qb, b);
+  const int64_t bk = b % a.kv_batch;
+  const int q0 = qb * QB + wave * NB;
+  const int qi = q0 + (lane & 31), qc = min(qi, L - 1);
+  const int my_tiles = q0 < L ? q0 / NB + 1 : 0;
+  const KeyWalk walk = key_walk(qb * QB, (min(L, qb * QB + QB) + NB - 1) / NB, a.window, a.sinks);
+  const uint16_t* Kb = a.K + bk * int64_t(L) * D;
+  const uint16_t* Vb = a.V + bk * int64_t(L) * D;
+  const float c = a.scale * LOG2E;
+  uint32_t ro[PW];
+#pragma unroll
+  for (int q = 0; q < PW; ++q) ro[q] = row_off(wave * PW + q, lane);
+  auto copy = [&](int i) {
+    const int t = walk.tile(i);
+    u32x4a* st = smem + i % S * STAGE;
+    copy_rows<true, PW>(Kb + int64_t(t) * NB * D, ro, st, wave, lane, D, L - t * NB);
+    copy_rows<true, PW>(Vb + int64_t(t) * NB * D, ro, st + TILE16, wave, lane, D, L - t * NB);
+  };
+  bf16x8a qf[8], df[8];
+  {
+    const int64_t row = (b * L + qc) * int64_t(D) + 8 * (lane >> 5);
+    const int64_t orow = (TOK ? tok_off(a, b, qc) : (b * L + qc) * int64_t(D)) + 8 * (lane >> 5);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      qf[j] = __builtin_bit_cast(bf16x8a, *reinterpret_cast<const u32x4a*>(a.Q + row + 16 * j));
+      df[j] = __builtin_bit_cast(bf16x8a, *reinterpret_cast<const u32x4a*>(a.dO + orow + 16 * j));
+    }
+  }
+  const float lse = a.lse[b * L + qc];
+  float sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < S - 1; ++i)
+    if (i < walk.n) copy(i);
+  for (int i = 0; i < walk.n; ++i) {
+    wait_tiles<2 * PW>(min(S - 2, walk.n - 1 - i));
+    lds_wait_barrier();
+    if (i + S - 1 < walk.n) copy(i + S - 1);
+    const int t = walk.tile(i);
+    if (t >= my_tiles || !(t * NB < a.sinks || t >= first_tile(q0, a.window))) continue;
+    const u32x4a* tk = smem + i % S * STAGE;
+    f32x16a s = zero16(), dp = zero16();
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      s = mfma(row_frag(tk, j, lane), qf[j], s);
+      dp = mfma(row_frag(tk + TILE16, j, lane), df[j], dp);
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int j = t * NB + slot_row(r, lane);
+      const bool hidden = j > qi || (qi - j >= a.window && j >= a.sinks);
+      sum += hidden ? 0.0f : exp2a(fmaf(s[r], c, -lse)) * dp[r];
+    }
+  }
+  sum += __shfl_xor(sum, 32, 64);
+  if (lane < 32 && qi < L) a.delta[b * L + qi] = sum;
+}
+
 // Backward for the queries: delta = dO . O per row, then per key tile
 // S -> P (from lse), dP = dO V^T, dS = bf16(P (dP - delta)), dQ += dS K;
 // dQ * scale stored in fp32, delta stored for the key kernel.
@@ -579,12 +652,16 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(2,
     for (int j = 0; j < 8; ++j) {
       qf[j] = __builtin_bit_cast(bf16x8a, *reinterpret_cast<const u32x4a*>(a.Q + row + 16 * j));
       df[j] = __builtin_bit_cast(bf16x8a, *reinterpret_cast<const u32x4a*>(a.dO + orow + 16 * j));
-      const bf16x8a ov = __builtin_bit_cast(bf16x8a, *reinterpret_cast<const u32x4a*>(a.O + orow + 16 * j));
+      if constexpr (!WIN) {
+        const bf16x8a ov = __builtin_bit_cast(bf16x8a, *reinterpret_cast<const u32x4a*>(a.O + orow + 16 * j));
 #pragma unroll
-      for (int i = 0; i < 8; ++i) dl += float(df[j][i]) * float(ov[i]);
+        for (int i = 0; i < 8; ++i) dl += float(df[j][i]) * float(ov[i]);
+      }
     }
   }
-  {  // delta: this lane's 64 d values plus the other half-wave's (lower half first)
+  if constexpr (WIN) {
+    dl = a.delta[b * L + qc];
+  } else {  // delta: this lane's 64 d values plus the other half-wave's (lower half first)
     const float d2 = __shfl_xor(dl, 32, 64);
     dl = lane < 32 ? dl + d2 : d2 + dl;
   }
@@ -645,7 +722,7 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(2,
     if (ks != 0) return;
   }
   if (!active || (WIN && qi >= L)) return;
-  if (lane < 32) a.delta[b * L + qi] = dl;
+  if (!WIN && lane < 32) a.delta[b * L + qi] = dl;
   if constexpr (TOK) store_bf16_row<true>(a.dQ_tok + tok_off(a, b, qi), dq, a.scale, a.cs, qi, lane);
   else store_f32_rows(a.dQ + (b * L + qi) * int64_t(D), dq, a.scale, lane);
 }
@@ -664,7 +741,7 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(2,
   constexpr int KB = NW * NB;
   constexpr int PW = 8 / NW;
   constexpr int STAGE = 2 * TILE16 + 64;  // Q, dO tiles, row terms
-  constexpr int NPARK = WIN ? 5 : 3;
+  constexpr int NPARK = WIN ? 6 : 3;
   __shared__ u32x4a smem[S * KS * STAGE + NW * KS * NPARK * 64];
   const int lane = threadIdx.x & 63;
   const int wv = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6));
@@ -673,7 +750,19 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(2,
   int kb;
   int64_t b;
   block_of((L + KB - 1) / KB, a.batch, kb, b);
-  if constexpr (WIN) kb = (L + KB - 1) / KB - 1 - kb;  // the sinks, which most queries see, first
+  if constexpr (WIN) {
+    // the blocks with sinks, which most queries see, first; then all others alike, an XCD's by batch
+    const int nblk = (L + KB - 1) / KB, heavy = min((a.sinks + KB - 1) / KB, nblk), light = nblk - heavy;
+    const int64_t w = blockIdx.x, v = w - heavy * a.batch;
+    const bool even = (a.batch & 7) == 0;
+    if (v < 0) {
+      b = w % a.batch;
+      kb = int(w / a.batch);
+    } else {
+      b = even ? (v & 7) + 8 * ((v >> 3) / light) : v / light;
+      kb = heavy + int((even ? v >> 3 : v) % light);
+    }
+  }
   const int64_t bk = b % a.kv_batch;
   const int k0 = kb * KB + wave * NB;
   const bool active = k0 < L;
@@ -914,6 +1003,11 @@ hipError_t launch_attn_bwd(const AttnLaunch& q, hipStream_t st) {
   const int64_t blocks = nblk * q.batch;
   const bool split = splits(q, nblk);
   const int ks = split ? 2 : 1;
+  if (win) {
+    const auto kern = tok ? attn_window_delta_kernel<NW, S, true> : attn_window_delta_kernel<NW, S, false>;
+    launch(kern, blocks, 1, a, st);
+    if (hipError_t e = hipGetLastError()) return e;
+  }
   launch(UQ_ATTN_FORM(attn_bwd_dq_kernel)(tok, split, win), blocks, ks, a, st);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;

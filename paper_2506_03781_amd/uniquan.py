@@ -100,6 +100,9 @@ _SIGS = {
     "uniquan_attn_decode_ws": ([_i64, _i32, _i32, _i32, _i64, _i32], ctypes.c_size_t),
     "uniquan_attn_decode": ([_i64, _i32, _i32, _i32, _vp, _i64, _vp, _vp, _i64, _i32, _i32, _i64, _i32, _vp, _vp, _vp,
                              _vp, _f32, _vp, _i64, _vp, _vp, ctypes.c_size_t, _vp], _i32),
+    "uniquan_attn_extend_ws": ([_i64, _i64, _i32, _i32, _i32, _i64, _i32], ctypes.c_size_t),
+    "uniquan_attn_extend": ([_i64, _i64, _i32, _i32, _i32, _vp, _i64, _vp, _vp, _vp, _i32, _vp, _i32, _i32, _vp, _i64, _i32,
+                             _i32, _i64, _i32, _vp, _vp, _vp, _vp, _f32, _vp, _i64, _vp, _vp, ctypes.c_size_t, _vp], _i32),
     "uniquan_sample_ws": ([_i64, _i64], ctypes.c_size_t),
     "uniquan_sample": ([_i64, _i64, _vp, _i64, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp], _i32),
     "uniquan_probe_mfma_flops": ([_i32], ctypes.c_double),
@@ -292,6 +295,7 @@ _U8 = (torch.uint8,)
 _H = (torch.float16,)
 _U32 = (torch.int32, torch.uint32)  # bit-plane words (bits only)
 _I32 = (torch.int32,)
+_U64 = (torch.int64, torch.uint64)  # mask words (bits only)
 
 
 def uniquan_fq_fwd(R, C, k, g, W, s, s_r, delta, z_u, alpha, z_b, mode, codes, W_hat, stream=None):
@@ -805,6 +809,32 @@ def uniquan_attn_decode(n_seq, H, Hkv, d, Q, lens, table, k_cache, v_cache, scal
         n_seq, H, Hkv, d, pq, ld_q, _p(lens, n_seq, _I32, "lens"), pg, mp, *f, *m, float(scale), po, ld_o,
         _p(row_lse, n_seq * H, _F, "row_lse"), _p(ws, None, _F, "ws"), 0 if ws is None else ws.numel(),
         _stream(stream)))
+
+
+def uniquan_attn_extend_ws(T, n_seq, H, Hkv, d, max_pages, page_len) -> int:
+    return int(lib().uniquan_attn_extend_ws(T, n_seq, H, Hkv, d, max_pages, page_len))
+
+
+def uniquan_attn_extend(T, n_seq, H, Hkv, d, Q, row_start, lens, table, k_cache, v_cache, scale, O, row_lse=None, ws=None,
+                        mask=None, pos=None, window=0, sinks=0, fmt=KV_BF16, group=0, page_len=64, k_stat=None,
+                        v_stat=None, stream=None):
+    """O [T, H d] (bf16; a column slice allowed) and row_lse [T, H]: attention of the rows Q [T, H d] (bf16; a column
+    slice allowed), row_start[s] .. row_start[s + 1] of them of sequence s, whose places are the last of its lens[s]
+    positions.  mask [T, words] (64-bit words): the new places that a row sees, None: those up to its own; window,
+    sinks, pos [T]: which of the others (see the header).  ws: fp32 workspace of uniquan_attn_extend_ws floats."""
+    _one_device(Q, row_start, lens, table, k_cache, v_cache, O, row_lse, ws, mask, pos, k_stat, v_stat)
+    (pg, ns, mp), f, m = _kv(Hkv, d, page_len, table, k_cache, v_cache, k_stat, v_stat, fmt, group)
+    if ns != n_seq:
+        raise ValueError(f"table has {ns} rows, n_seq is {n_seq}")
+    if mask is not None and (not isinstance(mask, torch.Tensor) or mask.dim() != 2 or mask.shape[0] < T):
+        raise ValueError(f"mask must be a [{T}, words] tensor")
+    pq, ld_q = _ld(Q, T, H * d, _B, "Q")
+    po, ld_o = _ld(O, T, H * d, _B, "O")
+    _check(lib().uniquan_attn_extend(
+        T, n_seq, H, Hkv, d, pq, ld_q, _p(row_start, n_seq + 1, _I32, "row_start"), _p(lens, n_seq, _I32, "lens"),
+        _p(mask, None, _U64, "mask"), 0 if mask is None else mask.shape[1], _p(pos, T, _I32, "pos"), int(window), int(sinks),
+        pg, mp, *f, *m, float(scale), po, ld_o, _p(_whole(row_lse, (T, H), "row_lse"), T * H, _F, "row_lse"),
+        _p(ws, None, _F, "ws"), 0 if ws is None else ws.numel(), _stream(stream)))
 
 
 def uniquan_sample_ws(T, V) -> int:

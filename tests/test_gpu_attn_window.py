@@ -4,7 +4,7 @@ Bars, element by element, from the roundings alone (u = 2^-24; bf16 rounds by 2^
   scores   d products and sums in fp32, scale, exponent: dx = (d + 16) u max scale sum |q||k| of the row; weights are
            then off by e^(2 dx) - 1 (numerator and log-sum-exp), and 2^-20 for the exponential and the logarithm
   P        2^-8 more in the products with V and dO; O is stored in bf16, 2^-8
-  dP       (d + 4) u sum |dO||V|;  delta: |dO| times the bar of O, and (d + 4) u sum |dO||O|
+  dP       (d + 4) u sum |dO||V|;  delta = sum P dP: the errors of both, and (n + 4) u sum P |dP|
   dS       weights' error of P |dP - delta|, P times the errors of dP and delta, 2^-8 for its rounding
   sums over n terms in fp32: (n + 4) u of the terms' absolute sum; outputs in bf16 2^-8; a rotated pair carries the
   bars of both its halves, and 2^-22 for the table and its products."""
@@ -84,11 +84,10 @@ class Case:
         ew = (torch.expm1(2 * dx) + 2.0 ** -20)[..., None]
         n = see.sum(1).double()[:, None]
         tO = P @ v.abs() * (ew + H8 + (n + 4) * U)
-        tO_stored = tO + H8 * (O.abs() + tO)
         dP = g @ v.transpose(1, 2)
         tdP = (D + 4) * U * (g.abs() @ v.abs().transpose(1, 2))
         delta = (g * O).sum(-1, keepdim=True)
-        tdelta = (g.abs() * tO_stored).sum(-1, keepdim=True) + (D + 4) * U * (g * O).abs().sum(-1, keepdim=True)
+        tdelta = (P * (dP.abs() * (ew + (n + 4) * U) + (1 + ew) * tdP)).sum(-1, keepdim=True)
         dS = P * (dP - delta)
         tdS = dS.abs() * ew + P * (1 + ew) * (tdP + tdelta)
         tdS = tdS + H8 * (dS.abs() + tdS)
