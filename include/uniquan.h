@@ -968,7 +968,7 @@ uq_status uniquan_attn_extend(int64_t T, int64_t n_seq, int H, int H_kv, int d,
 /*
  * uniquan_sample -- one token per row of logits x [V], from a given random number:
  * the end of a serving step.  With t = temperature and M the largest logit,
- *   w_i = e^((x_i - M) / t), in units of 2^-sh, sh = min(52, 62 - ceil(log2 V))
+ *   w_i = e^((x_i - M) / t), in units of 2^-sh, sh = min(51, 62 - ceil(log2 V))
  *         (an integer each, rounded to nearest from 64-bit arithmetic);
  *   order: larger logits first, equal ones by index;
  *   top_k  the first top_k in order (<= 0 or >= V: all);

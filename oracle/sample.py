@@ -6,7 +6,7 @@ import numpy as np
 
 
 def shift(V):
-    return min(52, 62 - max(0, math.ceil(math.log2(V))))
+    return min(51, 62 - max(0, math.ceil(math.log2(V))))
 
 
 def weights(x, t, sh):

@@ -1,27 +1,31 @@
 // One token per row of logits (uniquan_sample); definition and errors in
 // uniquan.h.
 //
-// Weights.  w = rint(2^sh e^((x - max) / t)), sh = 62 - ceil(log2 V): integers
-// whose sums are exact and the same in any order, so that every comparison of
-// a running sum with a border has one answer however the work is split.  The
+// Weights.  w = rint(2^sh e^((x - max) / t)), sh = min(51, 62 - ceil(log2 V)):
+// integers whose sums are exact and the same in any order, so that every comparison
+// of a running sum with a border has one answer however the work is split.  The
 // exponential is taken in 64 bits: with one in 32 bits the running sums of some
-// ten thousand tokens are off by 1e-7 of their total, and a random number
-// falls that near to one of the borders once in some hundred rows.
+// ten thousand tokens are off by 1e-7 of their total, and a random number falls that
+// near to one of the borders once in some hundred rows.
 //
-// A workgroup takes a row and reads it once per pass (the first time from
-// memory, then from the caches):
-//   maximum    of (value, lowest index): also the greedy answer.
-//   histogram  counts and sums of weights in BINS equal steps of (max - x) / t,
-//              where top-k or top-p is on.  Its running sums say in which bin
-//              the k-th token lies and in which the nucleus ends.
-//   gather     what lies up to there, if it is at most CAP tokens, goes to LDS
-//              and everything else happens there (sorted by value, cut, sorted by
-//              index); else the bin in which the cut lies, to find it exactly.
-//              A bin of more than CAP tokens is cut by further histograms, of
-//              equal steps between its smallest and largest value; many tokens of
-//              one value by their indices.
-//   sums       of the weights kept, per run of indices of a wavefront; the run in
-//              which u times the total falls is read again by one wavefront.
+// A workgroup takes a row and reads it once per pass (the first time from memory,
+// then from the caches):
+//   maximum    of every lane's tokens and of all: also the greedy answer.
+//   top-k of up to ENOUGH: the k-th best of the lanes' best tokens is a value that k
+//              tokens reach at least, and few more.  They are gathered in LDS, and
+//              everything else happens there.
+//   histogram  (top-p, larger k) counts and sums of weights in BINS equal steps of
+//              (max - x) / t: its running sums say in which bin the k-th token lies
+//              and in which the nucleus ends.  A nucleus of up to CAP tokens is
+//              gathered too; else the bin in which the cut lies, to find it exactly.
+//              A bin of more than CAP tokens is cut by further histograms, of equal
+//              steps between its smallest and largest value; many tokens of one value
+//              by their indices.
+//   sums       of the weights kept, a sixteenth of the indices a wavefront, then of
+//              the one in whose share u times the total falls, and so on.
+// Up to FEW gathered tokens are not sorted: 1024 / n threads a token go through the
+// others for its rank and the sums before it (of 1024 tokens that takes 55 us, their
+// sorting 4).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -35,11 +39,19 @@ namespace uq {
 namespace {
 
 constexpr int THREADS = 1024, WAVES = THREADS / 64;
-constexpr int BINS = 2048;  // two a thread
-constexpr int CAP = 4096;   // tokens that are sorted in LDS
-constexpr int RUNS = 1024;  // runs of indices
+constexpr int BINS = 2048;   // two a thread
+constexpr int CAP = 1024;    // tokens gathered in LDS
+constexpr int FEW = 128;     // of those that are not sorted
+constexpr int ENOUGH = 512;  // best tokens of lanes that are asked for
 
 typedef unsigned long long u64;
+
+// x, the same in every lane, in scalar registers.
+__device__ __forceinline__ uint32_t uni(uint32_t x) { return uint32_t(__builtin_amdgcn_readfirstlane(int(x))); }
+__device__ __forceinline__ int uni(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ float uni(float x) { return __uint_as_float(uni(__float_as_uint(x))); }
+__device__ __forceinline__ u64 uni(u64 x) { return u64(uni(uint32_t(x >> 32))) << 32 | uni(uint32_t(x)); }
+__device__ __forceinline__ double uni(double x) { return __longlong_as_double((long long)uni(u64(__double_as_longlong(x)))); }
 
 // Order of the tokens, best first: larger values, then lower indices.
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -52,38 +64,40 @@ __device__ __forceinline__ float value_of(uint32_t key) {
 }
 __device__ __forceinline__ u64 place_of(float x, int i) { return u64(key_of(x)) << 32 | uint32_t(i); }
 
-__device__ __forceinline__ u64 shfl_up(u64 x, int d) {
-  return u64(__shfl_up(uint32_t(x >> 32), d)) << 32 | __shfl_up(uint32_t(x), d);
-}
 __device__ __forceinline__ u64 shfl_xor(u64 x, int d) {
   return u64(__shfl_xor(uint32_t(x >> 32), d)) << 32 | __shfl_xor(uint32_t(x), d);
 }
-__device__ __forceinline__ u64 shfl(u64 x, int l) {
-  return u64(__shfl(uint32_t(x >> 32), l)) << 32 | __shfl(uint32_t(x), l);
-}
-__device__ __forceinline__ u64 wave_sum(u64 x) {
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) x += shfl_xor(x, d);
-  return x;
+// x of the lane that a DPP control names, 0 where there is none.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ u64 moved(u64 x) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, uint32_t(x), CTRL, ROWS, 0xF, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, uint32_t(x >> 32), CTRL, ROWS, 0xF, false);
+  return u64(hi) << 32 | lo;
 }
 // Sum over the lanes up to this one.
 __device__ __forceinline__ u64 wave_upto(u64 x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const u64 y = shfl_up(x, d);
-    x += lane >= d ? y : 0;
-  }
+  x += moved<0x111, 0xF>(x);  // row_shr:1
+  x += moved<0x112, 0xF>(x);
+  x += moved<0x114, 0xF>(x);
+  x += moved<0x118, 0xF>(x);
+  x += moved<0x142, 0xA>(x);  // row_bcast:15
+  x += moved<0x143, 0xC>(x);  // row_bcast:31
   return x;
+}
+__device__ __forceinline__ u64 wave_sum(u64 x) {
+  x = wave_upto(x);
+  return u64(uint32_t(__builtin_amdgcn_readlane(uint32_t(x >> 32), 63))) << 32 |
+         uint32_t(__builtin_amdgcn_readlane(uint32_t(x), 63));
 }
 
 struct Lds {
   u64 mass[BINS];
   uint32_t count[BINS];
-  u64 list[CAP];
+  u64 list[CAP], weight[FEW];
   u64 wave[WAVES];
   u64 found[4];
   uint32_t n, lo, hi;
+  float top[WAVES];
 };
 
 // Sum over the workgroup's threads before this one; all: of all of them.
@@ -104,13 +118,19 @@ __device__ __forceinline__ u64 block_before(Lds& s, u64 x, u64& all) {
   return before + upto - x;
 }
 
+// What a row without a whole chunk loads in place of one.
+__device__ const uint4 no_chunk = {};
+
 // A row as aligned chunks of 16 bytes, the first and the last in part.
 template <bool F32>
 struct Row {
   static constexpr int E = F32 ? 4 : 8;
+  static constexpr uint32_t NONE = F32 ? 0xFF800000u : 0xFF80FF80u;  // -infinity
   const char* at;  // of chunk 0
   int shift;       // elements of chunk 0 before the row
   int V, chunks;
+  int per;         // chunks of a lane: a wavefront's lie side by side
+  int lo, hi;      // the whole chunks (lo > hi: none)
 
   __device__ Row(const void* x, int64_t off, int V) : V(V) {
     const char* p = static_cast<const char*>(x) + off * (F32 ? 4 : 2);
@@ -118,88 +138,139 @@ struct Row {
     at = p - over;
     shift = over / (F32 ? 4 : 2);
     chunks = (shift + V + E - 1) / E;
+    per = (chunks + THREADS - 1) / THREADS;
+    lo = shift > 0;
+    hi = (shift + V) / E - 1;
   }
+  __device__ __forceinline__ int chunk(int wave, int i) const { return (wave * per + i) * 64 + int(threadIdx.x & 63); }
   __device__ __forceinline__ int first(int c) const { return c * E - shift; }
-  __device__ __forceinline__ bool whole(int c) const { return first(c) >= 0 && first(c) + E <= V; }
-  // Words of chunk c; what is outside the row is -infinity.
-  __device__ __forceinline__ uint4 load(int c) const {
-    if (whole(c)) return reinterpret_cast<const uint4*>(at)[c];
-    uint32_t w[4] = {};
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int i = first(c) + e;
-      const bool in = i >= 0 && i < V;
-      if constexpr (F32) {
-        w[e] = in ? reinterpret_cast<const uint32_t*>(at)[int64_t(c) * E + e] : 0xFF800000u;
-      } else {
-        w[e / 2] |= uint32_t(in ? reinterpret_cast<const uint16_t*>(at)[int64_t(c) * E + e] : 0xFF80u) << (16 * (e & 1));
-      }
-    }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+  // Words of chunk c, without a branch: of one in part, or of none, some other's.
+  __device__ __forceinline__ uint4 ask(int c) const {
+    const uint4* p = reinterpret_cast<const uint4*>(lo <= hi ? at : reinterpret_cast<const char*>(&no_chunk));
+    return p[lo <= hi ? min(max(c, lo), hi) : 0];
   }
-  // Element e of a chunk; NaN as -infinity, -0 as 0.
-  static __device__ __forceinline__ float value(const uint4& c, int e) {
+  // The words asked for, or those of a chunk in part; what is outside the row is -infinity.
+  __device__ __forceinline__ uint4 get(int c, uint4 q) const {
+    if (c < lo || c > hi) {
+      uint32_t w[4] = {NONE, NONE, NONE, NONE};
+      if (c < chunks) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const int i = first(c) + e;
+          if (i < 0 || i >= V) continue;
+          if constexpr (F32) {
+            w[e] = reinterpret_cast<const uint32_t*>(at)[int64_t(c) * E + e];
+          } else {
+            const uint32_t h = reinterpret_cast<const uint16_t*>(at)[int64_t(c) * E + e];
+            w[e / 2] = e & 1 ? (w[e / 2] & 0xFFFFu) | h << 16 : (w[e / 2] & 0xFFFF0000u) | h;
+          }
+        }
+      }
+      q = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return q;
+  }
+  __device__ __forceinline__ uint4 load(int c) const { return get(c, ask(c)); }
+  // Element e of a chunk as it stands.
+  static __device__ __forceinline__ float raw(const uint4& c, int e) {
     const uint32_t w[4] = {c.x, c.y, c.z, c.w};
-    const float x = F32 ? __uint_as_float(w[e]) : __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
-    return x == x ? x + 0.0f : -__builtin_inff();
+    return F32 ? __uint_as_float(w[e]) : __uint_as_float(e & 1 ? w[e / 2] & 0xFFFF0000u : w[e / 2] << 16);
   }
 };
 
-// f(chunk, its words) for every chunk of the row, thread by thread; the wavefront
-// stays together (chunks behind the end are -infinity).
+// f(chunk, its words) for chunk groups [i0, i1) of wavefront `of`; the wavefront stays
+// together (chunks behind the end are -infinity).  Four chunks are on their way while
+// one is worked on.  The loop is not unrolled: a row is few iterations, and code that
+// runs once is bound by its own loads (with eight chunks in registers and their code in
+// a row, the maximum of 32000 logits took 18 us in place of 9).
 template <bool F32, typename Fn>
-__device__ __forceinline__ void over_row(const Row<F32>& r, Fn f) {
-  constexpr int AHEAD = 4;
-  for (int c0 = threadIdx.x; c0 - int(threadIdx.x & 63) < r.chunks; c0 += AHEAD * THREADS) {
-    uint4 w[AHEAD];
-#pragma unroll
-    for (int a = 0; a < AHEAD; ++a) w[a] = r.load(c0 + a * THREADS);
-#pragma unroll
-    for (int a = 0; a < AHEAD; ++a)
-      if (c0 + a * THREADS - int(threadIdx.x & 63) < r.chunks) f(c0 + a * THREADS, w[a]);
+__device__ __forceinline__ void over_chunks(const Row<F32>& row, int of, int i0, int i1, Fn f) {
+  auto at = [&](int i) { return row.chunk(of, i); };
+  uint4 a = row.ask(at(i0)), b = row.ask(at(i0 + 1)), c = row.ask(at(i0 + 2)), d = row.ask(at(i0 + 3));
+#pragma unroll 1
+  for (int i = i0; i < i1; ++i) {
+    const uint4 q = row.get(at(i), a);
+    a = b;
+    b = c;
+    c = d;
+    d = row.ask(at(i + 4));
+    f(at(i), q);
   }
+}
+// A logit as it counts: NaN as -infinity, -0 as 0.
+__device__ __forceinline__ float clean(float x) { return x == x ? x + 0.0f : -__builtin_inff(); }
+
+// f(x, index) for their elements as they stand, two at a time for the same reason;
+// only of chunks that have one of `from` or more in some lane.
+template <bool F32, typename Fn>
+__device__ __forceinline__ void over_part(const Row<F32>& row, int of, int i0, int i1, float from, Fn f) {
+  over_chunks(row, of, i0, i1, [&](int c, uint4 q) {
+    float m = row.raw(q, 0);
+#pragma unroll
+    for (int e = 1; e < Row<F32>::E; ++e) m = fmaxf(m, row.raw(q, e));  // (not NaN, if there is another)
+    if (!__any(m >= from)) return;
+    int i = row.first(c);
+#pragma unroll 1
+    for (int e = 0; e < Row<F32>::E; e += 2, i += 2) {
+      f(row.raw(q, 0), i);
+      f(row.raw(q, 1), i + 1);
+      q = F32 ? make_uint4(q.z, q.w, q.x, q.y) : make_uint4(q.y, q.z, q.w, q.x);
+    }
+  });
+}
+template <bool F32, typename Fn>
+__device__ __forceinline__ void over_row(const Row<F32>& row, float from, Fn f) {
+  over_part(row, uni(int(threadIdx.x >> 6)), 0, row.per, from, f);
+}
+
+// A token's weight in units of 2^-sh: 2^y, y = n + r with r in [-1/2, 1/2], by the
+// polynomial of degree 10 through 2^r at the 11 Chebyshev points (off by 3e-16 of
+// it at most); n + sh from the low bits of a sum with 2^52 and into the exponent by an
+// integer addition.  20 instructions; with the library's exponential and conversions
+// a pass took three times as long.
+__constant__ const double kPower[11] = {  // highest first
+    7.07258594926922339e-09, 1.02086902999583060e-07, 1.32154425879216893e-06,
+    1.52526572602008367e-05, 1.54035304417360499e-04, 1.33335582301649744e-03,
+    9.61812910760688825e-03, 5.55041086644477225e-02, 2.40226506959100972e-01,
+    6.93147180559949949e-01, 1.00000000000000000e+00};
+
+// a b + c with c in scalar registers, which the compiler copies to vector registers
+// first (11 pairs of them, for which others went to memory).
+__device__ __forceinline__ double fma_s(double a, double b, double c) {
+  double d;
+  asm("v_fma_f64 %0, %1, %2, %3" : "=v"(d) : "v"(a), "v"(b), "s"(c));
+  return d;
 }
 
 struct Weigh {
-  float top;       // the row's maximum
-  double inv_t;    // 1 / temperature
+  float top;       // the row's maximum, 0 where that is +infinity
+  bool endless;    // it is: tokens at it count as 0, others as -infinity
+  double per_t;    // log2(e) / temperature
+  double magic;    // 1.5 2^52 + sh
+  double lead;     // the power's first coefficient
   float bins;      // bins per unit of max - x
-  int sh;
+  float width;     // of a bin
 
-  // Monotone in x; weights in the last bin are 0.
-  __device__ __forceinline__ int bin(float x) const {
-    if (x == top) return 0;
-    const float z = (top - x) * bins;
-    return z < float(BINS - 1) ? int(z) : BINS - 1;
+  // A logit as it stands, for a row of +infinity's.
+  __device__ __forceinline__ float seen(float x) const {
+    return endless ? (x == __builtin_inff() ? 0.0f : -__builtin_inff()) : x;
   }
+  // Monotone in x; weights in the last bin are 0.
+  __device__ __forceinline__ int bin(float x) const { return int(fminf((top - x) * bins, float(BINS - 1))); }
+  // Values of bin b lie in [floor_of(b), ceil_of(b)]: a bin to spare for the roundings.
+  __device__ __forceinline__ float floor_of(int b) const { return uni(top - float(b + 2) * width); }
+  __device__ __forceinline__ float ceil_of(int b) const { return uni(b < 2 ? top : top - float(b - 1) * width); }
   __device__ __forceinline__ u64 operator()(float x) const {
-    if (x == top) return u64(1) << sh;
-    const double y = (double(x) - double(top)) * inv_t;
-    if (!(y > -0.6931472 * (sh + 2))) return 0;  // also x = -infinity
-    return u64(rint(ldexp(exp(y), sh)));
+    // (no less than 2^-1000, which rounds to 0 as -infinity and NaN have to)
+    const double y = fmax((double(x) - double(top)) * per_t, -1000.0), t = y + magic, r = y - (t - magic);
+    double v = fma_s(r, lead, kPower[1]);
+#pragma unroll
+    for (int i = 2; i < 11; ++i) v = fma_s(v, r, kPower[i]);
+    // 2^(n + sh) times it, rounded to an integer in the low bits
+    v = __hiloint2double(__double2hiint(v) + (__double2loint(t) << 20), __double2loint(v)) + 0x1p52;
+    return u64(uint32_t(__double2hiint(v)) & 0xFFFFFu) << 32 | uint32_t(__double2loint(v));
   }
 };
-
-// Sorts list[0, n) ascending, n <= CAP; what is behind up to the next power of two is overwritten.
-__device__ void sort_list(Lds& s, int n) {
-  int m = 64;
-  while (m < n) m <<= 1;
-  for (int i = n + threadIdx.x; i < m; i += THREADS) s.list[i] = ~u64(0);
-  __syncthreads();
-  for (int k = 2; k <= m; k <<= 1) {
-    for (int j = k >> 1; j > 0; j >>= 1) {
-      for (int t = threadIdx.x; t < m / 2; t += THREADS) {
-        const int i = (t & ~(j - 1)) << 1 | (t & (j - 1));
-        const u64 a = s.list[i], b = s.list[i + j];
-        if ((a > b) == ((i & k) == 0)) {
-          s.list[i] = b;
-          s.list[i + j] = a;
-        }
-      }
-      __syncthreads();
-    }
-  }
-}
 
 // A cut in the order of the tokens: the first `count` of them, or, where by_mass,
 // those before which the weights sum to less than `mass`.
@@ -209,21 +280,27 @@ struct Cut {
   u64 mass;
 };
 
-// Running sums of the histogram before each thread's bins 2 i and 2 i + 1.
+// Running sums of the histogram before each thread's bins 2 i and 2 i + 1; of the
+// weights where MASS, else 0.
 struct Before {
-  uint32_t c[2];
+  uint32_t c[2], all_c;
   u64 m[2];
 };
+template <bool MASS>
 __device__ __forceinline__ Before bins_before(Lds& s, u64& all) {
   const int b = 2 * threadIdx.x;
-  u64 nc;
-  const u64 m0 = s.mass[b], m1 = s.mass[b + 1];
   const uint32_t c0 = s.count[b], c1 = s.count[b + 1];
-  Before r;
-  r.m[0] = block_before(s, m0 + m1, all);
-  r.m[1] = r.m[0] + m0;
-  r.c[0] = uint32_t(block_before(s, u64(c0) + c1, nc));
+  u64 counted;
+  Before r{};
+  all = 0;
+  r.c[0] = uint32_t(block_before(s, u64(c0) + c1, counted));
+  r.all_c = uint32_t(counted);
   r.c[1] = r.c[0] + c0;
+  if constexpr (MASS) {
+    const u64 m0 = s.mass[b], m1 = s.mass[b + 1];
+    r.m[0] = block_before(s, m0 + m1, all);
+    r.m[1] = r.m[0] + m0;
+  }
   return r;
 }
 
@@ -236,27 +313,124 @@ __device__ __forceinline__ void clear_bins(Lds& s) {
   __syncthreads();
 }
 
-// The bin in which the cut lies; sums before it. Bins behind the last token's do not count.
+// The bin in which the cut lies, the one that its sums reach first; the sums before
+// it.  (A cut behind all tokens that are counted lies in the last one's bin.)
 __device__ __forceinline__ int bin_of_cut(Lds& s, const Before& r, const Cut& cut, uint32_t& c, u64& m) {
-  if (threadIdx.x == 0) s.found[0] = 0;
-  __syncthreads();
+  const uint32_t count = min(cut.count, r.all_c);
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int b = 2 * threadIdx.x + i;
-    const bool starts = s.count[b] > 0 && (cut.by_mass ? r.m[i] < cut.mass : r.c[i] < cut.count);
-    if (starts) atomicMax(&s.found[0], u64(b));
+    if (cut.by_mass ? r.m[i] < cut.mass && cut.mass <= r.m[i] + s.mass[b] : r.c[i] < count && count <= r.c[i] + s.count[b]) {
+      s.found[0] = b;
+      s.found[1] = r.c[i];
+      s.found[2] = r.m[i];
+    }
   }
   __syncthreads();
-  const int b = int(s.found[0]);
-  if (threadIdx.x == unsigned(b / 2)) {
-    s.found[1] = b & 1 ? r.c[1] : r.c[0];
-    s.found[2] = b & 1 ? r.m[1] : r.m[0];
-  }
-  __syncthreads();
-  c = uint32_t(s.found[1]);
-  m = s.found[2];
+  c = uni(uint32_t(s.found[1]));
+  m = uni(s.found[2]);
+  const int b = uni(int(s.found[0]));
   __syncthreads();
   return b;
+}
+
+// The wavefront in whose sum `at` (below the total) falls; left: at less the sums before it.
+__device__ __forceinline__ int pick(Lds& s, u64 sum, u64 at, u64& left) {
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) s.wave[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  int v = 0;
+  while (v < WAVES - 1 && s.wave[v] <= at) at -= s.wave[v++];
+  left = uni(at);
+  return uni(v);
+}
+
+// f(x, index) of `from` and larger go to the list as far as it goes; s.n counts them all.
+template <bool F32, typename Keep>
+__device__ __forceinline__ void gather(Lds& s, const Row<F32>& row, const Weigh& w, float from, Keep keep) {
+  __syncthreads();
+  if (threadIdx.x == 0) s.n = 0;
+  __syncthreads();
+  over_row(row, w.endless ? __builtin_inff() : from, [&](float x, int i) {
+    x = w.seen(x);
+    if (!(x >= from)) return;
+    x = clean(x);
+    if (!keep(x)) return;
+    const uint32_t at = atomicAdd(&s.n, 1u);
+    if (at < CAP) s.list[at] = place_of(x, i);
+  });
+  __syncthreads();
+}
+
+// The n numbers x of threads 0 .. n - 1 (n > 64), ~0 elsewhere, in ascending order.
+__device__ __forceinline__ u64 sorted(Lds& s, u64 x, uint32_t n) {
+  const uint32_t me = threadIdx.x;
+#pragma unroll 1
+  for (uint32_t k = 2; k < 2 * n; k <<= 1) {
+#pragma unroll 1
+    for (uint32_t j = k / 2; j > 0; j >>= 1) {
+      u64 y;
+      if (j < 64) {
+        y = shfl_xor(x, int(j));
+      } else {
+        __syncthreads();
+        s.list[me] = x;
+        __syncthreads();
+        y = s.list[me ^ j];
+      }
+      const bool low = ((me & j) == 0) == ((me & k) == 0);
+      x = (x < y) == low ? x : y;
+    }
+  }
+  return x;
+}
+
+// A gathered token: thread `part` of the `parts` neighbouring ones that have it.
+struct Token {
+  bool is;
+  int parts, part;
+  u64 place, mine;   // its weight
+  uint32_t rank;     // tokens before it in order
+  u64 before;        // their weights
+};
+// Sum over the threads of a token, in all of them.
+__device__ __forceinline__ u64 over_parts(u64 x, int parts) {
+  for (int d = 1; d < parts; d <<= 1) x += shfl_xor(x, d);
+  return x;
+}
+__device__ __forceinline__ Token rank_list(Lds& s, const Weigh& w, uint32_t n) {
+  Token t;
+  const uint32_t me = threadIdx.x;
+  if (n > FEW) {
+    t.parts = 1;
+    t.part = 0;
+    t.is = me < n;
+    t.place = t.is ? s.list[me] : ~u64(0);
+    t.place = sorted(s, t.place, n);
+    t.mine = t.is ? w(value_of(uint32_t(t.place >> 32))) : 0;
+    u64 all;
+    t.before = block_before(s, t.mine, all);
+    t.rank = me;
+    return t;
+  }
+  t.parts = n <= THREADS / 32 ? 32 : THREADS / FEW;
+  t.part = me & (t.parts - 1);
+  const uint32_t i = me / t.parts;
+  t.is = i < n;
+  if (me < n) s.weight[me] = w(value_of(uint32_t(s.list[me] >> 32)));
+  __syncthreads();
+  t.place = t.is ? s.list[i] : 0;
+  t.mine = t.is ? s.weight[i] : 0;
+  uint32_t rank = 0;
+  u64 before = 0;
+  for (uint32_t j = t.part; j < n; j += t.parts) {
+    const bool better = s.list[j] < t.place;
+    rank += better;
+    before += better ? s.weight[j] : 0;
+  }
+  t.before = over_parts(before, t.parts);
+  t.rank = uint32_t(over_parts(rank, t.parts));
+  return t;
 }
 
 // The cut among the tokens of bin b (n of them): place of the last one before it, and the sum of the weights there.
@@ -264,6 +438,17 @@ template <bool F32>
 __device__ u64 cut_bin(Lds& s, const Row<F32>& row, const Weigh& w, int b, uint32_t n, Cut cut, u64& mass) {
   uint32_t lo = 0, hi = ~0u;  // keys still in question
   mass = 0;
+  const float from = w.floor_of(b), to = w.ceil_of(b);
+  // f(x, its key) for the tokens in question
+  auto over_bin = [&](auto f) {
+    over_row(row, w.endless ? __builtin_inff() : from, [&](float x, int) {
+      x = w.seen(x);
+      if (!(x >= from && x <= to)) return;
+      x = clean(x);
+      const uint32_t k = key_of(x);
+      if (w.bin(x) == b && k >= lo && k <= hi) f(x, k);
+    });
+  };
   while (n > CAP) {
     __syncthreads();
     if (threadIdx.x == 0) {
@@ -272,144 +457,95 @@ __device__ u64 cut_bin(Lds& s, const Row<F32>& row, const Weigh& w, int b, uint3
     }
     __syncthreads();
     uint32_t a = ~0u, z = 0;
-    over_row(row, [&](int, const uint4& c) {
-#pragma unroll
-      for (int e = 0; e < Row<F32>::E; ++e) {
-        const float x = row.value(c, e);
-        const uint32_t k = key_of(x);
-        if (w.bin(x) == b && k >= lo && k <= hi) {
-          a = min(a, k);
-          z = max(z, k);
-        }
-      }
+    over_bin([&](float, uint32_t k) {
+      a = min(a, k);
+      z = max(z, k);
     });
     atomicMin(&s.lo, a);
     atomicMax(&s.hi, z);
     __syncthreads();
-    lo = s.lo;
-    hi = s.hi;
+    lo = uni(s.lo);
+    hi = uni(s.hi);
     if (lo == hi) break;
     clear_bins(s);
-    const u64 span = u64(hi) - lo + 1;
-    auto sub = [&](uint32_t k) { return int((u64(k - lo) * BINS) / span); };
-    over_row(row, [&](int, const uint4& c) {
-#pragma unroll
-      for (int e = 0; e < Row<F32>::E; ++e) {
-        const float x = row.value(c, e);
-        const uint32_t k = key_of(x);
-        if (w.bin(x) == b && k >= lo && k <= hi) {
-          atomicAdd(&s.count[sub(k)], 1u);
-          atomicAdd(&s.mass[sub(k)], w(x));
-        }
-      }
+    const int drop = std::max(0, 32 - __builtin_clz(hi - lo) - 11);  // (hi - lo) >> drop is below BINS
+    over_bin([&](float x, uint32_t k) {
+      atomicAdd(&s.count[(k - lo) >> drop], 1u);
+      atomicAdd(&s.mass[(k - lo) >> drop], w(x));
     });
     __syncthreads();
     u64 all;
-    const Before r = bins_before(s, all);
+    const Before r = bins_before<true>(s, all);
     uint32_t c;
     u64 m;
     const int v = bin_of_cut(s, r, cut, c, m);
-    n = s.count[v];
+    n = uni(s.count[v]);
     cut.count -= cut.by_mass ? 0 : c;
     cut.mass -= cut.by_mass ? m : 0;
     mass += m;
-    // keys k with sub(k) == v
-    const u64 k0 = (u64(v) * span + BINS - 1) / BINS, k1 = (u64(v + 1) * span + BINS - 1) / BINS;
-    hi = uint32_t(lo + k1 - 1);
-    lo = uint32_t(lo + k0);
+    hi = lo + uint32_t(((u64(v) + 1) << drop) - 1);
+    lo += uint32_t(v) << drop;
   }
-  __syncthreads();
   if (n > CAP) {  // one value: the first r of them by index
     const u64 one = w(value_of(lo));
     u64 r = cut.by_mass ? (one ? (cut.mass + one - 1) / one : n) : cut.count;
     r = r < n ? r : n;
     mass += r * one;
     if (r == n) return ~u64(0);
-    // how many lie in each run of indices
-    const int per = (row.chunks + RUNS - 1) / RUNS;
-    for (int i = threadIdx.x; i < RUNS; i += THREADS) s.count[i] = 0;
-    __syncthreads();
-    over_row(row, [&](int c, const uint4& q) {
-      uint32_t k = 0;
-#pragma unroll
-      for (int e = 0; e < Row<F32>::E; ++e) k += key_of(row.value(q, e)) == lo;
-      if (k && c < row.chunks) atomicAdd(&s.count[c / per], k);
-    });
-    __syncthreads();
-    u64 all;
-    const u64 mine = s.count[threadIdx.x], before = block_before(s, mine, all);
-    if (before < r && r <= before + mine) {  // one thread: r >= 1
-      u64 left = r - before;
-      u64 at = 0;
-      for (int c = threadIdx.x * per; c < row.chunks && left; ++c) {
-        const uint4 q = row.load(c);
-#pragma unroll
-        for (int e = 0; e < Row<F32>::E; ++e)
-          if (left && key_of(row.value(q, e)) == lo) {
-            --left;
-            at = u64(row.first(c) + e);
-          }
+    // how many lie in each wavefront's share of the indices, then in each of its chunk groups
+    const float only = value_of(lo);
+    auto same = [&](float x) { return clean(w.seen(x)) == only; };
+    const float any = -__builtin_inff();
+    u64 mine = 0;
+    over_row(row, any, [&](float x, int) { mine += same(x); });
+    const int wave = pick(s, wave_sum(mine), r - 1, r);  // r: what is left, counted from 0
+    for (int i = 0; i < row.per && int(threadIdx.x >> 6) == wave; ++i) {
+      u64 here = 0;
+      over_part(row, wave, i, i + 1, any, [&](float x, int) { here += same(x); });
+      const u64 upto = wave_upto(here), end = wave_sum(here);
+      if (r >= end) {
+        r -= end;
+        continue;
       }
-      s.found[3] = u64(lo) << 32 | at;
+      u64 at = upto - here;
+      over_part(row, wave, i, i + 1, any, [&](float x, int j) {
+        if (same(x) && at++ == r) s.found[3] = place_of(only, j);
+      });
+      break;
     }
     __syncthreads();
     return s.found[3];
   }
-  if (threadIdx.x == 0) s.n = 0;
-  __syncthreads();
-  over_row(row, [&](int c, const uint4& q) {
-#pragma unroll
-    for (int e = 0; e < Row<F32>::E; ++e) {
-      const float x = row.value(q, e);
-      const uint32_t k = key_of(x);
-      const int i = row.first(c) + e;
-      if (i >= 0 && i < row.V && w.bin(x) == b && k >= lo && k <= hi) s.list[atomicAdd(&s.n, 1u) & (CAP - 1)] = u64(k) << 32 | uint32_t(i);
-    }
+  gather(s, row, w, from, [&](float x) {
+    const uint32_t k = key_of(x);
+    return x <= to && w.bin(x) == b && k >= lo && k <= hi;
   });
-  __syncthreads();
-  sort_list(s, n);
-  u64 v[CAP / THREADS], sum = 0, all;
-#pragma unroll
-  for (int i = 0; i < CAP / THREADS; ++i) {
-    const uint32_t at = threadIdx.x * (CAP / THREADS) + i;
-    v[i] = at < n ? w(value_of(uint32_t(s.list[at] >> 32))) : 0;
-    sum += v[i];
-  }
-  u64 before = block_before(s, sum, all);
-  if (threadIdx.x == 0) s.found[0] = s.found[1] = 0;
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < CAP / THREADS; ++i) {
-    const uint32_t at = threadIdx.x * (CAP / THREADS) + i;
-    if (at < n && (cut.by_mass ? before < cut.mass : at < cut.count)) {
-      atomicMax(&s.found[0], u64(at) + 1);
-      atomicMax(&s.found[1], before + v[i]);
-    }
-    before += v[i];
+  if (threadIdx.x < 2) s.found[threadIdx.x] = 0;
+  const Token t = rank_list(s, w, n);
+  if (t.is && t.part == 0 && (cut.by_mass ? t.before < cut.mass : t.rank < cut.count)) {
+    atomicMax(&s.found[0], t.place);
+    atomicMax(&s.found[1], t.before + t.mine);
   }
   __syncthreads();
-  const u64 kept = s.found[0];
   mass += s.found[1];
-  return kept ? s.list[kept - 1] : 0;
+  return s.found[0];
 }
 
 // Counts and sums of weights per bin, and the sums before each thread's bins.
 template <bool F32>
 __device__ __forceinline__ Before histogram(Lds& s, const Row<F32>& row, const Weigh& w, u64& total) {
   clear_bins(s);
-  over_row(row, [&](int, const uint4& q) {
-#pragma unroll
-    for (int e = 0; e < Row<F32>::E; ++e) {
-      const float x = row.value(q, e);
-      const int b = w.bin(x);
-      if (b < BINS - 1) {  // not what is outside the row
-        atomicAdd(&s.count[b], 1u);
-        atomicAdd(&s.mass[b], w(x));
-      }
-    }
+  const float from = w.floor_of(BINS - 2);  // the last bin's tokens, and what is outside the row, have no weight
+  over_row(row, w.endless ? __builtin_inff() : from, [&](float x, int) {
+    x = w.seen(x);
+    if (!(x >= from)) return;
+    const int b = w.bin(x);
+    if (b == BINS - 1) return;
+    atomicAdd(&s.count[b], 1u);
+    atomicAdd(&s.mass[b], w(x));
   });
   __syncthreads();
-  return bins_before(s, total);
+  return bins_before<true>(s, total);
 }
 
 // floor(u total) for u in [0, 1); the last unit from 1 on.
@@ -426,202 +562,206 @@ __device__ __forceinline__ u64 border_of(float p, u64 total) {
   return hi + (lo != 0);
 }
 
+// The answer from the gathered tokens, if they are not too many and hold all that
+// stays.  total: the weights' sum over the row where top-k is off.
+template <typename Answer>
+__device__ __forceinline__ bool answer_of_list(Lds& s, const Weigh& w, uint32_t k, float top_p, u64 least, u64 total,
+                                               float u, Answer answer) {
+  const uint32_t n = uni(s.n);
+  if (n > CAP) return false;
+  if (threadIdx.x == 0) s.found[0] = 0;
+  const Token t = rank_list(s, w, n);
+  const bool first = t.is && t.part == 0;
+  if (first && (!k || t.rank < k)) atomicMax(&s.found[0], t.before + t.mine);
+  __syncthreads();
+  const u64 held = s.found[0], border = top_p < 1.0f ? border_of(top_p, k ? held : total) : ~u64(0);
+  if (top_p < 1.0f && border > held) return false;
+  const bool stays = t.is && (!k || t.rank < k) && t.before < border && t.mine >= least;
+  u64 place = t.place, mine = stays ? t.mine : 0, upto = 0, sum = 0;
+  if (n > FEW) {  // by index, what does not stay behind
+    place = sorted(s, stays ? place << 32 | place >> 32 : ~u64(0), n);
+    mine = place == ~u64(0) ? 0 : w(value_of(uint32_t(place)));
+    upto = block_before(s, mine, sum);
+    place >>= 32;
+  } else {
+    if (first) s.weight[threadIdx.x / t.parts] = mine;
+    __syncthreads();
+    for (uint32_t j = t.part; j < n; j += t.parts) {
+      const u64 v = s.weight[j];
+      sum += v;
+      upto += uint32_t(s.list[j]) < uint32_t(place) ? v : 0;
+    }
+    upto = over_parts(upto, t.parts);
+    sum = over_parts(sum, t.parts);
+  }
+  const u64 target = part_of(u, sum);
+  if (t.part == 0 && upto <= target && target < upto + mine) answer(int(uint32_t(place)), float(double(mine) / double(sum)));
+  return true;
+}
+
 template <bool F32>
 __global__ __launch_bounds__(THREADS) void sample_kernel(SampleLaunch p) {
   __shared__ Lds s;
   const int64_t t = blockIdx.x;
   const Row<F32> row(p.x, t * p.ld, p.V);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = uni(int(threadIdx.x >> 6));
 
-  u64 best = ~u64(0);
-  over_row(row, [&](int c, const uint4& q) {
+  // the lane's best value and the first chunk that has it
+  float own = -__builtin_inff();
+  int own_at = 0;
+  over_chunks(row, wave, 0, row.per, [&](int c, const uint4& q) {
+    float m = row.raw(q, 0);
 #pragma unroll
-    for (int e = 0; e < Row<F32>::E; ++e) {
-      const float x = row.value(q, e);
-      const u64 at = place_of(x, row.first(c) + e);
-      best = x > -__builtin_inff() && at < best ? at : best;
-    }
+    for (int e = 1; e < Row<F32>::E; ++e) m = fmaxf(m, row.raw(q, e));  // (not NaN, if there is another)
+    own_at = m > own ? c : own_at;
+    own = m > own ? m : own;
   });
+  float top = own;
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) best = min(best, shfl_xor(best, d));
-  if (lane == 0) s.wave[wave] = best;
+  for (int d = 1; d < 64; d <<= 1) top = fmaxf(top, __shfl_xor(top, d));
+  if (lane == 0) s.top[wave] = top;
   __syncthreads();
 #pragma unroll
-  for (int v = 0; v < WAVES; ++v) best = min(best, s.wave[v]);
+  for (int v = 0; v < WAVES; ++v) top = fmaxf(top, s.top[v]);
+  top = uni(top + 0.0f);
   auto answer = [&](int token, float prob) {
     p.token[t] = token;
     if (p.prob) p.prob[t] = prob;
   };
   const float temp = p.temperature ? p.temperature[t] : 1.0f;
-  if (best == ~u64(0) || !(temp > 0.0f)) {
-    if (threadIdx.x == 0) answer(best == ~u64(0) ? -1 : int(uint32_t(best)), best == ~u64(0) ? 0.0f : 1.0f);
+  if (top == -__builtin_inff()) {
+    if (threadIdx.x == 0) answer(-1, 0.0f);
+    return;
+  }
+  if (!(temp > 0.0f)) {
+    if (threadIdx.x == 0) s.n = ~0u;
+    __syncthreads();
+    if (own == top) atomicMin(&s.n, uint32_t(own_at));
+    __syncthreads();
+    if (own != top || s.n != uint32_t(own_at)) return;
+    const uint4 q = row.load(own_at);
+#pragma unroll
+    for (int e = Row<F32>::E - 1; e >= 0; --e) own_at = row.raw(q, e) == top ? row.first(int(s.n)) + e : own_at;
+    answer(own_at, 1.0f);
     return;
   }
   Weigh w;
-  w.top = value_of(uint32_t(best >> 32));
-  w.inv_t = 1.0 / double(temp);
-  w.sh = p.sh;
+  w.endless = top == __builtin_inff();
+  w.top = w.endless ? 0.0f : top;
+  w.lead = kPower[0];
+  w.magic = 0x1.8p52 + double(p.sh);
+  w.per_t = uni(1.4426950408889634 / double(temp));
   // the last bin begins at (sh + 1.98) ln 2, where weights round to 0
-  w.bins = fminf(float(BINS) / (float(p.sh + 2) * 0.6931472f) / temp, 3e38f);
+  w.bins = uni(fminf(float(BINS) / (float(p.sh + 2) * 0.6931472f) / temp, 3e38f));
+  w.width = uni(1.0f / w.bins);
   const int k_in = p.top_k ? p.top_k[t] : 0;
   const uint32_t k = k_in > 0 && k_in < p.V ? uint32_t(k_in) : 0u;
   const float top_p = p.top_p ? p.top_p[t] : 1.0f;
   const float min_p = p.min_p ? p.min_p[t] : 0.0f;
-  const u64 least = min_p > 0.0f ? u64(ceil(ldexp(fmin(double(min_p), 1.0), p.sh))) : 0;
+  const u64 least = uni(min_p > 0.0f ? u64(ceil(ldexp(fmin(double(min_p), 1.0), p.sh))) : u64(0));
 
   int last_bin = BINS;     // tokens of bins below it are kept,
   u64 last = ~u64(0);      // of its own those up to this place
   if (k || top_p < 1.0f) {
-    u64 total;
-    Before r = histogram(s, row, w, total);
+    u64 total = 0, m0 = 0;
     uint32_t c0 = 0;
-    u64 m0 = 0;
-    int kb = BINS - 1, kb_of = 0;
-    u64 kept = total;  // of the top k
-    if (k) {
-      kb = bin_of_cut(s, r, Cut{false, k, 0}, c0, m0);
-      const uint32_t n = s.count[kb];
-      last_bin = kb_of = kb;
-      kept = m0 + s.mass[kb];
-      if (c0 + n <= k) kb = BINS - 1;  // whole bins, the rest has no weight or none is left
-    }
-    // everything up to the end of the cut's bin in LDS?
-    uint32_t cp = c0;
-    u64 mp;
-    const int end = k ? kb_of : bin_of_cut(s, r, Cut{true, 0, border_of(top_p, total)}, cp, mp);
-    {
-      const uint32_t upto = cp + s.count[end];
-      if (upto <= CAP) {
-        if (threadIdx.x == 0) s.n = 0;
+    // The k-th best of the lanes' best values is one that k tokens reach at least, and few more: with top-k they
+    // hold the answer, and no histogram of the row is needed.
+    if (k && k <= ENOUGH) {
+      clear_bins(s);
+      own = clean(w.seen(own));
+      const int b = w.bin(own);
+      if (b < BINS - 1) atomicAdd(&s.count[b], 1u);
+      if (threadIdx.x == 0) s.hi = 0;
+      __syncthreads();
+      const Before r = bins_before<false>(s, total);
+      if (r.all_c >= k) {
+        const int end = bin_of_cut(s, r, Cut{false, k, 0}, c0, m0);
+        if (b <= end) atomicMax(&s.hi, key_of(own));
         __syncthreads();
-        over_row(row, [&](int c, const uint4& q) {
-#pragma unroll
-          for (int e = 0; e < Row<F32>::E; ++e) {
-            const float x = row.value(q, e);
-            const int i = row.first(c) + e;
-            if (i >= 0 && i < row.V && w.bin(x) <= end) s.list[atomicAdd(&s.n, 1u) & (CAP - 1)] = place_of(x, i);
-          }
-        });
-        __syncthreads();
-        uint32_t n = upto;
-        sort_list(s, n);
-        if (k && k < n) n = k;
-        u64 v[CAP / THREADS], sum = 0, all;
-#pragma unroll
-        for (int i = 0; i < CAP / THREADS; ++i) {
-          const uint32_t at = threadIdx.x * (CAP / THREADS) + i;
-          v[i] = at < n ? w(value_of(uint32_t(s.list[at] >> 32))) : 0;
-          sum += v[i];
-        }
-        u64 before = block_before(s, sum, all);
-        if (!k) all = total;
-        const u64 border = top_p < 1.0f ? border_of(top_p, all) : ~u64(0);
-        if (threadIdx.x == 0) s.found[0] = 0;
-        __syncthreads();
-        uint32_t mine = 0;
-#pragma unroll
-        for (int i = 0; i < CAP / THREADS; ++i) {
-          const uint32_t at = threadIdx.x * (CAP / THREADS) + i;
-          if (at < n && before < border && v[i] >= least) mine = at + 1;
-          before += v[i];
-        }
-        if (mine) atomicMax(&s.found[0], u64(mine));
-        __syncthreads();
-        n = uint32_t(s.found[0]);
-        // by index: (index, key)
-        for (uint32_t i = threadIdx.x; i < n; i += THREADS) s.list[i] = s.list[i] << 32 | s.list[i] >> 32;
-        sort_list(s, n);
-        sum = 0;
-#pragma unroll
-        for (int i = 0; i < CAP / THREADS; ++i) {
-          const uint32_t at = threadIdx.x * (CAP / THREADS) + i;
-          v[i] = at < n ? w(value_of(uint32_t(s.list[at]))) : 0;
-          sum += v[i];
-        }
-        before = block_before(s, sum, all);
-        const u64 target = part_of(p.u[t], all);
-#pragma unroll
-        for (int i = 0; i < CAP / THREADS; ++i) {
-          const uint32_t at = threadIdx.x * (CAP / THREADS) + i;
-          if (before <= target && target < before + v[i])
-            answer(int(uint32_t(s.list[at] >> 32)), float(double(v[i]) / double(all)));
-          before += v[i];
-        }
-        return;
+        gather(s, row, w, uni(value_of(s.hi)), [](float) { return true; });
+        if (answer_of_list(s, w, k, top_p, least, total, p.u[t], answer)) return;
       }
     }
-    bool stale = false;  // the histogram was used for another
-    if (kb < BINS - 1) {
-      const uint32_t n = s.count[kb];
-      stale = n > CAP;
-      u64 m;
-      last = cut_bin(s, row, w, kb, n, Cut{false, k - c0, 0}, m);
-      kept = m0 + m;
+    Before r = histogram(s, row, w, total);
+    if (!k) {  // a nucleus of few tokens
+      const int end = bin_of_cut(s, r, Cut{true, 0, border_of(top_p, total)}, c0, m0);
+      if (c0 + s.count[end] <= CAP) {
+        gather(s, row, w, w.floor_of(end), [&](float x) { return w.bin(x) <= end; });
+        if (answer_of_list(s, w, k, top_p, least, total, p.u[t], answer)) return;
+      }
+    }
+    u64 kept = total;  // sum of the top k
+    if (k) {
+      const int end = bin_of_cut(s, r, Cut{false, k, 0}, c0, m0);
+      const uint32_t n = s.count[end];
+      kept = m0 + s.mass[end];
+      last_bin = end;
+      __syncthreads();
+      if (c0 + n > k) {
+        u64 m;
+        last = cut_bin(s, row, w, end, n, Cut{false, k - c0, 0}, m);
+        kept = m0 + m;
+        if (top_p < 1.0f && n > CAP) r = histogram(s, row, w, total);  // the bins were used
+      }
     }
     if (top_p < 1.0f) {
-      if (stale) r = histogram(s, row, w, total);
       const u64 border = border_of(top_p, kept);
-      const int pb = bin_of_cut(s, r, Cut{true, 0, border}, cp, mp);
       u64 m;
-      const u64 end = cut_bin(s, row, w, pb, s.count[pb], Cut{true, 0, border - mp}, m);
-      last = pb < last_bin ? end : min(last, end);
+      const int pb = bin_of_cut(s, r, Cut{true, 0, border}, c0, m0);
+      const u64 at = cut_bin(s, row, w, pb, s.count[pb], Cut{true, 0, border - m0}, m);
+      last = pb < last_bin ? at : min(last, at);
       last_bin = pb;
     }
   }
 
-  // sums of the kept weights per run of indices
-  const int pieces = (row.chunks + 63) / 64;  // of a wavefront's chunks
-  const int per = (pieces + RUNS - 1) / RUNS;
+  // the indices in whose share of the sum the target falls: a wavefront's, a few of its chunk groups, one
+  last = uni(last);
+  last_bin = uni(last_bin);
+  const float from = last_bin < BINS ? w.floor_of(last_bin) : -__builtin_inff();
+  const float chunks_from = w.endless ? __builtin_inff() : from;
   auto weight = [&](float x, int i) -> u64 {
-    if (i < 0 || i >= row.V) return 0;
+    x = w.seen(x);
+    bool stays = true;
+    if (last_bin < BINS) {
+      const int b = w.bin(x);
+      stays = x >= from && b <= last_bin;
+      if (__any(stays && b == last_bin)) stays = stays && (b < last_bin || place_of(clean(x), i) <= last);
+      if (!__any(stays)) return 0;
+    }
     const u64 v = w(x);
-    const int b = w.bin(x);
-    return v >= least && (b < last_bin || (b == last_bin && place_of(x, i) <= last)) ? v : 0;
+    return stays && v >= least ? v : 0;
   };
-  __syncthreads();
-  for (int i = threadIdx.x; i < RUNS; i += THREADS) s.mass[i] = 0;
-  __syncthreads();
-  over_row(row, [&](int c, const uint4& q) {
+  u64 all = 0, left = 0;
+  int of = 0, at0 = 0, n = WAVES * row.per;  // chunk groups at0 .. at0 + n of wavefront `of` (first: of all)
+  for (bool first = true; first || n > 1; first = false) {
+    const int each = first ? row.per : (n + WAVES - 1) / WAVES;
+    const int i0 = first ? 0 : at0 + std::min(wave * each, n), i1 = first ? row.per : at0 + std::min((wave + 1) * each, n);
     u64 sum = 0;
-#pragma unroll
-    for (int e = 0; e < Row<F32>::E; ++e) sum += weight(row.value(q, e), row.first(c) + e);
+    over_part(row, first ? wave : of, i0, i1, chunks_from, [&](float x, int i) { sum += weight(x, i); });
     sum = wave_sum(sum);
-    if (lane == 0 && sum) atomicAdd(&s.mass[c / 64 / per], sum);
-  });
-  __syncthreads();
-  u64 all;
-  const u64 mine = s.mass[threadIdx.x], before = block_before(s, mine, all);
-  const u64 target = part_of(p.u[t], all);
-  if (before <= target && target < before + mine) {
-    s.found[0] = threadIdx.x;
-    s.found[1] = target - before;
+    if (first) {
+      block_before(s, lane ? 0 : sum, all);
+      left = part_of(p.u[t], all);
+    }
+    const int v = pick(s, sum, left, left);
+    if (first) {
+      of = v;
+      n = row.per;
+    } else {
+      at0 += v * each;
+      n = std::min(n - v * each, each);
+    }
   }
-  __syncthreads();
   if (wave) return;
-  u64 left = s.found[1];
-  const int run = int(s.found[0]);
-  for (int piece = run * per; piece < run * per + per; ++piece) {
-    const int c = piece * 64 + lane;
-    const uint4 q = row.load(c);
-    u64 v[Row<F32>::E], sum = 0;
-#pragma unroll
-    for (int e = 0; e < Row<F32>::E; ++e) {
-      v[e] = weight(row.value(q, e), row.first(c) + e);
-      sum += v[e];
-    }
-    const u64 upto = wave_upto(sum), end = shfl(upto, 63);
-    if (left >= end) {
-      left -= end;
-      continue;
-    }
-    u64 at = upto - sum;
-#pragma unroll
-    for (int e = 0; e < Row<F32>::E; ++e) {
-      if (at <= left && left < at + v[e]) answer(row.first(c) + e, float(double(v[e]) / double(all)));
-      at += v[e];
-    }
-    return;
-  }
+  u64 mine = 0;
+  over_part(row, of, at0, at0 + 1, chunks_from, [&](float x, int i) { mine += weight(x, i); });
+  u64 at = wave_upto(mine) - mine;
+  over_part(row, of, at0, at0 + 1, chunks_from, [&](float x, int i) {
+    const u64 v = weight(x, i);
+    if (at <= left && left < at + v) answer(i, float(double(v) / double(all)));
+    at += v;
+  });
 }
 
 }  // namespace
@@ -631,7 +771,7 @@ size_t sample_ws(int64_t, int64_t) { return 0; }
 hipError_t launch_sample(SampleLaunch p, hipStream_t st) {
   p.sh = 62;
   for (int64_t v = 1; v < p.V; v <<= 1) --p.sh;
-  p.sh = std::min(p.sh, 52);
+  p.sh = std::min(p.sh, 51);  // weights below 2^52
   if (p.x_dtype == F32)
     sample_kernel<true><<<unsigned(p.T), THREADS, 0, st>>>(p);
   else

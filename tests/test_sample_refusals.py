@@ -54,9 +54,9 @@ def test_binding_refuses():
 
 
 def test_reference_weights_and_shift():
-    assert [shift(v) for v in (1, 2, 1024, 1025, 131072, 1 << 22)] == [52, 52, 52, 51, 45, 40]
-    w = weights(np.array([0.0, -np.log(2.0), -np.inf], np.float32), 1.0, 52)
-    assert w[0] == 1 << 52 and abs(w[1] - 2 ** 51) < 2 ** 29 and w[2] == 0
+    assert [shift(v) for v in (1, 2, 1024, 1025, 131072, 1 << 22)] == [51, 51, 51, 51, 45, 40]
+    w = weights(np.array([0.0, -np.log(2.0), -np.inf], np.float32), 1.0, 51)
+    assert w[0] == 1 << 51 and abs(w[1] - 2 ** 50) < 2 ** 29 and w[2] == 0
 
 
 def test_reference_filters_in_turn():
