@@ -151,24 +151,24 @@ struct Row {
   }
   // The words asked for, or those of a chunk in part; what is outside the row is -infinity.
   __device__ __forceinline__ uint4 get(int c, uint4 q) const {
-    if (c < lo || c > hi) {
-      uint32_t w[4] = {NONE, NONE, NONE, NONE};
-      if (c < chunks) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int i = first(c) + e;
-          if (i < 0 || i >= V) continue;
-          if constexpr (F32) {
-            w[e] = reinterpret_cast<const uint32_t*>(at)[int64_t(c) * E + e];
-          } else {
-            const uint32_t h = reinterpret_cast<const uint16_t*>(at)[int64_t(c) * E + e];
-            w[e / 2] = e & 1 ? (w[e / 2] & 0xFFFFu) | h << 16 : (w[e / 2] & 0xFFFF0000u) | h;
-          }
+    if (!__any(c < lo || c > hi)) return q;
+    uint4 part = make_uint4(NONE, NONE, NONE, NONE);
+    if (__any((c < lo || c > hi) && c < chunks)) {
+#pragma unroll 1
+      for (int e = 0; e < E; ++e) {  // moved in from behind
+        const int i = first(c) + e;
+        const bool in = i >= 0 && i < V;
+        if constexpr (F32) {
+          const uint32_t v = in ? reinterpret_cast<const uint32_t*>(at)[int64_t(c) * E + e] : NONE;
+          part = make_uint4(part.y, part.z, part.w, v);
+        } else {
+          const uint32_t v = in ? reinterpret_cast<const uint16_t*>(at)[int64_t(c) * E + e] : 0xFF80u;
+          part = make_uint4(part.x >> 16 | part.y << 16, part.y >> 16 | part.z << 16, part.z >> 16 | part.w << 16,
+                            part.w >> 16 | v << 16);
         }
       }
-      q = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    return q;
+    return c < lo || c > hi ? part : q;
   }
   __device__ __forceinline__ uint4 load(int c) const { return get(c, ask(c)); }
   // Element e of a chunk as it stands.
@@ -211,10 +211,10 @@ __device__ __forceinline__ void over_part(const Row<F32>& row, int of, int i0, i
     if (!__any(m >= from)) return;
     int i = row.first(c);
 #pragma unroll 1
-    for (int e = 0; e < Row<F32>::E; e += 2, i += 2) {
-      f(row.raw(q, 0), i);
-      f(row.raw(q, 1), i + 1);
-      q = F32 ? make_uint4(q.z, q.w, q.x, q.y) : make_uint4(q.y, q.z, q.w, q.x);
+    for (int h = 0; h < Row<F32>::E / 4; ++h, i += 4) {  // four at a time
+#pragma unroll
+      for (int e = 0; e < 4; ++e) f(row.raw(q, e), i + e);
+      q = make_uint4(q.z, q.w, q.z, q.w);
     }
   });
 }
@@ -729,8 +729,9 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleLaunch p) {
       if (__any(stays && b == last_bin)) stays = stays && (b < last_bin || place_of(clean(x), i) <= last);
       if (!__any(stays)) return 0;
     }
-    const u64 v = w(x);
-    return stays && v >= least ? v : 0;
+    u64 v = w(x);
+    if (least) v = v >= least ? v : 0;
+    return stays ? v : 0;
   };
   u64 all = 0, left = 0;
   int of = 0, at0 = 0, n = WAVES * row.per;  // chunk groups at0 .. at0 + n of wavefront `of` (first: of all)
