@@ -35,6 +35,7 @@
 #include "uq_device.h"
 #include "uq_kv.h"
 #include "uq_launch.h"
+#include "uq_tile.h"
 
 namespace uq {
 
@@ -634,10 +635,383 @@ __global__ __launch_bounds__(256, (kHeld<FMT, D, NG, NT>)) void attn_extend_kern
   }
 }
 
+// ---------------------------------------------------------------------------
+// many columns: tiles in LDS, read by four wavefronts of 32 columns each
+// ---------------------------------------------------------------------------
+constexpr int WIDE = 128;  // columns of a workgroup
+
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+__device__ __forceinline__ float max2(float x) {
+  const uint32_t u = __float_as_uint(x);
+  const auto a = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+
+// The codes of a thread's piece of a tile and their statistics, between their loads
+// and LDS: row threadIdx.x / 8 of 32, codes 16 q .. + 16 as they lie (q = threadIdx.x % 8).
+template <int FMT, int NG>
+struct Codes {
+  static constexpr int W = FMT == KV_U8 ? 4 : 2;  // words of 16 codes
+  uint32_t k[W], v[W], ks[NG == 1 ? 1 : 2], vs[NG];
+  bool is;
+
+  __device__ __forceinline__ void load(const KvCache& c, const uint64_t (&at)[2], const uint64_t (&st)[2],
+                                       const int (&nv)[2]) {
+    const int r = threadIdx.x >> 3, q = threadIdx.x & 7, t = r >> 4;
+    is = (r & 15) < nv[t];
+    const uint64_t o = at[t] + uint32_t(r & 15) * (FMT == KV_U8 ? 128u : 64u) + uint32_t(q) * (4 * W);
+    if constexpr (FMT == KV_U8) {
+      const uint4 a = *reinterpret_cast<const uint4*>(static_cast<const char*>(c.k) + o);
+      const uint4 b = *reinterpret_cast<const uint4*>(static_cast<const char*>(c.v) + o);
+      k[0] = a.x; k[1] = a.y; k[2] = a.z; k[3] = a.w;
+      v[0] = b.x; v[1] = b.y; v[2] = b.z; v[3] = b.w;
+    } else {
+      const uint2 a = *reinterpret_cast<const uint2*>(static_cast<const char*>(c.k) + o);
+      const uint2 b = *reinterpret_cast<const uint2*>(static_cast<const char*>(c.v) + o);
+      k[0] = a.x; k[1] = a.y;
+      v[0] = b.x; v[1] = b.y;
+    }
+    const uint32_t* kst = reinterpret_cast<const uint32_t*>(c.k_stat) + st[t] + (r & 15);
+    const uint32_t* vst = reinterpret_cast<const uint32_t*>(c.v_stat) + st[t] + (r & 15);
+    const uint32_t len = uint32_t(c.page_len);
+    if constexpr (NG == 1) {
+      ks[0] = kst[0];
+    } else {  // the piece's two runs of eight channels lie in groups 2 (q % 2) and the next
+      ks[0] = kst[(2 * (q & 1)) * len];
+      ks[1] = kst[(2 * (q & 1) + 1) * len];
+    }
+#pragma unroll
+    for (int e = 0; e < NG; ++e) vs[e] = vst[uint32_t(e) * len];
+  }
+
+  static __device__ __forceinline__ float code(const uint32_t (&w)[W], int i) {
+    return float(FMT == KV_U8 ? w[i / 4] >> (8 * (i & 3)) & 255u : w[i / 8] >> (4 * (i & 7)) & 15u);
+  }
+  // Two values as two bf16 terms each.
+  static __device__ __forceinline__ void terms(float a, float b, uint32_t& hi, uint32_t& lo) {
+    hi = pack_bf16x2(a, b);
+    lo = pack_bf16x2(a - __uint_as_float(hi << 16), b - __uint_as_float(hi & 0xFFFF0000u));
+  }
+  static __device__ __forceinline__ float value(uint32_t st, float c) {
+    return __builtin_fmaf(__uint_as_float(st << 16), c, __uint_as_float(st & 0xFFFF0000u));
+  }
+
+  // Into the tiles kh, kl, vh, vl of LDS; rows that do not exist are 0.
+  __device__ __forceinline__ void store(u32x4a* stage) const {
+    const int r = threadIdx.x >> 3, q = threadIdx.x & 7, rho = perm32(r);
+    u32x4a* row = stage + rho * 16;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {  // channels 32 cc + 8 (q / 2) .. + 8, cc = 2 (q % 2) + h
+      u32x4a hi, lo;
+      const uint32_t st = is ? ks[NG == 1 ? 0 : h] : 0u;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        // (4-bit codes of a run lie in the order 0 2 4 6 1 3 5 7)
+        const int a = 8 * h + (FMT == KV_U8 ? 2 * j : j), b = 8 * h + (FMT == KV_U8 ? 2 * j + 1 : j + 4);
+        uint32_t x, y;
+        terms(value(st, code(k, a)), value(st, code(k, b)), x, y);
+        hi[j] = x;
+        lo[j] = y;
+      }
+      const int chunk = (4 * (2 * (q & 1) + h) + (q >> 1)) ^ swz(rho);
+      row[chunk] = hi;
+      row[TILE16 + chunk] = lo;
+    }
+    uint32_t* vrow = reinterpret_cast<uint32_t*>(row + 2 * TILE16);
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {  // channels 16 b + 2 q and the next
+      uint32_t hi, lo;
+      const uint32_t st = is ? vs[b * NG / 8] : 0u;
+      terms(value(st, code(v, b)), value(st, code(v, b + 8)), hi, lo);
+      const int at = ((2 * b + (q >> 2)) ^ swz(rho)) * 4 + (q & 3);
+      vrow[at] = hi;
+      vrow[TILE16 * 4 + at] = lo;
+    }
+  }
+};
+
+// As attn_extend_kernel, for heads of 128 channels: a wavefront owns 32 columns and
+// walks all steps of the workgroup's share, whose keys and values lie in LDS as
+// bf16 tiles of 32 rows (uq_tile.h), copied a stage ahead.  Codes are made values on
+// the way, two bf16 terms each (off by 2^-18 of a value): both products then need
+// neither scales nor offsets, and the work of that is shared by 128 columns.
+template <int FMT, int NG>
+__global__ __launch_bounds__(256, 2) void attn_extend_wide_kernel(AttnExtendLaunch p, int target) {
+  constexpr bool CODES = FMT != KV_BF16;
+  constexpr int TERMS = CODES ? 2 : 1;              // of a key and of a value
+  constexpr int TILES = CODES ? 1 : 2;              // steps of a stage
+  constexpr int TILE = 2 * TERMS * TILE16;          // a step's keys and values
+  constexpr uint32_t ROW = FMT == KV_BF16 ? 256 : FMT == KV_U8 ? 128 : 64;
+  __shared__ u32x4a smem[2][TILES * TILE];
+  const KvCache& c = p.c;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const int G = p.H / c.H_kv;
+  const int64_t b = workgroup();
+  const int g = int(b % c.H_kv);
+  Unit unit;
+  if (!find<WIDE, false>(p, G, b / c.H_kv, target, unit)) return;
+  const int s = unit.s;
+  const Seq seq = seq_of(p, scalar(p.row_start, s), scalar(p.row_start, s + 1), scalar(p.lens, s));
+  const Work<WIDE> work{p, G};
+  const int tiles = work.tiles(seq), parts = std::max(1, (work.steps(seq) + unit.per - 1) / unit.per);
+  const int part = unit.at / tiles, tile = tiles - 1 - unit.at % tiles;  // the longest first
+  const int len = capped(p, seq.len);
+  const int base = seq.len < 0 ? -seq.m : std::max(seq.len - seq.m, -seq.m);
+  const bool tree = p.mask != nullptr;
+
+  // the lane's column, and what the workgroup's and the wavefront's see
+  const int64_t idx = int64_t(tile) * WIDE + 32 * wave + (lane & 31);
+  const int j = int(idx / G), head = g * G + int(idx % G);
+  const int64_t row = j < seq.m && int64_t(seq.first) + j < p.T ? int64_t(seq.first) + j : -1;
+  auto limits = [&](int64_t r, int j, int& end, int& low) {
+    end = tree ? base : base + j + 1;
+    const int64_t at = r >= 0 && p.pos ? p.pos[r] : int64_t(base) + j;
+    low = p.window > 0 ? int(std::min<int64_t>(std::max<int64_t>(at - p.window + 1, 0), 0x7FFFFFFF)) : 0;
+  };
+  int end, low;
+  limits(row, j, end, low);
+  const int end_min = uniform(wave_min(row >= 0 ? end : 0x7FFFFFFF)), end_max = uniform(wave_max(row >= 0 ? end : 0));
+  const int low_min = uniform(wave_min(row >= 0 ? low : 0x7FFFFFFF)), low_max = uniform(wave_max(row >= 0 ? low : 0));
+  int all_end = 0, all_low = 0x7FFFFFFF;
+  {
+    __shared__ int ends[4], lows[4];
+    if (lane == 0) {
+      ends[wave] = end_max;
+      lows[wave] = low_min;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      all_end = std::max(all_end, ends[w]);
+      all_low = std::min(all_low, lows[w]);
+    }
+    all_end = uniform(all_end);
+    all_low = uniform(all_low);
+  }
+  const int hi = tree ? len : std::min(len, all_end);
+  const int lo = std::max(0, tree ? std::min(all_low, base) : all_low);
+  const int n_sink = p.window > 0 ? (std::min(p.sinks, std::max(hi, 0)) + STEP - 1) / STEP : 0;
+  const int u_lo = std::max(lo / STEP, n_sink);
+  const int n_steps = n_sink + std::max(0, (std::max(hi, 0) + STEP - 1) / STEP - u_lo);
+  const int i0 = int(int64_t(n_steps) * part / parts), i1 = int(int64_t(n_steps) * (part + 1) / parts);
+  auto step_at = [&](int i) { return i < n_sink ? i : u_lo + (i - n_sink); };
+
+  const uint32_t page_bytes = uint32_t(c.H_kv) * uint32_t(c.page_len) * ROW;
+  const uint32_t page_stats = uint32_t(c.H_kv) * uint32_t(c.page_len) * NG;
+  const uint32_t head_bytes = uint32_t(g) * uint32_t(c.page_len) * ROW, head_stats = uint32_t(g) * uint32_t(c.page_len) * NG;
+  const int32_t* pages = c.pages + int64_t(s) * c.max_pages;
+  // where a step's two halves of 16 positions lie (of those on no page: page 0), and how many of them exist
+  auto look_up = [&](int i, uint64_t (&at)[2], uint64_t (&st)[2], int (&nv)[2]) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int pos = step_at(i) * STEP + 16 * t;
+      const int page = i < i1 && pos < len ? scalar(pages, pos >> c.log_page) : -1;
+      const bool is = page >= 0 && page < c.n_pages;
+      const uint32_t pg = is ? uint32_t(page) : 0u, r = is ? uint32_t(pos & (c.page_len - 1)) : 0u;
+      nv[t] = is ? std::min(16, len - pos) : 0;
+      at[t] = uint64_t(pg) * page_bytes + (head_bytes + r * ROW);
+      st[t] = uint64_t(pg) * page_stats + (head_stats + r);
+    }
+  };
+
+  // queries, a negative scale's sign on them
+  bf16x8a qf[8];
+  {
+    const uint16_t* q = p.Q + (row < 0 ? 0 : row) * p.ld_q + int64_t(head) * D + 8 * (lane >> 5);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      u32x4a v = row >= 0 ? *reinterpret_cast<const u32x4a*>(q + 16 * k) : u32x4a{0, 0, 0, 0};
+      if (p.scale < 0.0f) v ^= 0x80008000u;
+      qf[k] = __builtin_bit_cast(bf16x8a, v);
+    }
+  }
+  const float cl = fabsf(p.scale) * LOG2E;  // scores to exponents of 2
+
+  // a stage's copies: of a bf16 cache straight into LDS, two blocks of 64 slots of every tile a wavefront
+  int nv[TILES][2];
+  uint32_t off[2];
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int slot = (2 * wave + k) * 64 + lane, rho = slot >> 4;
+    off[k] = uint32_t(perm32(rho) & 15) * ROW + uint32_t(((slot & 15) ^ swz(rho)) * 16);
+  }
+  auto copy_stage = [&](int i, u32x4a* stage, int (&n)[TILES][2]) {
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+      uint64_t at[2], st[2];
+      look_up(i + t, at, st, n[t]);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const int blk = 2 * wave + k;  // rows of half blk / 4
+        copy16(static_cast<const char*>(c.k) + at[blk >> 2], off[k], stage + t * TILE + blk * 64);
+        copy16(static_cast<const char*>(c.v) + at[blk >> 2], off[k], stage + t * TILE + TILE16 + blk * 64);
+      }
+    }
+  };
+  Codes<CODES ? FMT : KV_U8, NG> codes;
+  int nv_next[TILES][2];
+  uint64_t at[2], st[2];
+
+  f32x16a o[4] = {zero16(), zero16(), zero16(), zero16()};
+  // weights count in 2^-24 against the running maximum (see attn_decode.hip): m is 24 above it
+  constexpr float DOWN = 24.0f;
+  float m = LOWEST, l = 0.0f;
+
+  // products of one step out of tile tk, nvt of whose positions exist
+  auto step = [&](const u32x4a* tk, int t0, const int (&nvt)[2]) {
+    const u32x4a* tv = tk + TERMS * TILE16;
+    f32x16a x = zero16();
+#pragma unroll
+    for (int term = 0; term < TERMS; ++term)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x = mfma(row_frag(tk + term * TILE16, k, lane), qf[k], x);
+    const bool cut = nvt[0] + nvt[1] < STEP || t0 + STEP > end_min || (t0 < low_max && t0 + STEP > p.sinks);
+    uint32_t seen = 0;  // bit r: slot r
+    if (cut) {
+      uint32_t drafts = 0;
+      if (tree && t0 + STEP > base && row >= 0) drafts = mask_bits(p.mask + row * p.words, p.words, t0 - base);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int in = slot_row(r, lane), at = t0 + in;
+        const bool ok = at < end ? (at >= low || (p.window > 0 && at < p.sinks)) : (at >= base && (drafts >> in & 1));
+        seen |= ok && (in & 15) < nvt[r >> 3] ? 1u << r : 0u;
+        x[r] = seen >> r & 1 ? x[r] : -__builtin_inff();
+      }
+    }
+    float mx = x[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, x[r]);
+    mx = max2(mx) * cl;
+    if (__any(mx > m - DOWN + SLACK)) {
+      const float m1 = fmaxf(m, mx + DOWN);
+      const float f = exp2a(m - m1);
+      m = m1;
+      l *= f;
+#pragma unroll
+      for (int db = 0; db < 4; ++db) o[db] *= f;
+    }
+    float w[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) w[r] = exp2a(__builtin_fmaf(x[r], cl, -m));
+    bool wild_values = false;
+    if (cut) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) w[r] = seen >> r & 1 ? w[r] : 0.0f;
+      // values that are not finite, which a weight of 0 does not take out of a product
+      bool any = false;
+      for (int k = 0; k < TILE16 / 64; ++k) {
+        const u32x4a v = tv[k * 64 + lane];
+        any |= wild(v.x) || wild(v.y) || wild(v.z) || wild(v.w);
+      }
+      wild_values = __any(any);
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sum += w[r];
+    l += sum;
+    if (wild_values) {
+      // one position after the other, those with a weight only
+#pragma unroll 1
+      for (int pos = 0; pos < STEP; ++pos) {
+        // held by lane half (pos / 8) % 2 in slot 8 (pos / 16) + pos % 8
+        float z = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (r == 8 * (pos >> 4) + (pos & 7)) z = __shfl(w[r], (lane & 31) + 32 * (pos >> 3 & 1));
+        z = float(__bf16(z));
+        const int rho = perm32(pos);
+        const uint16_t* vrow = reinterpret_cast<const uint16_t*>(tv + rho * 16);
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int ch = 32 * db + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+            const int at = ((ch >> 3) ^ swz(rho)) * 8 + (ch & 7);
+            float v = bf16_to_f32(vrow[at]);
+            if constexpr (CODES) v += bf16_to_f32(vrow[TILE16 * 8 + at]);
+            if (z != 0.0f) o[db][r] += z * v;
+          }
+      }
+      return;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const bf16x8a pb = pack_half(w, h);
+#pragma unroll
+      for (int term = 0; term < TERMS; ++term)
+#pragma unroll
+        for (int db = 0; db < 4; ++db) o[db] = mfma(col_frag(tv + term * TILE16, db, h, lane), pb, o[db]);
+    }
+  };
+
+  int cur = 0;
+  if constexpr (CODES) {
+    look_up(i0, at, st, nv[0]);
+    codes.load(c, at, st, nv[0]);
+    codes.store(smem[0]);
+    look_up(i0 + 1, at, st, nv_next[0]);
+    codes.load(c, at, st, nv_next[0]);
+    __syncthreads();
+  } else {
+    copy_stage(i0, smem[0], nv);
+  }
+  for (int i = i0; i < i1; i += TILES, cur ^= 1) {
+    if constexpr (CODES) {
+      step(smem[cur], step_at(i) * STEP, nv[0]);
+      nv[0][0] = nv_next[0][0];
+      nv[0][1] = nv_next[0][1];
+      codes.store(smem[cur ^ 1]);
+      look_up(i + 2, at, st, nv_next[0]);
+      codes.load(c, at, st, nv_next[0]);
+      __syncthreads();
+    } else {
+      vm_wait<0>();
+      lds_wait_barrier();
+      copy_stage(i + TILES, smem[cur ^ 1], nv_next);
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+        if (i + t < i1) step(smem[cur] + t * TILE, step_at(i + t) * STEP, nv[t]);
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) nv[t][k] = nv_next[t][k];
+    }
+  }
+  if constexpr (!CODES) vm_wait<0>();  // no copy is on its way when the workgroup ends
+
+  l += other_half(l);
+  if (row < 0) return;
+  if (parts == 1) {
+    const float inv = 1.0f / l;
+    uint16_t* out = p.O + row * p.ld_o + int64_t(head) * D;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4) {
+        const uint32_t a = pack_bf16x2(o[db][4 * g4] * inv, o[db][4 * g4 + 1] * inv);
+        const uint32_t e = pack_bf16x2(o[db][4 * g4 + 2] * inv, o[db][4 * g4 + 3] * inv);
+        // no weight at all: 0
+        *reinterpret_cast<u32x2a*>(out + 32 * db + 8 * g4 + 4 * (lane >> 5)) = l == 0.0f ? u32x2a{0, 0} : u32x2a{a, e};
+      }
+    if (lane < 32 && p.lse) p.lse[row * p.H + head] = l == 0.0f ? -__builtin_inff() : m + __builtin_amdgcn_logf(l);
+    return;
+  }
+  const int64_t slot = int64_t(unit.slot) + unit.at;
+  if (slot >= 2 * int64_t(target)) return;
+  float* out = part_of<WIDE, D>(p, slot, g, 32 * wave + (lane & 31));
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int g4 = 0; g4 < 4; ++g4)
+      *reinterpret_cast<float4*>(out + 4 + 32 * db + 8 * g4 + 4 * (lane >> 5)) =
+          make_float4(o[db][4 * g4], o[db][4 * g4 + 1], o[db][4 * g4 + 2], o[db][4 * g4 + 3]);
+  if (lane < 32) *reinterpret_cast<float2*>(out) = make_float2(m, l);
+}
+
 // Joins the shares of a tile's columns: D / 4 lanes a share of a column, PAR
 // shares of it at a time, four of each in flight; 256 / (PAR D / 4) columns.
 template <int D, int COLS, int PAR>
-__global__ __launch_bounds__(256) void attn_extend_join_kernel(AttnExtendLaunch p, int target) {
+__global__ __launch_bounds__(256) void attn_extend_join_kernel(AttnExtendLaunch p, int target, float back) {
   constexpr int LANES = D / 4, ROWS = 256 / LANES / PAR, GROUPS = COLS / ROWS;
   const int G = p.H / p.c.H_kv;
   const int64_t b = workgroup();
@@ -704,45 +1078,58 @@ __global__ __launch_bounds__(256) void attn_extend_join_kernel(AttnExtendLaunch 
   }
   if (!real) return;
   const int hd = g * G + int(idx % G);
-  const float inv = (p.c.format == KV_BF16 ? BF16_BACK : 1.0f) / t;
+  const float inv = back / t;
   *reinterpret_cast<uint2*>(p.O + r * p.ld_o + int64_t(hd) * D + 4 * lane) =
       t == 0.0f ? make_uint2(0u, 0u) : make_uint2(pack_bf16x2(a[0] * inv, a[1] * inv), pack_bf16x2(a[2] * inv, a[3] * inv));
   if (lane == 0 && p.lse) p.lse[r * p.H + hd] = t == 0.0f ? -__builtin_inff() : m + __builtin_amdgcn_logf(t);
 }
 
-// Column tiles of a workgroup, for the columns that a sequence has on average.
-int col_tiles(int64_t T, int64_t n_seq, int H, int H_kv) {
+// Columns of a workgroup, for those that a sequence has on average: 16, 32, and of heads of 128 channels WIDE.
+int columns_of(int64_t T, int64_t n_seq, int H, int H_kv, int d) {
   const int64_t cols = (T + n_seq - 1) / n_seq * (H / H_kv);
-  return cols <= 16 ? 1 : 2;
+  return cols <= 16 ? 16 : cols <= 32 || d != 128 ? 32 : WIDE;
 }
 // Tiles of one key/value head, if no row is padding.
-int64_t tiles_of(int64_t T, int H, int H_kv, int nt) { return T * (H / H_kv) / (16 * nt); }
+int64_t tiles_of(int64_t T, int H, int H_kv, int cols) { return T * (H / H_kv) / cols; }
 // Shares of one key/value head that are wanted (0: no tile is cut).
-int target_of(int64_t T, int64_t n_seq, int H, int H_kv, int64_t max_pages, int page_len) {
-  const int nt = col_tiles(T, n_seq, H, H_kv);
-  const int64_t want = 2 * CUS / H_kv;
-  if (max_pages * page_len <= MIN_STEPS * STEP || tiles_of(T, H, H_kv, nt) >= want) return 0;
+int target_of(int64_t T, int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len) {
+  const int cols = columns_of(T, n_seq, H, H_kv, d);
+  const int64_t want = std::max(1, 2 * CUS / H_kv);
+  if (max_pages * page_len <= MIN_STEPS * STEP || tiles_of(T, H, H_kv, cols) >= 4 * want) return 0;
   return int(want);
 }
 
-template <int FMT, int D, int NG, int NT>
-hipError_t launch_nt(const AttnExtendLaunch& p, hipStream_t st) {
-  const int H_kv = p.c.H_kv, target = target_of(p.T, p.c.n_seq, p.H, H_kv, p.c.max_pages, p.c.page_len);
-  const int64_t tiles = tiles_of(p.T, p.H, H_kv, NT) + std::min(p.T, p.c.n_seq);
-  attn_extend_kernel<FMT, D, NG, NT><<<grid_of((tiles + target) * H_kv), 256, 0, st>>>(p, target);
-  if (hipError_t e = hipGetLastError()) return e;
-  if (!target) return hipSuccess;
-  constexpr int COLS = 16 * NT, LANES = D / 4;
+template <int D, int COLS>
+hipError_t launch_join(const AttnExtendLaunch& p, int64_t tiles, int target, float back, hipStream_t st) {
+  constexpr int LANES = D / 4;
   if (p.T * p.H <= 2048)
-    attn_extend_join_kernel<D, COLS, 256 / LANES><<<grid_of(tiles * H_kv * COLS), 256, 0, st>>>(p, target);
+    attn_extend_join_kernel<D, COLS, 256 / LANES><<<grid_of(tiles * p.c.H_kv * COLS), 256, 0, st>>>(p, target, back);
   else
-    attn_extend_join_kernel<D, COLS, 1><<<grid_of(tiles * H_kv * COLS * LANES / 256), 256, 0, st>>>(p, target);
+    attn_extend_join_kernel<D, COLS, 1><<<grid_of(tiles * p.c.H_kv * COLS * LANES / 256), 256, 0, st>>>(p, target, back);
   return hipGetLastError();
 }
 
 template <int FMT, int D, int NG>
 hipError_t launch_form(const AttnExtendLaunch& p, hipStream_t st) {
-  return col_tiles(p.T, p.c.n_seq, p.H, p.c.H_kv) == 1 ? launch_nt<FMT, D, NG, 1>(p, st) : launch_nt<FMT, D, NG, 2>(p, st);
+  const int H_kv = p.c.H_kv, cols = columns_of(p.T, p.c.n_seq, p.H, H_kv, D);
+  const int target = target_of(p.T, p.c.n_seq, p.H, H_kv, D, p.c.max_pages, p.c.page_len);
+  const int64_t tiles = tiles_of(p.T, p.H, H_kv, cols) + std::min(p.T, p.c.n_seq);
+  const dim3 grid = grid_of((tiles + target) * H_kv);
+  const float back = FMT == KV_BF16 ? BF16_BACK : 1.0f;
+  if constexpr (D == 128) {
+    if (cols == WIDE) {
+      attn_extend_wide_kernel<FMT, NG><<<grid, 256, 0, st>>>(p, target);
+      if (hipError_t e = hipGetLastError()) return e;
+      return target ? launch_join<D, WIDE>(p, tiles, target, 1.0f, st) : hipSuccess;
+    }
+  }
+  if (cols == 16)
+    attn_extend_kernel<FMT, D, NG, 1><<<grid, 256, 0, st>>>(p, target);
+  else
+    attn_extend_kernel<FMT, D, NG, 2><<<grid, 256, 0, st>>>(p, target);
+  if (hipError_t e = hipGetLastError()) return e;
+  if (!target) return hipSuccess;
+  return cols == 16 ? launch_join<D, 16>(p, tiles, target, back, st) : launch_join<D, 32>(p, tiles, target, back, st);
 }
 
 template <int D>
@@ -756,8 +1143,8 @@ hipError_t launch_d(const AttnExtendLaunch& p, hipStream_t st) {
 }  // namespace
 
 size_t attn_extend_ws(int64_t T, int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len) {
-  const size_t target = size_t(target_of(T, n_seq, H, H_kv, max_pages, page_len));
-  return 2 * target * size_t(H_kv) * size_t(16 * col_tiles(T, n_seq, H, H_kv)) * size_t(d + 4);
+  const size_t target = size_t(target_of(T, n_seq, H, H_kv, d, max_pages, page_len));
+  return 2 * target * size_t(H_kv) * size_t(columns_of(T, n_seq, H, H_kv, d)) * size_t(d + 4);
 }
 
 hipError_t launch_attn_extend(const AttnExtendLaunch& p, hipStream_t st) {

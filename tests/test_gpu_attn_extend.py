@@ -67,9 +67,10 @@ def test_a_mask_word_too_few_hides_the_rest():
 @pytest.mark.parametrize("fmt,group", FORMS)
 @pytest.mark.parametrize("window,sinks", [(1, 0), (5, 1), (31, 4), (32, 0), (64, 40), (100, 33), (1000, 3), (1 << 30, 0),
                                           (2 ** 31 - 1, 2 ** 31 - 1)])
-def test_windows(fmt, group, window, sinks):
+@pytest.mark.parametrize("d,n_kv,grp", [(64, 2, 3), (128, 1, 9)])
+def test_windows(fmt, group, window, sinks, d, n_kv, grp):
     seqs = [(1, 200), (9, 140), (40, 40), (3, 300), (0, 3), (1, 1)]
-    rs, c, m, q, start, lens = case(seqs, 2, 3, 64, 16, fmt, group)
+    rs, c, m, q, start, lens = case(seqs, n_kv, grp, d, 16, fmt, group)
     X.check(c, m, q, start, lens, 0.125, window=window, sinks=sinks, what="rows")
     at = [ln - r + j for r, ln in seqs for j in range(r)]
     O, l = X.call(c, m, q, start, lens, 0.125, window=window, sinks=sinks)
@@ -100,10 +101,13 @@ def test_long_sequences_cut_into_shares(fmt, group, d, n_kv, grp, rows):
 
 
 @pytest.mark.parametrize("fmt,group", FORMS)
-def test_many_tiles(fmt, group):
-    """More tiles than are cut: a prompt's part of many rows."""
-    rs, c, m, q, start, lens = case([(300, 420), (211, 211)], 2, 8, 64, 32, fmt, group)
+@pytest.mark.parametrize("d", [64, 128])
+def test_many_tiles(fmt, group, d):
+    """A prompt's part of many rows; with pages of 16 that lie apart, holes among them."""
+    rs, c, m, q, start, lens = case([(300, 420), (211, 211)], 2, 8, d, 16, fmt, group)
     X.check(c, m, q, start, lens, 0.125)
+    c.table[0, 3] = c.table[0, 20] = c.table[1, 0] = -1
+    X.check(c, on_device(c), q, start, lens, 0.125, what="holes")
 
 
 def test_many_sequences():
@@ -144,7 +148,7 @@ def test_pages_that_are_none_and_lengths_out_of_range(fmt, group):
 
 
 @pytest.mark.parametrize("fmt,group", FORMS)
-@pytest.mark.parametrize("d,grp", [(64, 1), (64, 6), (128, 2)])
+@pytest.mark.parametrize("d,grp", [(64, 1), (64, 6), (128, 2), (128, 5)])
 def test_what_is_not_seen_may_be_anything(fmt, group, d, grp):
     """NaN and infinities in drafts of other branches, behind a window and behind a row's own place, in keys, values,
     scales and offsets: rows that see them may come out as they like, the others as without."""
@@ -197,11 +201,12 @@ def test_infinite_values_that_are_seen(d):
         assert np.all(np.isfinite(np.delete(o, ch, -1)))
 
 
-def test_largest_values_of_a_bf16_cache():
+@pytest.mark.parametrize("d", [64, 128])
+def test_largest_values_of_a_bf16_cache(d):
     rs = np.random.default_rng(1)
-    c = filled(rs, [600], 1, 64, 16, "bf16", 0)
+    c = filled(rs, [600], 1, d, 16, "bf16", 0)
     c.v[...] = np.where(c.v == 0x7FC1, c.v, 0x7F7F)  # the largest finite number
-    q = rounded(rs, 40, 2, 64)
+    q = rounded(rs, 40, 2, d)
     O, _ = X.call(c, on_device(c), q, X.starts([40]), [600], 0.125)
     assert np.all(O.float().cpu().numpy() == np.float32(KV.from_bf16(np.uint16(0x7F7F))))
 
@@ -224,9 +229,10 @@ def test_row_starts_out_of_range_are_not_followed():
 @pytest.mark.parametrize("fmt,group", [("bf16", 0), ("u4", 32)])
 @pytest.mark.parametrize("scale", [-0.125, 0.0, 3.0])
 def test_scales(fmt, group, scale):
-    rs, c, m, q, start, lens = case(SEQS, 2, 2, 64, 16, fmt, group)
-    X.check(c, m, q, start, lens, scale)
-    X.check(c, m, q, start, lens, scale, window=9, sinks=2)
+    for d, grp in ((64, 2), (128, 9)):
+        rs, c, m, q, start, lens = case(SEQS, 2, grp, d, 16, fmt, group)
+        X.check(c, m, q, start, lens, scale)
+        X.check(c, m, q, start, lens, scale, window=9, sinks=2)
 
 
 @pytest.mark.parametrize("fmt,group", [("bf16", 0), ("u8", 32)])
