@@ -4,16 +4,21 @@
 //
 // Split.  The rows of a sequence and the query heads of a key/value head are the
 // columns of one product, m (H / H_kv) of them in the order row, head.  A
-// workgroup of four wavefronts takes 16 NT columns (a tile) and a share of the
-// positions that its rows see, its wavefronts every fourth step of 32 positions.
-// Where the tiles are fewer than the workgroups that the GPU holds, the sequences'
-// positions are cut into shares of equal length and attn_extend_join_kernel joins
-// them; workgroups find their place by adding up all sequences' tiles and steps.
+// workgroup of four wavefronts takes some columns (a tile) and all positions that
+// its rows see, or a share of them.  Where the tiles are fewer than the GPU holds
+// workgroups, and where some are much longer than others, they are cut into shares
+// of about equal length, and attn_extend_join_kernel joins those; workgroups find
+// their place by adding up all sequences' tiles and steps of 32 positions.
 //
-// One step is that of the single-token attention (attn_decode.hip): S^T = K Q^T and
-// O^T += V^T P^T with the heads as columns, K and V straight from the cache into
-// registers, codes fed as they are.  Each key and value operand meets NT column
-// tiles, which shares out its load and its preparation.
+// Few columns (attn_extend_kernel: 16 or 32).  One step is that of the single-token
+// attention (attn_decode.hip): S^T = K Q^T and O^T += V^T P^T with the heads as
+// columns, K and V straight from the cache into registers, codes fed as they are;
+// a workgroup's wavefronts take every fourth step.  Bound by the loads: 64 x 8 rows
+// over 8192 positions of 8 heads in bf16 (2.2 GB) in 382 us, 5.7 TB/s.
+// Many columns (attn_extend_wide_kernel: 128).  Tiles of keys and values in LDS, read
+// by four wavefronts with 32 columns each.  Bound by the products and the weights
+// between them: 2 x 2048 rows behind 6144 positions, 32 heads over 8, in 640 us,
+// 750 TFLOP/s.  columns_of says which is taken where.
 //
 // What is seen.  A step in which some column does not see all 32 positions (its
 // own end, a window's edge, a tree's drafts, the end of the sequence or a missing
@@ -21,10 +26,10 @@
 // of a value or a scale that is not finite where the weight is 0 (its products
 // are 0, not NaN).  All other steps, nearly all of a long history, have no masks.
 //
-// Precision.  As in attn_decode.hip, but that with more than one column tile a
-// weight enters the second product as one bf16 value, rounded to nearest (2^-9 of it
-// at most, either way), as in the block's causal attention: a second term would
-// double that product, which bounds such calls.
+// Precision.  With 16 columns as in attn_decode.hip.  With more a weight enters the
+// second product as one bf16 value, rounded to nearest (2^-9 of it at most, either
+// way), as in the block's causal attention: a second term would double that product,
+// which bounds such calls.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -77,10 +82,19 @@ struct Unit {
   int s;          // sequence
   int at;         // of the sequence's units
   int slot;       // of the workspace, where the sequence is cut
-  int per;        // steps of a share
+  int64_t total;  // steps of all tiles
+  double rate;    // shares a step
+  int target;
+  // Shares of a tile of so many steps: floor(steps target / total), so that all sequences' cuts are no more than
+  // are wanted, of MIN_STEPS at least.
+  __device__ __forceinline__ int parts(int steps) const {
+    int64_t n = int64_t(double(steps) * rate + 1e-6);
+    n -= n * total > int64_t(steps) * target;
+    return int(std::max<int64_t>(1, std::min<int64_t>(n, steps / MIN_STEPS)));
+  }
 };
 
-// Unit x: a share of a tile, or with TILES a tile; false: there are fewer.
+// Unit x: a share of a tile, or with TILES a tile that is cut; false: there are fewer.
 // target: shares that are wanted (0: no tile is cut).
 template <int COLS, bool TILES>
 __device__ __forceinline__ bool find(const AttnExtendLaunch& p, int G, int64_t x, int target, Unit& u) {
@@ -88,25 +102,28 @@ __device__ __forceinline__ bool find(const AttnExtendLaunch& p, int G, int64_t x
   const int lane = threadIdx.x & 63;
   const int n = int(p.c.n_seq), run = (n + 63) / 64;
   auto seq = [&](int j) { return seq_of(p, p.row_start[j], p.row_start[j + 1], p.lens[j]); };
-  u.per = 0x40000000;
+  u.rate = 0.0;
+  u.total = 0;
+  u.target = target;
   if (target > 0) {
-    float mine = 0.0f;  // (an estimate: every wavefront adds up the same numbers in the same order)
+    int64_t total = 0;
     for (int j = lane * run; j < lane * run + run && j < n; ++j) {
       const Seq s = seq(j);
-      mine += float(w.tiles(s)) * float(w.steps(s));
+      total += int64_t(w.tiles(s)) * w.steps(s);
     }
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1) mine += __shfl_xor(mine, d);
-    const int per = int(fminf(mine / float(target), 1e9f)) + WAVES;
-    u.per = std::max(MIN_STEPS, per & ~(WAVES - 1));
+    for (int d = 1; d < 64; d <<= 1)
+      total += int64_t(uint64_t(uint32_t(__shfl_xor(int(total >> 32), d))) << 32 | uint32_t(__shfl_xor(int(total), d)));
+    u.total = total;
+    u.rate = double(target) / double(total > 0 ? total : 1);
   }
   auto count = [&](int j, int& un, int& sp) {
     un = sp = 0;
     if (j >= n) return;
     const Seq s = seq(j);
-    const int tiles = w.tiles(s), parts = std::max(1, (w.steps(s) + u.per - 1) / u.per);
-    un = TILES ? tiles : tiles * parts;
+    const int tiles = w.tiles(s), parts = u.parts(w.steps(s));
     sp = parts > 1 ? tiles * parts : 0;
+    un = !TILES ? tiles * parts : parts > 1 ? tiles : 0;
   };
   int un = 0, sp = 0;
   for (int j = lane * run; j < lane * run + run; ++j) {
@@ -199,7 +216,7 @@ __global__ __launch_bounds__(256, (kHeld<FMT, D, NG, NT>)) void attn_extend_kern
   const int s = unit.s;
   const Seq seq = seq_of(p, scalar(p.row_start, s), scalar(p.row_start, s + 1), scalar(p.lens, s));
   const Work<COLS> work{p, G};
-  const int tiles = work.tiles(seq), parts = std::max(1, (work.steps(seq) + unit.per - 1) / unit.per);
+  const int tiles = work.tiles(seq), parts = unit.parts(work.steps(seq));
   const int part = unit.at / tiles, tile = tiles - 1 - unit.at % tiles;  // the longest first
   const int len = capped(p, seq.len);
   const int base = seq.len < 0 ? -seq.m : std::max(seq.len - seq.m, -seq.m);
@@ -448,7 +465,7 @@ __global__ __launch_bounds__(256, (kHeld<FMT, D, NG, NT>)) void attn_extend_kern
       for (int j = 1; j < 8; ++j) mx = fmaxf(mx, x[n][j]);
       mx = max4(mx) * cl[n];
       if (__any(mx > m[n] + SLACK)) {
-        const float m1 = fmaxf(m[n], mx);
+        const float m1 = mx > m[n] + SLACK ? mx : m[n];  // a column's alone: rows do not depend on others
         const float f = __builtin_amdgcn_exp2f(m[n] - m1);
         m[n] = m1;
         l[n] *= f;
@@ -626,7 +643,7 @@ __global__ __launch_bounds__(256, (kHeld<FMT, D, NG, NT>)) void attn_extend_kern
         // no weight at all: 0, where the values may have made the sums NaN
         *reinterpret_cast<uint32_t*>(p.O + r * p.ld_o + int64_t(hd) * D + cn) = t == 0.0f ? 0u : pack_bf16x2(x0 * inv, x1 * inv);
         if (cn == 0 && p.lse) p.lse[r * p.H + hd] = t == 0.0f ? -__builtin_inff() : top + __builtin_amdgcn_logf(t);
-      } else if (slot < 2 * int64_t(target)) {
+      } else if (slot < int64_t(target)) {
         float* out = part_of<COLS, D>(p, slot, g, 16 * n + h);
         *reinterpret_cast<float2*>(out + 4 + cn) = make_float2(x0, x1);
         if (cn == 0) *reinterpret_cast<float2*>(out) = make_float2(top, t);
@@ -649,10 +666,11 @@ __device__ __forceinline__ float max2(float x) {
 
 // The codes of a thread's piece of a tile and their statistics, between their loads
 // and LDS: row threadIdx.x / 8 of 32, codes 16 q .. + 16 as they lie (q = threadIdx.x % 8).
-template <int FMT, int NG>
+template <int FMT>
 struct Codes {
+  static constexpr int NG = 4;                    // groups of a head
   static constexpr int W = FMT == KV_U8 ? 4 : 2;  // words of 16 codes
-  uint32_t k[W], v[W], ks[NG == 1 ? 1 : 2], vs[NG];
+  uint32_t k[W], v[W], ks[2], vs[NG];
   bool is;
 
   __device__ __forceinline__ void load(const KvCache& c, const uint64_t (&at)[2], const uint64_t (&st)[2],
@@ -674,12 +692,9 @@ struct Codes {
     const uint32_t* kst = reinterpret_cast<const uint32_t*>(c.k_stat) + st[t] + (r & 15);
     const uint32_t* vst = reinterpret_cast<const uint32_t*>(c.v_stat) + st[t] + (r & 15);
     const uint32_t len = uint32_t(c.page_len);
-    if constexpr (NG == 1) {
-      ks[0] = kst[0];
-    } else {  // the piece's two runs of eight channels lie in groups 2 (q % 2) and the next
-      ks[0] = kst[(2 * (q & 1)) * len];
-      ks[1] = kst[(2 * (q & 1) + 1) * len];
-    }
+    // the piece's two runs of eight channels lie in groups 2 (q % 2) and the next
+    ks[0] = kst[(2 * (q & 1)) * len];
+    ks[1] = kst[(2 * (q & 1) + 1) * len];
 #pragma unroll
     for (int e = 0; e < NG; ++e) vs[e] = vst[uint32_t(e) * len];
   }
@@ -696,14 +711,14 @@ struct Codes {
     return __builtin_fmaf(__uint_as_float(st << 16), c, __uint_as_float(st & 0xFFFF0000u));
   }
 
-  // Into the tiles kh, kl, vh, vl of LDS; rows that do not exist are 0.
+  // Into LDS: tiles kh, kl, vh, vl of the values' two terms; rows that do not exist are 0.
   __device__ __forceinline__ void store(u32x4a* stage) const {
     const int r = threadIdx.x >> 3, q = threadIdx.x & 7, rho = perm32(r);
     u32x4a* row = stage + rho * 16;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {  // channels 32 cc + 8 (q / 2) .. + 8, cc = 2 (q % 2) + h
       u32x4a hi, lo;
-      const uint32_t st = is ? ks[NG == 1 ? 0 : h] : 0u;
+      const uint32_t st = is ? ks[h] : 0u;
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         // (4-bit codes of a run lie in the order 0 2 4 6 1 3 5 7)
@@ -721,7 +736,7 @@ struct Codes {
 #pragma unroll
     for (int b = 0; b < 8; ++b) {  // channels 16 b + 2 q and the next
       uint32_t hi, lo;
-      const uint32_t st = is ? vs[b * NG / 8] : 0u;
+      const uint32_t st = is ? vs[b / 2] : 0u;
       terms(value(st, code(v, b)), value(st, code(v, b + 8)), hi, lo);
       const int at = ((2 * b + (q >> 2)) ^ swz(rho)) * 4 + (q & 3);
       vrow[at] = hi;
@@ -732,17 +747,19 @@ struct Codes {
 
 // As attn_extend_kernel, for heads of 128 channels: a wavefront owns 32 columns and
 // walks all steps of the workgroup's share, whose keys and values lie in LDS as
-// bf16 tiles of 32 rows (uq_tile.h), copied a stage ahead.  Codes are made values on
-// the way, two bf16 terms each (off by 2^-18 of a value): both products then need
-// neither scales nor offsets, and the work of that is shared by 128 columns.
+// bf16 tiles of 32 rows (uq_tile.h), copied a stage ahead.
+// Codes in groups of 32 are made values on the way, two bf16 terms each (off by 2^-18
+// of a value): both products then need neither scales nor offsets, and the work of
+// that is shared by 128 columns.  With one group a head a scale and an offset a row
+// cost less than the second terms' products, and the tiles hold the codes.
 template <int FMT, int NG>
 __global__ __launch_bounds__(256, 2) void attn_extend_wide_kernel(AttnExtendLaunch p, int target) {
   constexpr bool CODES = FMT != KV_BF16;
   constexpr int TERMS = CODES ? 2 : 1;              // of a key and of a value
-  constexpr int TILES = CODES ? 1 : 2;              // steps of a stage
+  constexpr int STAGES = 2, STEPS = CODES ? 1 : 2;  // steps of a stage
   constexpr int TILE = 2 * TERMS * TILE16;          // a step's keys and values
   constexpr uint32_t ROW = FMT == KV_BF16 ? 256 : FMT == KV_U8 ? 128 : 64;
-  __shared__ u32x4a smem[2][TILES * TILE];
+  __shared__ u32x4a smem[STAGES][STEPS * TILE];
   const KvCache& c = p.c;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int G = p.H / c.H_kv;
@@ -753,7 +770,7 @@ __global__ __launch_bounds__(256, 2) void attn_extend_wide_kernel(AttnExtendLaun
   const int s = unit.s;
   const Seq seq = seq_of(p, scalar(p.row_start, s), scalar(p.row_start, s + 1), scalar(p.lens, s));
   const Work<WIDE> work{p, G};
-  const int tiles = work.tiles(seq), parts = std::max(1, (work.steps(seq) + unit.per - 1) / unit.per);
+  const int tiles = work.tiles(seq), parts = unit.parts(work.steps(seq));
   const int part = unit.at / tiles, tile = tiles - 1 - unit.at % tiles;  // the longest first
   const int len = capped(p, seq.len);
   const int base = seq.len < 0 ? -seq.m : std::max(seq.len - seq.m, -seq.m);
@@ -827,18 +844,17 @@ __global__ __launch_bounds__(256, 2) void attn_extend_wide_kernel(AttnExtendLaun
   }
   const float cl = fabsf(p.scale) * LOG2E;  // scores to exponents of 2
 
-  // a stage's copies: of a bf16 cache straight into LDS, two blocks of 64 slots of every tile a wavefront
-  int nv[TILES][2];
+  // copies of a bf16 cache straight into LDS, two blocks of 64 slots of every tile a wavefront
   uint32_t off[2];
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int slot = (2 * wave + k) * 64 + lane, rho = slot >> 4;
     off[k] = uint32_t(perm32(rho) & 15) * ROW + uint32_t(((slot & 15) ^ swz(rho)) * 16);
   }
-  auto copy_stage = [&](int i, u32x4a* stage, int (&n)[TILES][2]) {
+  uint64_t at[2], st[2];
+  auto copy_stage = [&](int i, u32x4a* stage, int (&n)[STEPS][2]) {
 #pragma unroll
-    for (int t = 0; t < TILES; ++t) {
-      uint64_t at[2], st[2];
+    for (int t = 0; t < STEPS; ++t) {
       look_up(i + t, at, st, n[t]);
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -848,9 +864,7 @@ __global__ __launch_bounds__(256, 2) void attn_extend_wide_kernel(AttnExtendLaun
       }
     }
   };
-  Codes<CODES ? FMT : KV_U8, NG> codes;
-  int nv_next[TILES][2];
-  uint64_t at[2], st[2];
+  Codes<CODES ? FMT : KV_U8> codes;
 
   f32x16a o[4] = {zero16(), zero16(), zero16(), zero16()};
   // weights count in 2^-24 against the running maximum (see attn_decode.hip): m is 24 above it
@@ -883,7 +897,7 @@ __global__ __launch_bounds__(256, 2) void attn_extend_wide_kernel(AttnExtendLaun
     for (int r = 1; r < 16; ++r) mx = fmaxf(mx, x[r]);
     mx = max2(mx) * cl;
     if (__any(mx > m - DOWN + SLACK)) {
-      const float m1 = fmaxf(m, mx + DOWN);
+      const float m1 = mx > m - DOWN + SLACK ? mx + DOWN : m;
       const float f = exp2a(m - m1);
       m = m1;
       l *= f;
@@ -928,7 +942,7 @@ __global__ __launch_bounds__(256, 2) void attn_extend_wide_kernel(AttnExtendLaun
             const int ch = 32 * db + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
             const int at = ((ch >> 3) ^ swz(rho)) * 8 + (ch & 7);
             float v = bf16_to_f32(vrow[at]);
-            if constexpr (CODES) v += bf16_to_f32(vrow[TILE16 * 8 + at]);
+            if constexpr (TERMS == 2) v += bf16_to_f32(vrow[TILE16 * 8 + at]);
             if (z != 0.0f) o[db][r] += z * v;
           }
       }
@@ -944,7 +958,7 @@ __global__ __launch_bounds__(256, 2) void attn_extend_wide_kernel(AttnExtendLaun
     }
   };
 
-  int cur = 0;
+  int nv[STEPS][2], nv_next[STEPS][2], cur = 0;
   if constexpr (CODES) {
     look_up(i0, at, st, nv[0]);
     codes.load(c, at, st, nv[0]);
@@ -955,24 +969,24 @@ __global__ __launch_bounds__(256, 2) void attn_extend_wide_kernel(AttnExtendLaun
   } else {
     copy_stage(i0, smem[0], nv);
   }
-  for (int i = i0; i < i1; i += TILES, cur ^= 1) {
+  for (int i = i0; i < i1; i += STEPS, cur ^= 1) {
     if constexpr (CODES) {
       step(smem[cur], step_at(i) * STEP, nv[0]);
+      codes.store(smem[cur ^ 1]);
       nv[0][0] = nv_next[0][0];
       nv[0][1] = nv_next[0][1];
-      codes.store(smem[cur ^ 1]);
       look_up(i + 2, at, st, nv_next[0]);
       codes.load(c, at, st, nv_next[0]);
       __syncthreads();
     } else {
       vm_wait<0>();
       lds_wait_barrier();
-      copy_stage(i + TILES, smem[cur ^ 1], nv_next);
+      copy_stage(i + STEPS, smem[cur ^ 1], nv_next);
 #pragma unroll
-      for (int t = 0; t < TILES; ++t)
+      for (int t = 0; t < STEPS; ++t)
         if (i + t < i1) step(smem[cur] + t * TILE, step_at(i + t) * STEP, nv[t]);
 #pragma unroll
-      for (int t = 0; t < TILES; ++t)
+      for (int t = 0; t < STEPS; ++t)
 #pragma unroll
         for (int k = 0; k < 2; ++k) nv[t][k] = nv_next[t][k];
     }
@@ -997,7 +1011,7 @@ __global__ __launch_bounds__(256, 2) void attn_extend_wide_kernel(AttnExtendLaun
     return;
   }
   const int64_t slot = int64_t(unit.slot) + unit.at;
-  if (slot >= 2 * int64_t(target)) return;
+  if (slot >= int64_t(target)) return;
   float* out = part_of<WIDE, D>(p, slot, g, 32 * wave + (lane & 31));
 #pragma unroll
   for (int db = 0; db < 4; ++db)
@@ -1021,13 +1035,12 @@ __global__ __launch_bounds__(256) void attn_extend_join_kernel(AttnExtendLaunch 
   const int s = unit.s;
   const Seq seq = seq_of(p, scalar(p.row_start, s), scalar(p.row_start, s + 1), scalar(p.lens, s));
   const Work<COLS> work{p, G};
-  const int tiles = work.tiles(seq), n = std::max(1, (work.steps(seq) + unit.per - 1) / unit.per);
-  if (n == 1) return;
+  const int tiles = work.tiles(seq), n = unit.parts(work.steps(seq));
   const int lane = threadIdx.x % LANES, rank = threadIdx.x / LANES % PAR, col = group * ROWS + threadIdx.x / LANES / PAR;
   const int tile = unit.at;
   const int64_t idx = int64_t(tile) * COLS + col;
   const int64_t r = int64_t(seq.first) + idx / G;
-  const bool real = idx / G < seq.m && r < p.T && int64_t(unit.slot) + int64_t(n) * tiles <= 2 * int64_t(target);
+  const bool real = idx / G < seq.m && r < p.T && int64_t(unit.slot) + int64_t(n) * tiles <= int64_t(target);
   float m = LOWEST, t = 0.0f;
   f32x4d a = {};
   if (real) {
@@ -1084,24 +1097,37 @@ __global__ __launch_bounds__(256) void attn_extend_join_kernel(AttnExtendLaunch 
   if (lane == 0 && p.lse) p.lse[r * p.H + hd] = t == 0.0f ? -__builtin_inff() : m + __builtin_amdgcn_logf(t);
 }
 
-// Columns of a workgroup, for those that a sequence has on average: 16, 32, and of heads of 128 channels WIDE.
-int columns_of(int64_t T, int64_t n_seq, int H, int H_kv, int d) {
+// Columns of a workgroup, for those that a sequence has on average: 16, 32, and of heads of 128 channels WIDE
+// (us, 24 sequences of 8192 positions, 8 key/value heads, with 16 | 32 | 128 columns):
+//   32 columns:  bf16 199 | 180 | 243,  u8 133 | 112 | -,    u8 in groups of 32 183 | 361 | 332
+//   64 columns:  bf16   - | 223 | 262,                       u8 in groups of 32 262 | 552 | 329
+//   128 columns: bf16 515 | 297 | 241,  u8 346 | 247 | 276,  u8 in groups of 32 444 | 957 | 342
+// Two column tiles and the statistics of four groups do not fit into the registers.
+enum Kind { PLAIN, ONE_GROUP, GROUPS };
+constexpr Kind kind_of(int fmt, int ng) { return fmt == KV_BF16 ? PLAIN : ng == 1 ? ONE_GROUP : GROUPS; }
+int columns_of(int64_t T, int64_t n_seq, int H, int H_kv, int d, Kind f) {
   const int64_t cols = (T + n_seq - 1) / n_seq * (H / H_kv);
-  return cols <= 16 ? 16 : cols <= 32 || d != 128 ? 32 : WIDE;
+  if (cols <= 16) return 16;
+  if (d != 128 || f == ONE_GROUP) return 32;
+  return cols > 64 ? WIDE : f == PLAIN ? 32 : 16;
 }
 // Tiles of one key/value head, if no row is padding.
 int64_t tiles_of(int64_t T, int H, int H_kv, int cols) { return T * (H / H_kv) / cols; }
-// Shares of one key/value head that are wanted (0: no tile is cut).
-int target_of(int64_t T, int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len) {
-  const int cols = columns_of(T, n_seq, H, H_kv, d);
-  const int64_t want = std::max(1, 2 * CUS / H_kv);
-  if (max_pages * page_len <= MIN_STEPS * STEP || tiles_of(T, H, H_kv, cols) >= 4 * want) return 0;
-  return int(want);
+// Shares of one key/value head that are wanted (0: no tile is cut).  The GPU holds two workgroups a CU; between a
+// quarter of those and all, two rounds of shares even out what rounding shares of whole steps leaves (24 x 32 rows
+// of 8192 positions at 8 bits, 1.5 tiles a place: 245 us with one round, 250 with two).  With more tiles than places
+// only a tile of twice the mean and more is cut, which costs equal sequences the join (1 x 2048 rows 85 -> 92 us) and
+// saves unequal ones more (96 x 8 rows, one sequence of 32768 positions and 95 of 1024: 470 -> 134 us).
+int target_of(int64_t T, int64_t n_seq, int H, int H_kv, int cols, int64_t max_pages, int page_len) {
+  const int64_t holds = std::max(1, 2 * CUS / H_kv), tiles = std::max(tiles_of(T, H, H_kv, cols), std::min(T, n_seq));
+  if (max_pages * page_len <= MIN_STEPS * STEP || tiles >= 4 * holds) return 0;
+  return int(4 * tiles <= holds || tiles >= holds ? holds : 2 * holds);
 }
 
 template <int D, int COLS>
-hipError_t launch_join(const AttnExtendLaunch& p, int64_t tiles, int target, float back, hipStream_t st) {
+hipError_t launch_join(const AttnExtendLaunch& p, int target, float back, hipStream_t st) {
   constexpr int LANES = D / 4;
+  const int64_t tiles = std::min<int64_t>(tiles_of(p.T, p.H, p.c.H_kv, COLS) + std::min(p.T, p.c.n_seq), target / 2);
   if (p.T * p.H <= 2048)
     attn_extend_join_kernel<D, COLS, 256 / LANES><<<grid_of(tiles * p.c.H_kv * COLS), 256, 0, st>>>(p, target, back);
   else
@@ -1111,25 +1137,29 @@ hipError_t launch_join(const AttnExtendLaunch& p, int64_t tiles, int target, flo
 
 template <int FMT, int D, int NG>
 hipError_t launch_form(const AttnExtendLaunch& p, hipStream_t st) {
-  const int H_kv = p.c.H_kv, cols = columns_of(p.T, p.c.n_seq, p.H, H_kv, D);
-  const int target = target_of(p.T, p.c.n_seq, p.H, H_kv, D, p.c.max_pages, p.c.page_len);
+  constexpr Kind KIND = kind_of(FMT, NG);
+  const int H_kv = p.c.H_kv, cols = columns_of(p.T, p.c.n_seq, p.H, H_kv, D, KIND);
+  const int target = target_of(p.T, p.c.n_seq, p.H, H_kv, cols, p.c.max_pages, p.c.page_len);
   const int64_t tiles = tiles_of(p.T, p.H, H_kv, cols) + std::min(p.T, p.c.n_seq);
   const dim3 grid = grid_of((tiles + target) * H_kv);
   const float back = FMT == KV_BF16 ? BF16_BACK : 1.0f;
-  if constexpr (D == 128) {
+  if constexpr (D == 128 && KIND != ONE_GROUP) {
     if (cols == WIDE) {
       attn_extend_wide_kernel<FMT, NG><<<grid, 256, 0, st>>>(p, target);
       if (hipError_t e = hipGetLastError()) return e;
-      return target ? launch_join<D, WIDE>(p, tiles, target, 1.0f, st) : hipSuccess;
+      return target ? launch_join<D, WIDE>(p, target, 1.0f, st) : hipSuccess;
     }
   }
-  if (cols == 16)
-    attn_extend_kernel<FMT, D, NG, 1><<<grid, 256, 0, st>>>(p, target);
-  else
-    attn_extend_kernel<FMT, D, NG, 2><<<grid, 256, 0, st>>>(p, target);
+  if constexpr (D == 64 || KIND != GROUPS) {
+    if (cols == 32) {
+      attn_extend_kernel<FMT, D, NG, 2><<<grid, 256, 0, st>>>(p, target);
+      if (hipError_t e = hipGetLastError()) return e;
+      return target ? launch_join<D, 32>(p, target, back, st) : hipSuccess;
+    }
+  }
+  attn_extend_kernel<FMT, D, NG, 1><<<grid, 256, 0, st>>>(p, target);
   if (hipError_t e = hipGetLastError()) return e;
-  if (!target) return hipSuccess;
-  return cols == 16 ? launch_join<D, 16>(p, tiles, target, back, st) : launch_join<D, 32>(p, tiles, target, back, st);
+  return target ? launch_join<D, 16>(p, target, back, st) : hipSuccess;
 }
 
 template <int D>
@@ -1143,8 +1173,12 @@ hipError_t launch_d(const AttnExtendLaunch& p, hipStream_t st) {
 }  // namespace
 
 size_t attn_extend_ws(int64_t T, int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len) {
-  const size_t target = size_t(target_of(T, n_seq, H, H_kv, d, max_pages, page_len));
-  return 2 * target * size_t(H_kv) * size_t(columns_of(T, n_seq, H, H_kv, d)) * size_t(d + 4);
+  size_t most = 0;  // of all formats
+  for (const Kind f : {PLAIN, ONE_GROUP, GROUPS}) {
+    const int cols = columns_of(T, n_seq, H, H_kv, d, f);
+    most = std::max(most, size_t(target_of(T, n_seq, H, H_kv, cols, max_pages, page_len)) * size_t(cols));
+  }
+  return most * size_t(H_kv) * size_t(d + 4);
 }
 
 hipError_t launch_attn_extend(const AttnExtendLaunch& p, hipStream_t st) {
