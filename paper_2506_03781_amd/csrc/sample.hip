@@ -144,10 +144,14 @@ struct Row {
   }
   __device__ __forceinline__ int chunk(int wave, int i) const { return (wave * per + i) * 64 + int(threadIdx.x & 63); }
   __device__ __forceinline__ int first(int c) const { return c * E - shift; }
-  // Words of chunk c, without a branch: of one in part, or of none, some other's.
+  // Words of chunk c, without a branch: of one in part, or of none, some other's.  (Named global: the compiler
+  // does not see it through the choice, and a wait for one of its flat loads is one for all of them.)
   __device__ __forceinline__ uint4 ask(int c) const {
-    const uint4* p = reinterpret_cast<const uint4*>(lo <= hi ? at : reinterpret_cast<const char*>(&no_chunk));
-    return p[lo <= hi ? min(max(c, lo), hi) : 0];
+    typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+    typedef const __attribute__((address_space(1))) u32x4 Global;
+    const uintptr_t p = reinterpret_cast<uintptr_t>(lo <= hi ? static_cast<const void*>(at) : &no_chunk);
+    const u32x4 q = reinterpret_cast<Global*>(p)[lo <= hi ? min(max(c, lo), hi) : 0];
+    return make_uint4(q.x, q.y, q.z, q.w);
   }
   // The words asked for, or those of a chunk in part; what is outside the row is -infinity.
   __device__ __forceinline__ uint4 get(int c, uint4 q) const {
@@ -200,10 +204,10 @@ __device__ __forceinline__ void over_chunks(const Row<F32>& row, int of, int i0,
 // A logit as it counts: NaN as -infinity, -0 as 0.
 __device__ __forceinline__ float clean(float x) { return x == x ? x + 0.0f : -__builtin_inff(); }
 
-// f(x, index) for their elements as they stand, two at a time for the same reason;
-// only of chunks that have one of `from` or more in some lane.
+// f(four elements as they stand, the first one's index) for their elements; only of
+// chunks that have one of `from` or more in some lane.
 template <bool F32, typename Fn>
-__device__ __forceinline__ void over_part(const Row<F32>& row, int of, int i0, int i1, float from, Fn f) {
+__device__ __forceinline__ void over_fours(const Row<F32>& row, int of, int i0, int i1, float from, Fn f) {
   over_chunks(row, of, i0, i1, [&](int c, uint4 q) {
     float m = row.raw(q, 0);
 #pragma unroll
@@ -211,11 +215,19 @@ __device__ __forceinline__ void over_part(const Row<F32>& row, int of, int i0, i
     if (!__any(m >= from)) return;
     int i = row.first(c);
 #pragma unroll 1
-    for (int h = 0; h < Row<F32>::E / 4; ++h, i += 4) {  // four at a time
-#pragma unroll
-      for (int e = 0; e < 4; ++e) f(row.raw(q, e), i + e);
+    for (int h = 0; h < Row<F32>::E / 4; ++h, i += 4) {
+      const float x[4] = {row.raw(q, 0), row.raw(q, 1), row.raw(q, 2), row.raw(q, 3)};
+      f(x, i);
       q = make_uint4(q.z, q.w, q.z, q.w);
     }
+  });
+}
+// f(x, index) for them, one after the other.
+template <bool F32, typename Fn>
+__device__ __forceinline__ void over_part(const Row<F32>& row, int of, int i0, int i1, float from, Fn f) {
+  over_fours(row, of, i0, i1, from, [&](const float (&x)[4], int i) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) f(x[e], i + e);
   });
 }
 template <bool F32, typename Fn>
@@ -246,6 +258,7 @@ struct Weigh {
   float top;       // the row's maximum, 0 where that is +infinity
   bool endless;    // it is: tokens at it count as 0, others as -infinity
   double per_t;    // log2(e) / temperature
+  double least;    // of x - max, -1000 / per_t: the weight rounds to 0
   double magic;    // 1.5 2^52 + sh
   double lead;     // the power's first coefficient
   float bins;      // bins per unit of max - x
@@ -260,15 +273,37 @@ struct Weigh {
   // Values of bin b lie in [floor_of(b), ceil_of(b)]: a bin to spare for the roundings.
   __device__ __forceinline__ float floor_of(int b) const { return uni(top - float(b + 2) * width); }
   __device__ __forceinline__ float ceil_of(int b) const { return uni(b < 2 ? top : top - float(b - 1) * width); }
-  __device__ __forceinline__ u64 operator()(float x) const {
-    // (no less than 2^-1000, which rounds to 0 as -infinity and NaN have to)
-    const double y = fmax((double(x) - double(top)) * per_t, -1000.0), t = y + magic, r = y - (t - magic);
-    double v = fma_s(r, lead, kPower[1]);
+  // The weights of N tokens above BIAS, step by step side by side.
+  static constexpr u64 BIAS = u64(0x433) << 52;
+  template <int N>
+  __device__ __forceinline__ void biased(const float (&x)[N], u64 (&w)[N]) const {
+    double t[N], r[N], v[N];
 #pragma unroll
-    for (int i = 2; i < 11; ++i) v = fma_s(v, r, kPower[i]);
+    for (int e = 0; e < N; ++e) {  // (-infinity and NaN as the least)
+      r[e] = fmax(double(x[e]) - double(top), least);
+      t[e] = fma(r[e], per_t, magic);
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) r[e] = fma(r[e], per_t, magic - t[e]);
+#pragma unroll
+    for (int e = 0; e < N; ++e) v[e] = fma_s(r[e], lead, kPower[1]);
+#pragma unroll
+    for (int i = 2; i < 11; ++i) {
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] = fma_s(v[e], r[e], kPower[i]);
+    }
     // 2^(n + sh) times it, rounded to an integer in the low bits
-    v = __hiloint2double(__double2hiint(v) + (__double2loint(t) << 20), __double2loint(v)) + 0x1p52;
-    return u64(uint32_t(__double2hiint(v)) & 0xFFFFFu) << 32 | uint32_t(__double2loint(v));
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+      v[e] = __hiloint2double(__double2hiint(v[e]) + (__double2loint(t[e]) << 20), __double2loint(v[e])) + 0x1p52;
+      w[e] = u64(__double_as_longlong(v[e]));
+    }
+  }
+  __device__ __forceinline__ u64 operator()(float x) const {
+    const float one[1] = {x};
+    u64 v[1];
+    biased(one, v);
+    return v[0] - BIAS;
   }
 };
 
@@ -536,13 +571,23 @@ template <bool F32>
 __device__ __forceinline__ Before histogram(Lds& s, const Row<F32>& row, const Weigh& w, u64& total) {
   clear_bins(s);
   const float from = w.floor_of(BINS - 2);  // the last bin's tokens, and what is outside the row, have no weight
-  over_row(row, w.endless ? __builtin_inff() : from, [&](float x, int) {
-    x = w.seen(x);
-    if (!(x >= from)) return;
-    const int b = w.bin(x);
-    if (b == BINS - 1) return;
-    atomicAdd(&s.count[b], 1u);
-    atomicAdd(&s.mass[b], w(x));
+  over_fours(row, uni(int(threadIdx.x >> 6)), 0, row.per, w.endless ? __builtin_inff() : from, [&](const float (&in)[4], int) {
+    float x[4] = {in[0], in[1], in[2], in[3]};
+    if (w.endless) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = w.seen(x[e]);
+    }
+    u64 v[4];
+    w.biased(x, v);
+    int b[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) b[e] = x[e] >= from ? w.bin(x[e]) : BINS - 1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (b[e] == BINS - 1) continue;
+      atomicAdd(&s.count[b[e]], 1u);
+      atomicAdd(&s.mass[b[e]], v[e] - Weigh::BIAS);
+    }
   });
   __syncthreads();
   return bins_before<true>(s, total);
@@ -650,7 +695,8 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleLaunch p) {
   w.top = w.endless ? 0.0f : top;
   w.lead = kPower[0];
   w.magic = 0x1.8p52 + double(p.sh);
-  w.per_t = uni(1.4426950408889634 / double(temp));
+  w.per_t = uni(fmax(1.4426950408889634 / double(temp), 1e-300));  // (not 0 where the temperature is infinite)
+  w.least = uni(-1000.0 / w.per_t);
   // the last bin begins at (sh + 1.98) ln 2, where weights round to 0
   w.bins = uni(fminf(float(BINS) / (float(p.sh + 2) * 0.6931472f) / temp, 3e38f));
   w.width = uni(1.0f / w.bins);
@@ -733,14 +779,42 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleLaunch p) {
     if (least) v = v >= least ? v : 0;
     return stays ? v : 0;
   };
+  // Sum of the weights that stay.  Nearly all rows': of the tokens up to one of them in order, what is behind it
+  // counted as -infinity; four chains without a branch (one after the other, with the tests of the general case,
+  // took 55 us in place of XX for 256 x 131072 tokens).
+  const bool simple = !w.endless && !least && (last_bin == BINS || last != ~u64(0));
+  const float end_x = last_bin < BINS ? value_of(uint32_t(last >> 32)) : -__builtin_inff();
+  const float past_x = uni(value_of(key_of(end_x) - 1));  // the next larger value
+  const int end_i = last_bin < BINS ? int(uint32_t(last)) : 0x7FFFFFFF;
+  auto sum_of = [&](int of, int i0, int i1) {
+    u64 sum = 0;
+    if (simple) {
+      uint32_t n = 0;
+      over_fours(row, of, i0, i1, end_x, [&](const float (&x)[4], int i) {
+        const float least_x = i <= end_i ? end_x : past_x;
+        float y[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = x[e] >= least_x ? x[e] : -__builtin_inff();
+        if (i <= end_i && end_i < i + 3) {
+#pragma unroll
+          for (int e = 1; e < 4; ++e) y[e] = i + e <= end_i || x[e] > end_x ? y[e] : -__builtin_inff();
+        }
+        u64 v[4];
+        w.biased(y, v);
+        sum += (v[0] + v[1]) + (v[2] + v[3]);
+        n += 4;
+      });
+      return sum - n * Weigh::BIAS;
+    }
+    over_part(row, of, i0, i1, chunks_from, [&](float x, int i) { sum += weight(x, i); });
+    return sum;
+  };
   u64 all = 0, left = 0;
   int of = 0, at0 = 0, n = WAVES * row.per;  // chunk groups at0 .. at0 + n of wavefront `of` (first: of all)
   for (bool first = true; first || n > 1; first = false) {
     const int each = first ? row.per : (n + WAVES - 1) / WAVES;
     const int i0 = first ? 0 : at0 + std::min(wave * each, n), i1 = first ? row.per : at0 + std::min((wave + 1) * each, n);
-    u64 sum = 0;
-    over_part(row, first ? wave : of, i0, i1, chunks_from, [&](float x, int i) { sum += weight(x, i); });
-    sum = wave_sum(sum);
+    const u64 sum = wave_sum(sum_of(first ? wave : of, i0, i1));
     if (first) {
       block_before(s, lane ? 0 : sum, all);
       left = part_of(p.u[t], all);
