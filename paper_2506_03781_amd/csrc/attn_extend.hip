@@ -114,8 +114,8 @@ __device__ __forceinline__ bool find(const AttnExtendLaunch& p, int G, int64_t x
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1)
       total += int64_t(uint64_t(uint32_t(__shfl_xor(int(total >> 32), d))) << 32 | uint32_t(__shfl_xor(int(total), d)));
-    u.total = total;
-    u.rate = double(target) / double(total > 0 ? total : 1);
+    u.total = int64_t(uint64_t(uint32_t(uniform(int(total >> 32)))) << 32 | uint32_t(uniform(int(total))));
+    u.rate = double(target) / double(u.total > 0 ? u.total : 1);
   }
   auto count = [&](int j, int& un, int& sp) {
     un = sp = 0;
@@ -759,7 +759,7 @@ __global__ __launch_bounds__(256, 2) void attn_extend_wide_kernel(AttnExtendLaun
   constexpr int STAGES = 2, STEPS = CODES ? 1 : 2;  // steps of a stage
   constexpr int TILE = 2 * TERMS * TILE16;          // a step's keys and values
   constexpr uint32_t ROW = FMT == KV_BF16 ? 256 : FMT == KV_U8 ? 128 : 64;
-  __shared__ u32x4a smem[STAGES][STEPS * TILE];
+  __shared__ __attribute__((aligned(256))) u32x4a smem[STAGES][STEPS * TILE];
   const KvCache& c = p.c;
   const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
   const int G = p.H / c.H_kv;
@@ -770,8 +770,8 @@ __global__ __launch_bounds__(256, 2) void attn_extend_wide_kernel(AttnExtendLaun
   const int s = unit.s;
   const Seq seq = seq_of(p, scalar(p.row_start, s), scalar(p.row_start, s + 1), scalar(p.lens, s));
   const Work<WIDE> work{p, G};
-  const int tiles = work.tiles(seq), parts = unit.parts(work.steps(seq));
-  const int part = unit.at / tiles, tile = tiles - 1 - unit.at % tiles;  // the longest first
+  const int tiles = work.tiles(seq), parts = uniform(unit.parts(work.steps(seq)));
+  const int part = uniform(unit.at / tiles), tile = tiles - 1 - uniform(unit.at % tiles);  // the longest first
   const int len = capped(p, seq.len);
   const int base = seq.len < 0 ? -seq.m : std::max(seq.len - seq.m, -seq.m);
   const bool tree = p.mask != nullptr;
@@ -810,7 +810,7 @@ __global__ __launch_bounds__(256, 2) void attn_extend_wide_kernel(AttnExtendLaun
   const int n_sink = p.window > 0 ? (std::min(p.sinks, std::max(hi, 0)) + STEP - 1) / STEP : 0;
   const int u_lo = std::max(lo / STEP, n_sink);
   const int n_steps = n_sink + std::max(0, (std::max(hi, 0) + STEP - 1) / STEP - u_lo);
-  const int i0 = int(int64_t(n_steps) * part / parts), i1 = int(int64_t(n_steps) * (part + 1) / parts);
+  const int i0 = uniform(int(int64_t(n_steps) * part / parts)), i1 = uniform(int(int64_t(n_steps) * (part + 1) / parts));
   auto step_at = [&](int i) { return i < n_sink ? i : u_lo + (i - n_sink); };
 
   const uint32_t page_bytes = uint32_t(c.H_kv) * uint32_t(c.page_len) * ROW;
@@ -871,14 +871,16 @@ __global__ __launch_bounds__(256, 2) void attn_extend_wide_kernel(AttnExtendLaun
   constexpr float DOWN = 24.0f;
   float m = LOWEST, l = 0.0f;
 
-  // products of one step out of tile tk, nvt of whose positions exist
-  auto step = [&](const u32x4a* tk, int t0, const int (&nvt)[2]) {
+  const LaneTile frags(smem[0], lane);
+  // products of one step out of tile tk, at `bytes` of the stages, nvt of whose positions exist
+  auto step = [&](const u32x4a* tk, uint32_t stage, uint32_t bytes, int t0, const int (&nvt)[2]) {
     const u32x4a* tv = tk + TERMS * TILE16;
+    const LaneTile f = frags.at(stage);
     f32x16a x = zero16();
 #pragma unroll
     for (int term = 0; term < TERMS; ++term)
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x = mfma(row_frag(tk + term * TILE16, k, lane), qf[k], x);
+      for (int k = 0; k < 8; ++k) x = mfma(f.row(k, bytes + term * TILE16 * 16), qf[k], x);
     const bool cut = nvt[0] + nvt[1] < STEP || t0 + STEP > end_min || (t0 < low_max && t0 + STEP > p.sinks);
     uint32_t seen = 0;  // bit r: slot r
     if (cut) {
@@ -954,7 +956,7 @@ __global__ __launch_bounds__(256, 2) void attn_extend_wide_kernel(AttnExtendLaun
 #pragma unroll
       for (int term = 0; term < TERMS; ++term)
 #pragma unroll
-        for (int db = 0; db < 4; ++db) o[db] = mfma(col_frag(tv + term * TILE16, db, h, lane), pb, o[db]);
+        for (int db = 0; db < 4; ++db) o[db] = mfma(f.col(db, h, bytes + (TERMS + term) * TILE16 * 16), pb, o[db]);
     }
   };
 
@@ -971,7 +973,7 @@ __global__ __launch_bounds__(256, 2) void attn_extend_wide_kernel(AttnExtendLaun
   }
   for (int i = i0; i < i1; i += STEPS, cur ^= 1) {
     if constexpr (CODES) {
-      step(smem[cur], step_at(i) * STEP, nv[0]);
+      step(smem[cur], cur * uint32_t(sizeof(smem[0])), 0, step_at(i) * STEP, nv[0]);
       codes.store(smem[cur ^ 1]);
       nv[0][0] = nv_next[0][0];
       nv[0][1] = nv_next[0][1];
@@ -984,7 +986,8 @@ __global__ __launch_bounds__(256, 2) void attn_extend_wide_kernel(AttnExtendLaun
       copy_stage(i + STEPS, smem[cur ^ 1], nv_next);
 #pragma unroll
       for (int t = 0; t < STEPS; ++t)
-        if (i + t < i1) step(smem[cur] + t * TILE, step_at(i + t) * STEP, nv[t]);
+        if (i + t < i1)
+          step(smem[cur] + t * TILE, cur * uint32_t(sizeof(smem[0])), t * TILE * 16, step_at(i + t) * STEP, nv[t]);
 #pragma unroll
       for (int t = 0; t < STEPS; ++t)
 #pragma unroll

@@ -423,7 +423,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   constexpr int QB = NW * NB;
   constexpr int PW = 8 / NW;
   constexpr int TILE = 2 * TILE16;  // key tile, value tile
-  __shared__ u32x4a smem[2][2 * TILE];
+  __shared__ __attribute__((aligned(256))) u32x4a smem[2][2 * TILE];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6));
   const int L = a.L;
@@ -458,6 +458,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   f32x16a o[4] = {zero16(), zero16(), zero16(), zero16()};
   float m = -3.402823466e38f, l = 0.0f;
   copy(0, smem[0]);
+  const LaneTile frags(smem[0], lane);
   int cur = 0;
   for (int i = 0; i < walk.n; i += 2, cur ^= 1) {
     vm_wait<0>();
@@ -468,11 +469,11 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
       if (i + u >= walk.n) break;
       const int t = walk.tile(i + u);
       if (t >= my_tiles || !(t * NB < a.sinks || t >= first_tile(q0, a.window))) continue;
-      const u32x4a* tk = smem[cur] + u * TILE;
-      const u32x4a* tv = tk + TILE16;
+      const LaneTile f = frags.at(cur * uint32_t(sizeof(smem[0])));
+      const uint32_t tk = u * TILE * 16, tv = tk + TILE16 * 16;
       f32x16a s = zero16();
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s = mfma(row_frag(tk, j, lane), qf[j], s);
+      for (int j = 0; j < 8; ++j) s = mfma(f.row(j, tk), qf[j], s);
       if (t == my_tiles - 1 || (q0 + NB - 1 - t * NB >= a.window && (t + 1) * NB > a.sinks)) {
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -490,11 +491,11 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
       }
       if (__any(mx > m + SLACK_W)) {
         const float m1 = mx > m + SLACK_W ? mx : m;
-        const float f = exp2a(m - m1);
+        const float down = exp2a(m - m1);
         m = m1;
-        l *= f;
+        l *= down;
 #pragma unroll
-        for (int db = 0; db < 4; ++db) o[db] *= f;
+        for (int db = 0; db < 4; ++db) o[db] *= down;
       }
       float p[16];
 #pragma unroll
@@ -505,7 +506,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
       for (int h = 0; h < 2; ++h) {
         const bf16x8a pb = pack_half(p, h);
 #pragma unroll
-        for (int db = 0; db < 4; ++db) o[db] = mfma(col_frag(tv, db, h, lane), pb, o[db]);
+        for (int db = 0; db < 4; ++db) o[db] = mfma(f.col(db, h, tv), pb, o[db]);
       }
     }
   }
@@ -539,7 +540,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(3))) vo
   constexpr int QB = NW * NB;
   constexpr int PW = 8 / NW;
   constexpr int STAGE = 2 * TILE16;  // key tile, value tile
-  __shared__ u32x4a smem[S * STAGE];
+  __shared__ __attribute__((aligned(256))) u32x4a smem[S * STAGE];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6));
   const int L = a.L;
@@ -575,6 +576,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(3))) vo
   }
   const float lse = a.lse[b * L + qc];
   float sum = 0.0f;
+  const LaneTile frags(smem, lane);
 #pragma unroll
   for (int i = 0; i < S - 1; ++i)
     if (i < walk.n) copy(i);
@@ -584,12 +586,12 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(3))) vo
     if (i + S - 1 < walk.n) copy(i + S - 1);
     const int t = walk.tile(i);
     if (t >= my_tiles || !(t * NB < a.sinks || t >= first_tile(q0, a.window))) continue;
-    const u32x4a* tk = smem + i % S * STAGE;
+    const LaneTile f = frags.at(uint32_t(i % S * STAGE * 16));
     f32x16a s = zero16(), dp = zero16();
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      s = mfma(row_frag(tk, j, lane), qf[j], s);
-      dp = mfma(row_frag(tk + TILE16, j, lane), df[j], dp);
+      s = mfma(f.row(j, 0), qf[j], s);
+      dp = mfma(f.row(j, TILE16 * 16), df[j], dp);
     }
 #pragma unroll
     for (int r = 0; r < 16; ++r) {

@@ -108,6 +108,40 @@ __device__ __forceinline__ bf16x8a col_frag(const u32x4a* tile, int db, int h, i
   return __builtin_bit_cast(bf16x8a, part);
 }
 
+// row_frag and col_frag for a loop over tiles of one array of stages (256-byte aligned): a lane's addresses
+// differ from its first one in single bits and in constants, which are the reads' own, so that a read costs
+// one instruction for its address in place of three.  `bytes`: of the tile in the stage, a constant.
+typedef __attribute__((address_space(3))) u32x4a lds_u32x4a;
+struct LaneTile {
+  uint32_t r, c;  // of k-step 0; of d block 0, half 0
+
+  __device__ __forceinline__ LaneTile(const u32x4a* smem, int lane) {
+    const uint32_t at = uint32_t(reinterpret_cast<uintptr_t>((lds_void_a*)smem));
+    const int i = lane & 15, g = lane >> 4, rho = 4 * (g >> 1) + (i >> 2);
+    r = at + uint32_t((lane & 31) * 256 + (((lane >> 5) ^ swz(lane & 31)) << 4));
+    c = at + uint32_t(rho * 256 + (((2 * (g & 1) + ((i & 3) >> 1)) ^ swz(rho)) << 4) + (i & 1) * 8);
+  }
+  // Of the stage that begins `bytes` behind the first one (opaque: 16 addresses are not held across the loop).
+  __device__ __forceinline__ LaneTile at(uint32_t bytes) const {
+    LaneTile t = *this;
+    t.r += bytes;
+    t.c += bytes;
+    asm volatile("" : "+v"(t.r), "+v"(t.c));
+    return t;
+  }
+  __device__ __forceinline__ bf16x8a row(int j, uint32_t bytes) const {
+    return __builtin_bit_cast(bf16x8a, *reinterpret_cast<const lds_u32x4a*>(uintptr_t((r ^ uint32_t(j << 5)) + bytes)));
+  }
+  __device__ __forceinline__ bf16x8a col(int db, int h, uint32_t bytes) const {
+    v4i16a part[2];
+#pragma unroll
+    for (int hh = 0; hh < 2; ++hh)
+      part[hh] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+          reinterpret_cast<lds_v4i16a*>(uintptr_t((c ^ uint32_t(hh << 5 | db << 6)) + (bytes + h * 4096 + hh * 2048))));
+    return __builtin_bit_cast(bf16x8a, part);
+  }
+};
+
 // Slots 8 h .. 8 h + 7 as a bf16 B operand.
 __device__ __forceinline__ bf16x8a pack_half(const float (&v)[16], int h) {
   bf16x8a w;
