@@ -646,10 +646,12 @@ uq_status uniquan_attn_bwd(int64_t batch, int64_t kv_batch, int L, int d,
  * uniquan_attn_window_fwd / uniquan_attn_window_bwd -- uniquan_attn_fwd / _bwd with a
  * sliding window and a few first positions always in sight: query i sees the keys
  * j <= i with i - j < window or j < sinks, and only the tiles that hold one of them
- * are walked.  Formulas, layouts and outputs as there, but that P enters dS before
- * it is rounded: dS = bf16(2^(c S - row_lse) (dP - delta)), and that delta is
- * sum_j P_ij dP_ij (fp32; O is not read).  window >= 1, sinks >= 0
- * (window >= L: the causal attention); any L >= 1 (up to 2^22, batch ceil(L / 128) at
+ * are walked.  Formulas, layouts and outputs as there, but that the forward's weights
+ * may be rounded to bf16 as 2^(c S - m), m a running maximum, and O divided by their
+ * unrounded sum; that P enters dS before it is rounded: dS = bf16(2^(c S - row_lse)
+ * (dP - delta)); and that delta is sum_j P_ij dP_ij (fp32; O is not read).
+ * window >= 1, sinks >= 0 (window or sinks >= L: the causal attention, the forward's
+ * results its own where it takes that L); any L >= 1 (up to 2^22, batch ceil(L / 128) at
  * most 2^22); scale positive and finite.  Q, K, V, dO have to be finite: a key outside
  * a query's sight has weight 0, not no part.
  */
@@ -937,7 +939,7 @@ uq_status uniquan_attn_decode(int64_t n_seq, int H, int H_kv, int d,
  * where a row sees nothing, what it does not see has no influence whatever it
  * is, and the same limits on values, scales, offsets and queries hold.  Where a
  * sequence's rows and the query heads of a key/value head come to more than 16 on
- * average (ceil(T / n_seq) H / H_kv), a weight times the group's scale is rounded
+ * average (ceil(T / n_seq) H / H_kv), a weight times the group's scale may be rounded
  * once to bf16 (2^-8 of it at most), else it is two bf16 terms.  Rows behind
  * row_start[n_seq] are padding: their O and row_lse are left as they were.
  * Results do not change from run to run.

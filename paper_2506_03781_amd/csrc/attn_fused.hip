@@ -412,18 +412,19 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(KS
 }
 
 // A window's forward in one walk: weights against a running maximum that moves only
-// when a score exceeds it by SLACK_W, rounded to bf16 for the product with V, their
-// sum unrounded.  Two key tiles and their values a stage: half the barriers.  (The
-// causal forward's two walks, one for the log-sum-exp, took 182 us in place of 141 for 4
-// x 2048 rows of 32 heads in a window of 512.  It remains where walks are split, and
-// for a window over everything, whose results are the causal call's bit for bit.)
+// when a score exceeds it by SLACK_W (in powers of 2), rounded to bf16 for the
+// product with V, their sum unrounded.  166 registers and 32 KB of stages: three
+// waves per SIMD (two, with two tiles a stage: 141 us in place of 127 for 4 x 2048
+// rows of 32 heads in a window of 512).  The causal forward's two walks, one for the
+// log-sum-exp, took 182; they remain where walks are split, and for a window over
+// everything, whose results are the causal call's bit for bit.
 constexpr float SLACK_W = 8.0f;
 template <int NW, bool TOK>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) void attn_window_fwd_kernel(AttnArgs a) {
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(3))) void attn_window_fwd_kernel(AttnArgs a) {
   constexpr int QB = NW * NB;
   constexpr int PW = 8 / NW;
   constexpr int TILE = 2 * TILE16;  // key tile, value tile
-  __shared__ __attribute__((aligned(256))) u32x4a smem[2][2 * TILE];
+  __shared__ __attribute__((aligned(256))) u32x4a smem[2][TILE];
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(int(threadIdx.x >> 6));
   const int L = a.L;
@@ -442,12 +443,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
 #pragma unroll
   for (int q = 0; q < PW; ++q) ro[q] = row_off(wave * PW + q, lane);
   auto copy = [&](int i, u32x4a* st) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int at = walk.tile(min(i + t, walk.n - 1));  // (past the end the last tile again, unused)
-      copy_rows<true, PW>(Kb + int64_t(at) * NB * D, ro, st + t * TILE, wave, lane, D, L - at * NB);
-      copy_rows<true, PW>(Vb + int64_t(at) * NB * D, ro, st + t * TILE + TILE16, wave, lane, D, L - at * NB);
-    }
+    const int t = walk.tile(i);
+    copy_rows<true, PW>(Kb + int64_t(t) * NB * D, ro, st, wave, lane, D, L - t * NB);
+    copy_rows<true, PW>(Vb + int64_t(t) * NB * D, ro, st + TILE16, wave, lane, D, L - t * NB);
   };
   bf16x8a qf[8];
   {
@@ -460,54 +458,50 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
   copy(0, smem[0]);
   const LaneTile frags(smem[0], lane);
   int cur = 0;
-  for (int i = 0; i < walk.n; i += 2, cur ^= 1) {
+  for (int i = 0; i < walk.n; ++i, cur ^= 1) {
     vm_wait<0>();
     lds_wait_barrier();
-    if (i + 2 < walk.n) copy(i + 2, smem[cur ^ 1]);
+    if (i + 1 < walk.n) copy(i + 1, smem[cur ^ 1]);
+    const int t = walk.tile(i);
+    if (t >= my_tiles || !(t * NB < a.sinks || t >= first_tile(q0, a.window))) continue;
+    const LaneTile f = frags.at(cur * uint32_t(sizeof(smem[0])));
+    constexpr uint32_t VALUES = TILE16 * 16;
+    f32x16a s = zero16();
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      if (i + u >= walk.n) break;
-      const int t = walk.tile(i + u);
-      if (t >= my_tiles || !(t * NB < a.sinks || t >= first_tile(q0, a.window))) continue;
-      const LaneTile f = frags.at(cur * uint32_t(sizeof(smem[0])));
-      const uint32_t tk = u * TILE * 16, tv = tk + TILE16 * 16;
-      f32x16a s = zero16();
+    for (int j = 0; j < 8; ++j) s = mfma(f.row(j, 0), qf[j], s);
+    if (t == my_tiles - 1 || (q0 + NB - 1 - t * NB >= a.window && (t + 1) * NB > a.sinks)) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) s = mfma(f.row(j, tk), qf[j], s);
-      if (t == my_tiles - 1 || (q0 + NB - 1 - t * NB >= a.window && (t + 1) * NB > a.sinks)) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int j = t * NB + slot_row(r, lane);
-          if (j > qi || (qi - j >= a.window && j >= a.sinks)) s[r] = -INFINITY;
-        }
+      for (int r = 0; r < 16; ++r) {
+        const int j = t * NB + slot_row(r, lane);
+        if (j > qi || (qi - j >= a.window && j >= a.sinks)) s[r] = -INFINITY;
       }
-      float mx = s[0];
+    }
+    float mx = s[0];
 #pragma unroll
-      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
-      {
-        const uint32_t x = __float_as_uint(mx);
-        const auto y = __builtin_amdgcn_permlane32_swap(x, x, false, false);
-        mx = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1])) * c;
-      }
-      if (__any(mx > m + SLACK_W)) {
-        const float m1 = mx > m + SLACK_W ? mx : m;
-        const float down = exp2a(m - m1);
-        m = m1;
-        l *= down;
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+    {
+      const uint32_t x = __float_as_uint(mx);
+      const auto y = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+      mx = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1])) * c;
+    }
+    if (__any(mx > m + SLACK_W)) {
+      const float m1 = mx > m + SLACK_W ? mx : m;
+      const float down = exp2a(m - m1);
+      m = m1;
+      l *= down;
 #pragma unroll
-        for (int db = 0; db < 4; ++db) o[db] *= down;
-      }
-      float p[16];
+      for (int db = 0; db < 4; ++db) o[db] *= down;
+    }
+    float p[16];
 #pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = exp2a(fmaf(s[r], c, -m));
-      l += (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]))) +
-           (((p[8] + p[9]) + (p[10] + p[11])) + ((p[12] + p[13]) + (p[14] + p[15])));
+    for (int r = 0; r < 16; ++r) p[r] = exp2a(fmaf(s[r], c, -m));
+    l += (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]))) +
+         (((p[8] + p[9]) + (p[10] + p[11])) + ((p[12] + p[13]) + (p[14] + p[15])));
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const bf16x8a pb = pack_half(p, h);
+    for (int h = 0; h < 2; ++h) {
+      const bf16x8a pb = pack_half(p, h);
 #pragma unroll
-        for (int db = 0; db < 4; ++db) o[db] = mfma(f.col(db, h, tv), pb, o[db]);
-      }
+      for (int db = 0; db < 4; ++db) o[db] = mfma(f.col(db, h, VALUES), pb, o[db]);
     }
   }
   l += __shfl_xor(l, 32, 64);
@@ -534,7 +528,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
 // and with keys whose mean is not 0 (channels of outliers) it was the largest error
 // of dQ by far (4 x 2048 rows, 32 heads, window 512, one channel of the keys ten
 // times the others: dQ off by 4.0e-3 of its norm and by up to 0.66 of an element's
-// size, now 3.2e-3 and 0.25; the walk takes 147 of 924 us).
+// size, now 3.2e-3 and 0.25; the walk takes 124 of 725 us).
 template <int NW, int S, bool TOK>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(3))) void attn_window_delta_kernel(AttnArgs a) {
   constexpr int QB = NW * NB;
