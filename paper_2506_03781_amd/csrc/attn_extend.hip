@@ -14,11 +14,12 @@
 // attention (attn_decode.hip): S^T = K Q^T and O^T += V^T P^T with the heads as
 // columns, K and V straight from the cache into registers, codes fed as they are;
 // a workgroup's wavefronts take every fourth step.  Bound by the loads: 64 x 8 rows
-// over 8192 positions of 8 heads in bf16 (2.2 GB) in 382 us, 5.7 TB/s.
+// over 8192 positions of 8 heads in bf16 (2.2 GB) in 374 us, 5.8 TB/s.
 // Many columns (attn_extend_wide_kernel: 128).  Tiles of keys and values in LDS, read
-// by four wavefronts with 32 columns each.  Bound by the products and the weights
-// between them: 2 x 2048 rows behind 6144 positions, 32 heads over 8, in 640 us,
-// 750 TFLOP/s.  columns_of says which is taken where.
+// by four wavefronts with 32 columns each.  A wavefront's products wait for its weights
+// and the other way round, and 64 KB of tiles and 256 registers leave two wavefronts a
+// SIMD to cover that: 2 x 2048 rows behind 6144 positions, 32 heads over 8, in 606 us,
+// 795 TFLOP/s.  columns_of says which is taken where.
 //
 // What is seen.  A step in which some column does not see all 32 positions (its
 // own end, a window's edge, a tree's drafts, the end of the sequence or a missing
@@ -1102,9 +1103,9 @@ __global__ __launch_bounds__(256) void attn_extend_join_kernel(AttnExtendLaunch 
 
 // Columns of a workgroup, for those that a sequence has on average: 16, 32, and of heads of 128 channels WIDE
 // (us, 24 sequences of 8192 positions, 8 key/value heads, with 16 | 32 | 128 columns):
-//   32 columns:  bf16 199 | 180 | 243,  u8 133 | 112 | -,    u8 in groups of 32 183 | 361 | 332
-//   64 columns:  bf16   - | 223 | 262,                       u8 in groups of 32 262 | 552 | 329
-//   128 columns: bf16 515 | 297 | 241,  u8 346 | 247 | 276,  u8 in groups of 32 444 | 957 | 342
+//   32 columns:  bf16 185 | 171 | 225,  u8 113 | 103 | -,    u8 in groups of 32 144 | 361 | 296
+//   64 columns:  bf16 264 | 185 | 212,  u8 178 | 124 | -,    u8 in groups of 32 235 | 552 | 315
+//   128 columns: bf16 474 | 275 | 229,  u8 317 | 202 | 276,  u8 in groups of 32 423 | 957 | 338
 // Two column tiles and the statistics of four groups do not fit into the registers.
 enum Kind { PLAIN, ONE_GROUP, GROUPS };
 constexpr Kind kind_of(int fmt, int ng) { return fmt == KV_BF16 ? PLAIN : ng == 1 ? ONE_GROUP : GROUPS; }

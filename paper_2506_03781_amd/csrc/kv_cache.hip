@@ -13,7 +13,9 @@
 // rotary partners D / 2 further on, whose eight (cos, sin) pairs it keeps for
 // all its heads; a group of 32 channels is one half of four lanes.  Values
 // that become codes take 16 lanes, a lane the channels l + 16 c that lie side
-// by side in the row.
+// by side in the row.  With positions of several axes apart from the place
+// (AXES) a lane looks up an angle for each of its pairs in place of a run of them:
+// 8000 rows of 32 + 8 + 8 heads of a video 33.5 us in bf16, 197 MB at 5.9 TB/s.
 //
 // Read.  A wavefront takes 16 positions of one head of one sequence, which lie
 // on two pages at most, a lane 16 bytes of the output of several.  Its codes of a key are one word (two);
