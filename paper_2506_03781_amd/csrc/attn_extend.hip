@@ -19,7 +19,8 @@
 // by four wavefronts with 32 columns each.  A wavefront's products wait for its weights
 // and the other way round, and 64 KB of tiles and 256 registers leave two wavefronts a
 // SIMD to cover that: 2 x 2048 rows behind 6144 positions, 32 heads over 8, in 606 us,
-// 795 TFLOP/s.  columns_of says which is taken where.
+// 795 TFLOP/s.  columns_of says which is taken where; with four sequences or more, those
+// of few columns among many have the first kernel's tiles beside the second's.
 //
 // What is seen.  A step in which some column does not see all 32 positions (its
 // own end, a window's edge, a tree's drafts, the end of the sequence or a missing
@@ -69,7 +70,10 @@ template <int COLS>
 struct Work {
   const AttnExtendLaunch& p;
   int G;  // query heads of a key/value head
-  __device__ __forceinline__ int tiles(const Seq& s) const { return int((int64_t(s.m) * G + COLS - 1) / COLS); }
+  __device__ __forceinline__ int tiles(const Seq& s) const {
+    const int64_t cols = int64_t(s.m) * G;
+    return cols < p.from_cols || cols > p.to_cols ? 0 : int((cols + COLS - 1) / COLS);
+  }
   // steps that a tile's rows see, about
   __device__ __forceinline__ int steps(const Seq& s) const {
     const int all = (capped(p, s.len) + STEP - 1) / STEP;
@@ -1128,6 +1132,16 @@ int target_of(int64_t T, int64_t n_seq, int H, int H_kv, int cols, int64_t max_p
   return int(4 * tiles <= holds || tiles >= holds ? holds : 2 * holds);
 }
 
+// Where sequences have more than 64 columns on average, those with few have a launch of the smaller tiles to
+// themselves (single tokens beside a prompt), up to few_of columns, in so many shares.  One prompt of 512 rows and
+// single tokens, 8192 positions each, 32 heads over 8: 31 tokens in bf16 366 -> 334 us, of 8 bits in groups of 32
+// 632 -> 367; 7 tokens 198 -> 165 and 325 -> 222.  Sequences alike pay the empty launches (8 x 128 rows 225 -> 230 us,
+// 359 -> 370), so that fewer than four go without.
+int few_of(Kind f) { return f == PLAIN ? 16 : 64; }
+int target_of_few(int64_t n_seq, int H_kv, int64_t max_pages, int page_len) {
+  return n_seq < 4 || max_pages * page_len <= MIN_STEPS * STEP ? 0 : std::max(1, 2 * CUS / H_kv);
+}
+
 template <int D, int COLS>
 hipError_t launch_join(const AttnExtendLaunch& p, int target, float back, hipStream_t st) {
   constexpr int LANES = D / 4;
@@ -1149,9 +1163,19 @@ hipError_t launch_form(const AttnExtendLaunch& p, hipStream_t st) {
   const float back = FMT == KV_BF16 ? BF16_BACK : 1.0f;
   if constexpr (D == 128 && KIND != ONE_GROUP) {
     if (cols == WIDE) {
-      attn_extend_wide_kernel<FMT, NG><<<grid, 256, 0, st>>>(p, target);
+      AttnExtendLaunch many = p, few = p;
+      const int few_target = target_of_few(p.c.n_seq, H_kv, p.c.max_pages, p.c.page_len);
+      if (few_target) many.from_cols = (few.to_cols = few_of(KIND)) + 1;
+      attn_extend_wide_kernel<FMT, NG><<<grid, 256, 0, st>>>(many, target);
       if (hipError_t e = hipGetLastError()) return e;
-      return target ? launch_join<D, WIDE>(p, target, 1.0f, st) : hipSuccess;
+      if (few_target) {
+        const int64_t n = std::min(p.T, p.c.n_seq) * (few_of(KIND) / 16);
+        few.ws = p.ws + size_t(target) * size_t(H_kv) * WIDE * (D + 4);
+        attn_extend_kernel<FMT, D, NG, 1><<<grid_of((n + few_target) * H_kv), 256, 0, st>>>(few, few_target);
+        if (hipError_t e = hipGetLastError()) return e;
+        if (hipError_t e = launch_join<D, 16>(few, few_target, back, st)) return e;
+      }
+      return target ? launch_join<D, WIDE>(many, target, 1.0f, st) : hipSuccess;
     }
   }
   if constexpr (D == 64 || KIND != GROUPS) {
@@ -1180,12 +1204,15 @@ size_t attn_extend_ws(int64_t T, int64_t n_seq, int H, int H_kv, int d, int64_t 
   size_t most = 0;  // of all formats
   for (const Kind f : {PLAIN, ONE_GROUP, GROUPS}) {
     const int cols = columns_of(T, n_seq, H, H_kv, d, f);
-    most = std::max(most, size_t(target_of(T, n_seq, H, H_kv, cols, max_pages, page_len)) * size_t(cols));
+    const size_t few = cols == WIDE ? size_t(target_of_few(n_seq, H_kv, max_pages, page_len)) * 16 : 0;
+    most = std::max(most, size_t(target_of(T, n_seq, H, H_kv, cols, max_pages, page_len)) * size_t(cols) + few);
   }
   return most * size_t(H_kv) * size_t(d + 4);
 }
 
-hipError_t launch_attn_extend(const AttnExtendLaunch& p, hipStream_t st) {
+hipError_t launch_attn_extend(AttnExtendLaunch p, hipStream_t st) {
+  p.from_cols = 0;
+  p.to_cols = INT64_MAX;
   return p.c.d == 128 ? launch_d<128>(p, st) : launch_d<64>(p, st);
 }
 

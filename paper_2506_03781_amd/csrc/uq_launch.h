@@ -250,6 +250,7 @@ struct AttnExtendLaunch {
   uint16_t* O; int64_t ld_o;
   float* lse;
   float* ws;
+  int64_t from_cols, to_cols;       // sequences with as many columns (rows times H / H_kv) are taken
 };
 struct SampleLaunch {
   int64_t T;
@@ -261,7 +262,7 @@ struct SampleLaunch {
   void* ws;
   int sh;  // weights count in 2^-sh
 };
-hipError_t launch_attn_extend(const AttnExtendLaunch& p, hipStream_t st);
+hipError_t launch_attn_extend(AttnExtendLaunch p, hipStream_t st);
 size_t attn_extend_ws(int64_t T, int64_t n_seq, int H, int H_kv, int d, int64_t max_pages, int page_len);
 hipError_t launch_sample(SampleLaunch p, hipStream_t st);
 size_t sample_ws(int64_t T, int64_t V);

@@ -110,6 +110,22 @@ def test_many_tiles(fmt, group, d):
     X.check(c, on_device(c), q, start, lens, 0.125, what="holes")
 
 
+@pytest.mark.parametrize("fmt,group", FORMS)
+@pytest.mark.parametrize("n_kv,grp,rows", [(2, 4, (300, 1, 16, 17, 1, 0, 4, 5)), (1, 1, (1, 16, 17, 64, 65, 600, 0, 128)),
+                                           (3, 8, (1, 2, 3, 8, 9, 150))])
+def test_a_prompt_beside_single_tokens(fmt, group, n_kv, grp, rows):
+    """Sequences of many and of few rows in one call (more than 64 columns on average; up to 16, or of codes in groups of
+    32 up to 64, have tiles of their own), lengths of which some are cut into shares."""
+    lens = [2500, 1999, 700, 33, 1, 40, 900, 1300][:len(rows)]
+    seqs = [(r, max(r, ln)) for r, ln in zip(rows, lens)]
+    assert -(-sum(rows) // len(rows)) * grp > 64
+    rs, c, m, q, start, lens = case(seqs, n_kv, grp, 128, 32, fmt, group)
+    X.check(c, m, q, start, lens, 0.09, what="rows")
+    X.check(c, m, q, start, lens, 0.09, window=300, sinks=3, what="window")
+    path = sum((X.tree(rs, r, back=40)[1] for r, _ in seqs), [])
+    X.check(c, m, q, start, lens, 0.09, mask=path, words=10, what="trees")
+
+
 def test_many_sequences():
     """More sequences than lanes, in runs of several a lane."""
     rs = np.random.default_rng(5)
