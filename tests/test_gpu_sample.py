@@ -94,6 +94,20 @@ def test_many_equal_values(values):
     check(x, u, top_k=[15000, 9000, 4097, 7000, 12345, 19999, 300, 1], top_p=[0.5, 0.9, 0.3, 0.99, 0.01, 0.7, 0.6, 0.5])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("values", [1, 3])
+def test_the_last_token_kept(values, dtype):
+    """u = 1: the last one by index of those that stay, at cuts in every place of a chunk, in rows of every alignment."""
+    rs = np.random.default_rng(values)
+    V = 9001
+    x = dev(rs.integers(0, values, (16, V)) * 0.25, dtype)
+    k = 5000 + np.arange(16)
+    check(x, np.ones(16, np.float32), top_k=k)
+    check(x, np.ones(16, np.float32), top_k=k + 3000, top_p=[0.6] * 16)
+    if values == 1:
+        assert np.array_equal(call(x, np.ones(16), top_k=k)[0], k - 1)
+
+
 def test_neighbouring_values_in_one_bin():
     """Values a few steps of fp32 apart: the cut is found among them."""
     rs = np.random.default_rng(11)
