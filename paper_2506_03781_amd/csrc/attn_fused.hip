@@ -417,7 +417,7 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(KS
 // waves per SIMD (two, with two tiles a stage: 141 us in place of 127 for 4 x 2048
 // rows of 32 heads in a window of 512).  The causal forward's two walks, one for the
 // log-sum-exp, took 182; they remain where walks are split, and for a window over
-// everything, whose results are the causal call's bit for bit.
+// everything, whose walks are the causal call's (and its results, split alike).
 constexpr float SLACK_W = 8.0f;
 template <int NW, bool TOK>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(3))) void attn_window_fwd_kernel(AttnArgs a) {
@@ -988,7 +988,7 @@ hipError_t launch_attn_fwd(const AttnLaunch& q, hipStream_t st) {
   set_tok(a, q);
   const int nblk = (q.L + NW * NB - 1) / (NW * NB);
   const bool split = splits(q, nblk);
-  if (q.window > 0 && std::max(q.window, q.sinks) < q.L && !split) {  // (a window over everything keeps the causal call's results)
+  if (q.window > 0 && std::max(q.window, q.sinks) < q.L && !split) {  // (a window over everything: as the causal call)
     launch(q.tok_seqs > 0 ? attn_window_fwd_kernel<NW, true> : attn_window_fwd_kernel<NW, false>, nblk * q.batch, 1, a, st);
     return hipGetLastError();
   }
