@@ -14,6 +14,7 @@
 //   top-k of up to ENOUGH: the k-th best of the lanes' best tokens is a value that k
 //              tokens reach at least, and few more.  They are gathered in LDS, and
 //              everything else happens there.
+//   min-p      alike, where the lanes' best tokens say that few are left.
 //   histogram  (top-p, larger k) counts and sums of weights in BINS equal steps of
 //              (max - x) / t: its running sums say in which bin the k-th token lies
 //              and in which the nucleus ends.  A nucleus of up to CAP tokens is
@@ -594,6 +595,31 @@ __device__ __forceinline__ Before histogram(Lds& s, const Row<F32>& row, const W
   return bins_before<true>(s, total);
 }
 
+// Sum of the lane's weights of the tokens up to end_x, end_i in order, in a row without +infinity: what is behind
+// counts as -infinity, and four chains have no branch (one after the other, with the tests of the general case, 256 x
+// 131072 logits took 55 us in place of 37).
+template <bool F32>
+__device__ __forceinline__ u64 mass_upto(const Row<F32>& row, const Weigh& w, int of, int i0, int i1, float end_x, int end_i) {
+  const float past_x = uni(value_of(key_of(end_x) - 1));  // the next larger value
+  u64 sum = 0;
+  uint32_t n = 0;
+  over_fours(row, of, i0, i1, end_x, [&](const float (&x)[4], int i) {
+    const float least_x = i <= end_i ? end_x : past_x;
+    float y[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = x[e] >= least_x ? x[e] : -__builtin_inff();
+    if (i <= end_i && end_i < i + 3) {
+#pragma unroll
+      for (int e = 1; e < 4; ++e) y[e] = i + e <= end_i || x[e] > end_x ? y[e] : -__builtin_inff();
+    }
+    u64 v[4];
+    w.biased(y, v);
+    sum += (v[0] + v[1]) + (v[2] + v[3]);
+    n += 4;
+  });
+  return sum - n * Weigh::BIAS;
+}
+
 // floor(u total) for u in [0, 1); the last unit from 1 on.
 __device__ __forceinline__ u64 part_of(float u, u64 total) {
   if (!(u > 0.0f)) return 0;
@@ -609,10 +635,10 @@ __device__ __forceinline__ u64 border_of(float p, u64 total) {
 }
 
 // The answer from the gathered tokens, if they are not too many and hold all that
-// stays.  total: the weights' sum over the row where top-k is off.
+// stays.  total: the weights' sum over the row where top-k is off; all: they do, by min_p.
 template <typename Answer>
 __device__ __forceinline__ bool answer_of_list(Lds& s, const Weigh& w, uint32_t k, float top_p, u64 least, u64 total,
-                                               float u, Answer answer) {
+                                               bool all, float u, Answer answer) {
   const uint32_t n = uni(s.n);
   if (n > CAP) return false;
   if (threadIdx.x == 0) s.found[0] = 0;
@@ -621,7 +647,7 @@ __device__ __forceinline__ bool answer_of_list(Lds& s, const Weigh& w, uint32_t 
   if (first && (!k || t.rank < k)) atomicMax(&s.found[0], t.before + t.mine);
   __syncthreads();
   const u64 held = s.found[0], border = top_p < 1.0f ? border_of(top_p, k ? held : total) : ~u64(0);
-  if (top_p < 1.0f && border > held) return false;
+  if (top_p < 1.0f && border > held && !all) return false;
   const bool stays = t.is && (!k || t.rank < k) && t.before < border && t.mine >= least;
   u64 place = t.place, mine = stays ? t.mine : 0, upto = 0, sum = 0;
   if (n > FEW) {  // by index, what does not stay behind
@@ -707,9 +733,22 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleLaunch p) {
   const float min_p = p.min_p ? p.min_p[t] : 0.0f;
   const u64 least = uni(min_p > 0.0f ? u64(ceil(ldexp(fmin(double(min_p), 1.0), p.sh))) : u64(0));
 
+  // By min_p few tokens stay, and they are gathered right away (with the weights' sum over the row, where top-p asks
+  // for it): rows of 131072 with top-p 115-138 us, so 50.  The lanes that have one say about how many there are: of
+  // 1024 tokens anywhere six in ten lanes.
+  bool listed = false;
+  if (least && !w.endless && (!k || (k > ENOUGH && !(top_p < 1.0f)))) {
+    const float at = w.top + __builtin_amdgcn_logf(fminf(min_p, 1.0f)) / float(w.per_t);
+    const float from = w.floor_of(std::min(w.bin(at), BINS - 2));
+    if (__syncthreads_count(own >= from) <= THREADS / 2) {
+      gather(s, row, w, from, [](float) { return true; });
+      listed = uni(s.n) <= CAP;
+    }
+  }
+
   int last_bin = BINS;     // tokens of bins below it are kept,
   u64 last = ~u64(0);      // of its own those up to this place
-  if (k || top_p < 1.0f) {
+  if (!listed && (k || top_p < 1.0f)) {
     u64 total = 0, m0 = 0;
     uint32_t c0 = 0;
     // The k-th best of the lanes' best values is one that k tokens reach at least, and few more: with top-k they
@@ -727,7 +766,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleLaunch p) {
         if (b <= end) atomicMax(&s.hi, key_of(own));
         __syncthreads();
         gather(s, row, w, uni(value_of(s.hi)), [](float) { return true; });
-        if (answer_of_list(s, w, k, top_p, least, total, p.u[t], answer)) return;
+        if (answer_of_list(s, w, k, top_p, least, total, false, p.u[t], answer)) return;
       }
     }
     Before r = histogram(s, row, w, total);
@@ -735,7 +774,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleLaunch p) {
       const int end = bin_of_cut(s, r, Cut{true, 0, border_of(top_p, total)}, c0, m0);
       if (c0 + s.count[end] <= CAP) {
         gather(s, row, w, w.floor_of(end), [&](float x) { return w.bin(x) <= end; });
-        if (answer_of_list(s, w, k, top_p, least, total, p.u[t], answer)) return;
+        if (answer_of_list(s, w, k, top_p, least, total, false, p.u[t], answer)) return;
       }
     }
     u64 kept = total;  // sum of the top k
@@ -748,7 +787,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleLaunch p) {
       __syncthreads();
       if (top_p < 1.0f && c0 + n > k) {
         // The bin in which the nucleus of the top k ends is known before their sum is, nearly always: both bins'
-        // tokens are gathered at once (256 x 131072 with mixed settings 196 us, now 173).
+        // tokens are gathered at once, one pass of 22 us less over a row of 131072.
         uint32_t c1;
         u64 m1;
         const int pb = bin_of_cut(s, r, Cut{true, 0, std::max<u64>(border_of(top_p, m0), 1)}, c1, m1);
@@ -804,33 +843,13 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleLaunch p) {
     if (least) v = v >= least ? v : 0;
     return stays ? v : 0;
   };
-  // Sum of the weights that stay.  Nearly all rows': of the tokens up to one of them in order, what is behind it
-  // counted as -infinity; four chains without a branch (one after the other, with the tests of the general case,
-  // took 55 us in place of 37 for 256 x 131072 tokens).
-  const bool simple = !w.endless && !least && (last_bin == BINS || last != ~u64(0));
+  // nearly all rows keep the tokens up to one of them in order
+  const bool simple = !w.endless && (listed || !least) && (last_bin == BINS || last != ~u64(0));
   const float end_x = last_bin < BINS ? value_of(uint32_t(last >> 32)) : -__builtin_inff();
-  const float past_x = uni(value_of(key_of(end_x) - 1));  // the next larger value
   const int end_i = last_bin < BINS ? int(uint32_t(last)) : 0x7FFFFFFF;
   auto sum_of = [&](int of, int i0, int i1) {
+    if (simple) return mass_upto(row, w, of, i0, i1, end_x, end_i);
     u64 sum = 0;
-    if (simple) {
-      uint32_t n = 0;
-      over_fours(row, of, i0, i1, end_x, [&](const float (&x)[4], int i) {
-        const float least_x = i <= end_i ? end_x : past_x;
-        float y[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) y[e] = x[e] >= least_x ? x[e] : -__builtin_inff();
-        if (i <= end_i && end_i < i + 3) {
-#pragma unroll
-          for (int e = 1; e < 4; ++e) y[e] = i + e <= end_i || x[e] > end_x ? y[e] : -__builtin_inff();
-        }
-        u64 v[4];
-        w.biased(y, v);
-        sum += (v[0] + v[1]) + (v[2] + v[3]);
-        n += 4;
-      });
-      return sum - n * Weigh::BIAS;
-    }
     over_part(row, of, i0, i1, chunks_from, [&](float x, int i) { sum += weight(x, i); });
     return sum;
   };
@@ -839,9 +858,13 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleLaunch p) {
   for (bool first = true; first || n > 1; first = false) {
     const int each = first ? row.per : (n + WAVES - 1) / WAVES;
     const int i0 = first ? 0 : at0 + std::min(wave * each, n), i1 = first ? row.per : at0 + std::min((wave + 1) * each, n);
-    const u64 sum = wave_sum(sum_of(first ? wave : of, i0, i1));
+    const u64 sum = listed && !(top_p < 1.0f) ? 0 : wave_sum(sum_of(first ? wave : of, i0, i1));
     if (first) {
       block_before(s, lane ? 0 : sum, all);
+      if (listed) {
+        answer_of_list(s, w, k, top_p, least, all, true, p.u[t], answer);
+        return;
+      }
       left = part_of(p.u[t], all);
     }
     const int v = pick(s, sum, left, left);

@@ -95,6 +95,29 @@ def test_many_equal_values(values):
 
 
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [3001, 20011])
+def test_min_p_beside_the_others(V, dtype):
+    """Few or many tokens left by min_p, alone, with top_p and with a large top_k; the last token kept too (u = 1)."""
+    rs = np.random.default_rng(V)
+    x = logits(rs, 12, V)
+    x[3] = 0.5                                # all alike
+    x[4, 100:] = -np.inf
+    x[5, 7] = np.inf
+    x[6, ::3] = np.nan
+    x = dev(x, dtype)
+    lo = np.array([0.3, 0.05, 1e-3, 0.5, 0.2, 0.1, 0.05, 1e-6, 1.0, 3e-2, 1e-30, 1e-45], np.float32)
+    p = rs.uniform(0.2, 1.0, 12).astype(np.float32)
+    k = rs.integers(513, V, 12)
+    t = rs.uniform(0.4, 1.5, 12).astype(np.float32)
+    t[10] = np.inf
+    for u in (rs.random(12).astype(np.float32), np.ones(12, np.float32)):
+        check(x, u, temperature=t, min_p=lo)
+        check(x, u, temperature=t, min_p=lo, top_p=p)
+        check(x, u, temperature=t, min_p=lo, top_k=k)
+        check(x, u, temperature=t, min_p=lo, top_k=k, top_p=p)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("values", [1, 3])
 def test_the_last_token_kept(values, dtype):
     """u = 1: the last one by index of those that stay, at cuts in every place of a chunk, in rows of every alignment."""
