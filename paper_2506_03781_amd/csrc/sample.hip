@@ -528,7 +528,7 @@ __device__ __forceinline__ u64 cut_bin(Lds& s, const Row<F32>& row, const Weigh&
     u64 r = cut.by_mass ? (one ? (cut.mass + one - 1) / one : n) : cut.count;
     r = r < n ? r : n;
     mass += r * one;
-    if (r == n) return ~u64(0);
+    if (r == n) return u64(lo) << 32 | 0x7FFFFFFFu;  // all of them (the bin may hold lower values: behind any index)
     // how many lie in each wavefront's share of the indices, then in each of its chunk groups
     const float only = value_of(lo);
     auto same = [&](float x) { return clean(w.seen(x)) == only; };

@@ -1,0 +1,91 @@
+"""uniquan_sample where its cuts change hands: at the end of a run of equal values that shares its bin with worse ones,
+at the sizes where the kernel gathers, ranks, sorts or counts, and at the least top-p.  Bars as in test_gpu_sample."""
+import numpy as np
+import pytest
+import torch
+
+from oracle.sample import shift, weights
+from test_gpu_sample import check, dev
+
+pytestmark = pytest.mark.gpu
+
+
+def runs(rs, values, counts, V):
+    """A row of V logits: counts[i] copies of values[i], the others of the last value, shuffled."""
+    x = np.full(V, values[-1], np.float32)
+    at = 0
+    for v, n in zip(values, counts):
+        x[at:at + n] = v
+        at += n
+    return rs.permutation(x)
+
+
+def border_in_last(x, t, n, V=None):
+    """The top-p that falls in the middle of the weight of the n-th token in order (x: the row of V, or its top k)."""
+    w = sorted(weights(x, np.float32(t), shift(V or len(x))), reverse=True)
+    return np.float32((sum(w[:n - 1]) + 0.5 * w[n - 1]) / sum(w))
+
+
+def steps_below(x, n, dtype):
+    """The value n steps of the type below x > 0."""
+    if dtype == torch.float32:
+        return (np.float32(x).view(np.int32) - np.int32(n)).view(np.float32)
+    return (np.float32(x).view(np.int32) - np.int32(n << 16)).view(np.float32)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("counts", [(2000,), (1500, 2000), (1025, 1030, 3000), (1024, 2000)])
+def test_a_cut_at_the_end_of_a_run_of_equal_values(counts, dtype):
+    """The first 1, 2 ... of the runs, and one token less and more, by top-k, by top-p and by both; values a step of the
+    type apart (all in one bin, bf16 at a temperature of 200), alone and behind better tokens in bins before."""
+    rs = np.random.default_rng(sum(counts))
+    V, t, high = (10007, 1.0, 4.0) if dtype == torch.float32 else (10007, 200.0, 512.0)
+    values = [steps_below(1.0, i, dtype) for i in range(len(counts) + 1)]
+    x, k, p, both = [], [], [], []
+    for better in (0, 30):
+        for end in better + np.cumsum(counts):
+            for n in (int(end) - 1, int(end), int(end) + 1):
+                row = runs(rs, [high, *values], [better, *counts], V)
+                more = min(V, n + 700)
+                x.append(row)
+                k.append(n)
+                p.append(border_in_last(row, t, n))
+                both.append((more, border_in_last(-np.sort(-row)[:more], t, n, V)))
+    T = len(x)
+    xs = dev(np.stack(x), dtype)
+    for u in (np.ones(T, np.float32), rs.random(T).astype(np.float32)):
+        check(xs, u, temperature=[t] * T, top_k=k)
+        check(xs, u, temperature=[t] * T, top_p=p)
+        check(xs, u, temperature=[t] * T, top_k=[b[0] for b in both], top_p=[b[1] for b in both])
+        check(xs, u, temperature=[t] * T, top_k=k, min_p=[0.5] * T)
+
+
+def test_a_cut_at_the_end_of_a_run_of_infinities():
+    """Of 3000 logits of +infinity the first 2999, all, and no more than all."""
+    rs = np.random.default_rng(1)
+    x = np.stack([runs(rs, [np.float32(np.inf), np.float32(1.0)], [3000], 9000) for _ in range(6)])
+    for u in (1.0, 0.5):
+        check(dev(x), np.full(6, u, np.float32), top_k=[2999, 3000, 3001, 0, 0, 3000], top_p=[1.0, 1.0, 1.0, 0.9999, 0.5, 0.9])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [1, 31, 32, 33, 127, 128, 129, 511, 512, 513, 1023, 1024, 1025, 1026])
+def test_as_many_tokens_as_change_the_way(n, dtype):
+    """n tokens stand out of 8011, side by side or scattered: by top-k (512 is the most that the lanes' best tokens are
+    asked for), and gathered by top-p and by min-p as a list of n (of up to 1024, by min-p of those of up to half the
+    lanes; up to 128 are ranked, up to 32 by 32 threads each)."""
+    rs = np.random.default_rng(n)
+    V = 8011
+    x = rs.uniform(-26, -25, (6, V))
+    for r in range(6):
+        at = rs.permutation(V)[:n] if r < 3 else int(rs.integers(0, V - n)) + np.arange(n)
+        x[r, at] = rs.uniform(0.0, 1.0, n) if r % 3 == 1 else rs.uniform(0.4, 0.5, n)
+    xs = dev(x, dtype)
+    u = rs.random(6).astype(np.float32)
+    u[[0, 1, 4, 5]] = 1.0
+    check(xs, u, top_k=[n] * 6)
+    check(xs, u, top_k=[n + 1, max(1, n - 1)] * 3, top_p=[0.9] * 6)
+    check(xs, u, top_p=[0.9999995] * 6)
+    check(xs, u, top_p=[0.9999995] * 6, min_p=[1e-3] * 6)
+    check(xs, u, min_p=[1e-3] * 6)
+    check(xs, u, top_k=[5000] * 6, min_p=[1e-3] * 6)
