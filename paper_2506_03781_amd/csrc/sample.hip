@@ -627,11 +627,12 @@ __device__ __forceinline__ u64 part_of(float u, u64 total) {
   return __umul64hi(u64(double(u) * 0x1p64), total);
 }
 
-// Whether sums below it are below p total, p < 1: ceil(p total).
+// Whether sums below it are below p total, p < 1: ceil(p total), and 1 at least, the first token (also where p is
+// below 2^-64).
 __device__ __forceinline__ u64 border_of(float p, u64 total) {
-  if (!(p > 0.0f)) return 1;  // the first token
+  if (!(p > 0.0f)) return 1;
   const u64 f = u64(double(p) * 0x1p64), hi = __umul64hi(f, total), lo = f * total;
-  return hi + (lo != 0);
+  return std::max<u64>(hi + (lo != 0), 1);
 }
 
 // The answer from the gathered tokens, if they are not too many and hold all that
@@ -790,7 +791,7 @@ __global__ __launch_bounds__(THREADS) void sample_kernel(SampleLaunch p) {
         // tokens are gathered at once, one pass of 22 us less over a row of 131072.
         uint32_t c1;
         u64 m1;
-        const int pb = bin_of_cut(s, r, Cut{true, 0, std::max<u64>(border_of(top_p, m0), 1)}, c1, m1);
+        const int pb = bin_of_cut(s, r, Cut{true, 0, border_of(top_p, m0)}, c1, m1);
         const uint32_t np = s.count[pb];
         const u64 mp = s.mass[pb];
         both = pb < end && np + n <= CAP && border_of(top_p, kept) <= m1 + mp;

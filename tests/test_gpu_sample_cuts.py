@@ -89,3 +89,20 @@ def test_as_many_tokens_as_change_the_way(n, dtype):
     check(xs, u, top_p=[0.9999995] * 6, min_p=[1e-3] * 6)
     check(xs, u, min_p=[1e-3] * 6)
     check(xs, u, top_k=[5000] * 6, min_p=[1e-3] * 6)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_the_least_top_p(dtype):
+    """Any top-p above 0 keeps the first token: numbers below 2^-64, with subnormal ones, alone and beside the others."""
+    rs = np.random.default_rng(2)
+    p = np.array([1e-20, 1e-45, 2.0 ** -64, 2.0 ** -65, 5.5e-20, 1e-38, 1e-12, 2.0 ** -63], np.float32)
+    for V in (5, 300, 8011):
+        x = rs.standard_normal((8, V))
+        x[4:] = 0.25                              # all alike: the first by index
+        xs = dev(x, dtype)
+        for u in (np.zeros(8, np.float32), np.ones(8, np.float32), rs.random(8).astype(np.float32)):
+            check(xs, u, top_p=p)
+            check(xs, u, top_p=p, top_k=[50, 1, 3, 2, 50, 1, 600, 2])
+            check(xs, u, top_p=p, top_k=[5000] * 8, min_p=[0.1] * 8)
+            check(xs, u, top_p=p, min_p=[0.1, 1.0, 1e-3, 0.5] * 2)
+            check(xs, u, top_p=p, temperature=[100.0] * 8)
