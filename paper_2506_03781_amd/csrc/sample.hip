@@ -33,6 +33,7 @@
 #include <algorithm>
 
 #include "uq_device.h"
+#include "uq_kv.h"
 #include "uq_launch.h"
 
 namespace uq {
@@ -675,7 +676,8 @@ __device__ __forceinline__ bool answer_of_list(Lds& s, const Weigh& w, uint32_t 
 template <bool F32>
 __global__ __launch_bounds__(THREADS) void sample_kernel(SampleLaunch p) {
   __shared__ Lds s;
-  const int64_t t = blockIdx.x;
+  const int64_t t = workgroup();
+  if (t >= p.T) return;
   const Row<F32> row(p.x, t * p.ld, p.V);
   const int lane = threadIdx.x & 63, wave = uni(int(threadIdx.x >> 6));
 
@@ -897,9 +899,9 @@ hipError_t launch_sample(SampleLaunch p, hipStream_t st) {
   for (int64_t v = 1; v < p.V; v <<= 1) --p.sh;
   p.sh = std::min(p.sh, 51);  // weights below 2^52
   if (p.x_dtype == F32)
-    sample_kernel<true><<<unsigned(p.T), THREADS, 0, st>>>(p);
+    sample_kernel<true><<<grid_of(p.T), THREADS, 0, st>>>(p);
   else
-    sample_kernel<false><<<unsigned(p.T), THREADS, 0, st>>>(p);
+    sample_kernel<false><<<grid_of(p.T), THREADS, 0, st>>>(p);
   return hipGetLastError();
 }
 

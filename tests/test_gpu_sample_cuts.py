@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from oracle.sample import shift, weights
+from paper_2506_03781_amd import uniquan as uq
 from test_gpu_sample import check, dev
 
 pytestmark = pytest.mark.gpu
@@ -106,3 +107,21 @@ def test_the_least_top_p(dtype):
             check(xs, u, top_p=p, top_k=[5000] * 8, min_p=[0.1] * 8)
             check(xs, u, top_p=p, min_p=[0.1, 1.0, 1e-3, 0.5] * 2)
             check(xs, u, top_p=p, temperature=[100.0] * 8)
+
+
+def test_more_rows_than_a_dimension_of_the_grid_takes():
+    """2^22 rows and five (1024 threads each: 2^32 and more), equal to the rows in two calls, greedy ones to argmax."""
+    g = torch.Generator(device="cuda").manual_seed(3)
+    T, V, cut = (1 << 22) + 5, 3, 1 << 21
+    x, u = torch.randn(T, V, generator=g, device="cuda"), torch.rand(T, generator=g, device="cuda")
+    t = torch.ones(T, device="cuda")
+    t[::3] = 0.0
+    token, prob = torch.full((T + 9,), -7, dtype=torch.int32, device="cuda"), torch.full((T + 9,), -7.0, device="cuda")
+    uq.uniquan_sample(T, V, x, u, token, prob=prob, temperature=t)
+    t2, p2 = torch.empty(T, dtype=torch.int32, device="cuda"), torch.empty(T, device="cuda")
+    for a, b in ((0, cut), (cut, T)):
+        uq.uniquan_sample(b - a, V, x[a:b], u[a:b], t2[a:b], prob=p2[a:b], temperature=t[a:b].contiguous())
+    torch.cuda.synchronize()
+    assert (token[T:] == -7).all() and (prob[T:] == -7.0).all()
+    assert torch.equal(token[:T], t2) and torch.equal(prob[:T], p2)
+    assert torch.equal(token[:T][::3].long(), x[::3].argmax(1))
