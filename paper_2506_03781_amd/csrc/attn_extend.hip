@@ -1121,14 +1121,18 @@ int columns_of(int64_t T, int64_t n_seq, int H, int H_kv, int d, Kind f) {
 }
 // Tiles of one key/value head, if no row is padding.
 int64_t tiles_of(int64_t T, int H, int H_kv, int cols) { return T * (H / H_kv) / cols; }
-// Shares of one key/value head that are wanted (0: no tile is cut).  The GPU holds two workgroups a CU; between a
-// quarter of those and all, two rounds of shares even out what rounding shares of whole steps leaves (24 x 32 rows
-// of 8192 positions at 8 bits, 1.5 tiles a place: 245 us with one round, 250 with two).  With more tiles than places
-// only a tile of twice the mean and more is cut, which costs equal sequences the join (1 x 2048 rows 85 -> 92 us) and
-// saves unequal ones more (96 x 8 rows, one sequence of 32768 positions and 95 of 1024: 470 -> 134 us).
+// Whether a tile can be cut at all: two shares of a key/value head have to have a place, and steps enough.
+bool cuttable(int H_kv, int64_t max_pages, int page_len) {
+  return 2 * CUS / H_kv >= 2 && max_pages * page_len > MIN_STEPS * STEP;
+}
+// Shares of one key/value head that are wanted (0: no tile is cut; else two or more).  The GPU holds two workgroups a
+// CU; between a quarter of those and all, two rounds of shares even out what rounding shares of whole steps leaves
+// (24 x 32 rows of 8192 positions at 8 bits, 1.5 tiles a place: 245 us with one round, 250 with two).  With more tiles
+// than places only a tile of twice the mean and more is cut, which costs equal sequences the join (1 x 2048 rows 85 ->
+// 92 us) and saves unequal ones more (96 x 8 rows, one sequence of 32768 positions and 95 of 1024: 470 -> 134 us).
 int target_of(int64_t T, int64_t n_seq, int H, int H_kv, int cols, int64_t max_pages, int page_len) {
-  const int64_t holds = std::max(1, 2 * CUS / H_kv), tiles = std::max(tiles_of(T, H, H_kv, cols), std::min(T, n_seq));
-  if (max_pages * page_len <= MIN_STEPS * STEP || tiles >= 4 * holds) return 0;
+  const int64_t holds = 2 * CUS / H_kv, tiles = std::max(tiles_of(T, H, H_kv, cols), std::min(T, n_seq));
+  if (!cuttable(H_kv, max_pages, page_len) || tiles >= 4 * holds) return 0;
   return int(4 * tiles <= holds || tiles >= holds ? holds : 2 * holds);
 }
 
@@ -1139,7 +1143,7 @@ int target_of(int64_t T, int64_t n_seq, int H, int H_kv, int cols, int64_t max_p
 // 359 -> 370), so that fewer than four go without.
 int few_of(Kind f) { return f == PLAIN ? 16 : 64; }
 int target_of_few(int64_t n_seq, int H_kv, int64_t max_pages, int page_len) {
-  return n_seq < 4 || max_pages * page_len <= MIN_STEPS * STEP ? 0 : std::max(1, 2 * CUS / H_kv);
+  return n_seq < 4 || !cuttable(H_kv, max_pages, page_len) ? 0 : 2 * CUS / H_kv;
 }
 
 template <int D, int COLS>
