@@ -417,7 +417,7 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(KS
 // waves per SIMD (two, with two tiles a stage: 141 us in place of 127 for 4 x 2048
 // rows of 32 heads in a window of 512).  The causal forward's two walks, one for the
 // log-sum-exp, took 182; they remain where walks are split, and for a window over
-// everything, whose walks are the causal call's (and its results, split alike).
+// everything, which is the causal call bit for bit.
 constexpr float SLACK_W = 8.0f;
 template <int NW, bool TOK>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(3))) void attn_window_fwd_kernel(AttnArgs a) {
@@ -975,9 +975,12 @@ static void set_tok(AttnArgs& a, const AttnLaunch& q) {
   a.window = std::min(q.window, q.L); a.sinks = std::min(q.sinks, q.L);
 }
 
+// Whether a window, or the first positions, are everything: the causal attention, with its results bit for bit.
+static bool whole(const AttnLaunch& q) { return q.window <= 0 || std::max(q.window, q.sinks) >= q.L; }
+
 // Whether a call's walks are split, split_walk's rule for windows: all rows but the sinks' walk alike.
 static bool splits(const AttnLaunch& q, int nblk) {
-  if (q.window <= 0) return split_walk(nblk, q.batch, q.L);
+  if (whole(q)) return split_walk(nblk, q.batch, q.L);
   return nblk * q.batch <= 256 && std::min(q.L, std::min(q.window, q.L) + NW * NB) >= 512;
 }
 
@@ -988,7 +991,7 @@ hipError_t launch_attn_fwd(const AttnLaunch& q, hipStream_t st) {
   set_tok(a, q);
   const int nblk = (q.L + NW * NB - 1) / (NW * NB);
   const bool split = splits(q, nblk);
-  if (q.window > 0 && std::max(q.window, q.sinks) < q.L && !split) {  // (a window over everything: as the causal call)
+  if (!whole(q) && !split) {
     launch(q.tok_seqs > 0 ? attn_window_fwd_kernel<NW, true> : attn_window_fwd_kernel<NW, false>, nblk * q.batch, 1, a, st);
     return hipGetLastError();
   }
