@@ -166,7 +166,7 @@ __device__ __forceinline__ void copy_tile(const uint16_t* base, const uint32_t (
   for (int q = 0; q < PW; ++q) copy16(base, off[q], tile + (wave * PW + q) * 64);
 }
 
-// Windows (WIN).  Any L: the rows of the last tile that lie behind L are copies
+// Windows (WIN; over everything, the forward's ANY).  Any L: the rows of the last tile that lie behind L are copies
 // of row L - 1, which no query before them sees and whose own results are not
 // stored.  P enters dS before its rounding to bf16, one rounding less in dQ and dK.
 template <bool WIN, int PW>
@@ -243,7 +243,7 @@ __device__ __forceinline__ void add_groups(f32x16a (&acc)[4], float* smem, int w
 // fragments go from LDS straight into their MFMAs rather than into arrays
 // held across the tile: 156 registers, so three waves share a SIMD and one
 // wave's exponentials overlap another's products (two waves per SIMD at 243).
-template <int NW, int S, bool TOK, int KS, bool WIN = false>
+template <int NW, int S, bool TOK, int KS, bool ANY = false>
 __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(KS == 1 ? 3 : 2))) void attn_fwd_kernel(AttnArgs a) {
   constexpr int QB = NW * NB;
   constexpr int PW = 8 / NW;  // copy blocks per wave and tile
@@ -260,23 +260,11 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(KS
   const int q0 = qb * QB + wave * NB;
   const bool active = q0 < L;
   const int qi = q0 + (lane & 31);  // this lane's query
-  const int n_tiles = (min(L, qb * QB + QB) + (WIN ? NB - 1 : 0)) / NB;
+  const int n_tiles = (min(L, qb * QB + QB) + (ANY ? NB - 1 : 0)) / NB;
   const int my_tiles = active ? q0 / NB + 1 : 0;
-  const KeyWalk walk = WIN ? key_walk(qb * QB, n_tiles, a.window, a.sinks) : KeyWalk{0, 0, n_tiles};
   // step i of the walk: tile i KS + ks (past the end the last tile is copied, unused)
-  const int n_steps = (walk.n + KS - 1) / KS;
-  auto tile_at = [&](int i) {
-    const int j = KS == 1 ? i : min(i * KS + ks, walk.n - 1);
-    return int64_t(WIN ? walk.tile(j) : j);
-  };
-  // whether this wave's queries see anything of tile t, and whether they do not see all of it
-  auto sees = [&](int i, int t) {
-    return t < my_tiles && (!WIN || ((KS == 1 || i * KS + ks < walk.n) && (t * NB < a.sinks || t >= first_tile(q0, a.window))));
-  };
-  auto cut = [&](int t) {
-    return t == my_tiles - 1 || (WIN && q0 + NB - 1 - t * NB >= a.window && (t + 1) * NB > a.sinks);
-  };
-  auto hidden = [&](int j) { return j > qi || (WIN && qi - j >= a.window && j >= a.sinks); };
+  const int n_steps = (n_tiles + KS - 1) / KS;
+  auto tile_at = [&](int i) { return int64_t(KS == 1 ? i : min(i * KS + ks, n_tiles - 1)); };
   auto stage_at = [&](int i) { return smem + ((i % S) * KS + ks) * STAGE; };
   const uint16_t* Kb = a.K + bk * int64_t(L) * D;
   const uint16_t* Vb = a.V + bk * int64_t(L) * D;
@@ -294,24 +282,24 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(KS
   float m = -INFINITY, l = 0.0f;
 #pragma unroll
   for (int t = 0; t < S - 1; ++t)
-    if (t < n_steps) copy_rows<WIN, PW>(Kb + tile_at(t) * NB * D, ro, stage_at(t), wave, lane, D, L - int(tile_at(t)) * NB);
+    if (t < n_steps) copy_rows<ANY, PW>(Kb + tile_at(t) * NB * D, ro, stage_at(t), wave, lane, D, L - int(tile_at(t)) * NB);
   for (int i = 0; i < n_steps; ++i) {
     wait_tiles<PW>(min(S - 2, n_steps - 1 - i));
     lds_wait_barrier();
     if (i + S - 1 < n_steps) {
       const int u = i + S - 1;
-      copy_rows<WIN, PW>(Kb + tile_at(u) * NB * D, ro, stage_at(u), wave, lane, D, L - int(tile_at(u)) * NB);
+      copy_rows<ANY, PW>(Kb + tile_at(u) * NB * D, ro, stage_at(u), wave, lane, D, L - int(tile_at(u)) * NB);
     }
-    const int t = WIN ? int(tile_at(i)) : i * KS + ks;
-    if (!sees(i, t)) continue;
+    const int t = i * KS + ks;
+    if (t >= my_tiles) continue;
     const u32x4a* tk = stage_at(i);
     f32x16a s = zero16();
 #pragma unroll
     for (int j = 0; j < 8; ++j) s = mfma(row_frag(tk, j, lane), qf[j], s);
-    if (cut(t)) {
+    if (t == my_tiles - 1) {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        if (hidden(t * NB + slot_row(r, lane))) s[r] = -INFINITY;
+        if (t * NB + slot_row(r, lane) > qi) s[r] = -INFINITY;
     }
     float mx = s[0];
 #pragma unroll
@@ -353,19 +341,19 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(KS
 #pragma unroll
   for (int t = 0; t < S - 1; ++t)
     if (t < n_steps) {
-      copy_rows<WIN, PW>(Kb + tile_at(t) * NB * D, ro, stage_at(t), wave, lane, D, L - int(tile_at(t)) * NB);
-      copy_rows<WIN, PW>(Vb + tile_at(t) * NB * D, ro, stage_at(t) + TILE16, wave, lane, D, L - int(tile_at(t)) * NB);
+      copy_rows<ANY, PW>(Kb + tile_at(t) * NB * D, ro, stage_at(t), wave, lane, D, L - int(tile_at(t)) * NB);
+      copy_rows<ANY, PW>(Vb + tile_at(t) * NB * D, ro, stage_at(t) + TILE16, wave, lane, D, L - int(tile_at(t)) * NB);
     }
   for (int i = 0; i < n_steps; ++i) {
     wait_tiles<2 * PW>(min(S - 2, n_steps - 1 - i));
     lds_wait_barrier();
     if (i + S - 1 < n_steps) {
       const int u = i + S - 1;
-      copy_rows<WIN, PW>(Kb + tile_at(u) * NB * D, ro, stage_at(u), wave, lane, D, L - int(tile_at(u)) * NB);
-      copy_rows<WIN, PW>(Vb + tile_at(u) * NB * D, ro, stage_at(u) + TILE16, wave, lane, D, L - int(tile_at(u)) * NB);
+      copy_rows<ANY, PW>(Kb + tile_at(u) * NB * D, ro, stage_at(u), wave, lane, D, L - int(tile_at(u)) * NB);
+      copy_rows<ANY, PW>(Vb + tile_at(u) * NB * D, ro, stage_at(u) + TILE16, wave, lane, D, L - int(tile_at(u)) * NB);
     }
-    const int t = WIN ? int(tile_at(i)) : i * KS + ks;
-    if (!sees(i, t)) continue;
+    const int t = i * KS + ks;
+    if (t >= my_tiles) continue;
     const u32x4a* tk = stage_at(i);
     const u32x4a* tv = tk + TILE16;
     f32x16a s = zero16();
@@ -374,10 +362,10 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(KS
     float p[16];
 #pragma unroll
     for (int r = 0; r < 16; ++r) p[r] = exp2a(fmaf(s[r], c, -lse));
-    if (cut(t)) {
+    if (t == my_tiles - 1) {
 #pragma unroll
       for (int r = 0; r < 16; ++r)
-        if (hidden(t * NB + slot_row(r, lane))) p[r] = 0.0f;
+        if (t * NB + slot_row(r, lane) > qi) p[r] = 0.0f;
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -391,7 +379,7 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(KS
     add_groups<NW>(o, reinterpret_cast<float*>(smem), wave, ks, lane);
     if (ks != 0) return;
   }
-  if (!active || (WIN && qi >= L)) return;
+  if (!active || (ANY && qi >= L)) return;
   uint16_t* orow = a.O_out + (TOK ? tok_off(a, b, qi) : (b * L + qi) * int64_t(D));
 #pragma unroll
   for (int db = 0; db < 4; ++db)
@@ -416,8 +404,9 @@ __global__ __launch_bounds__(NW * KS * 64) __attribute__((amdgpu_waves_per_eu(KS
 // product with V, their sum unrounded.  166 registers and 32 KB of stages: three
 // waves per SIMD (two, with two tiles a stage: 141 us in place of 127 for 4 x 2048
 // rows of 32 heads in a window of 512).  The causal forward's two walks, one for the
-// log-sum-exp, took 182; they remain where walks are split, and for a window over
-// everything, which is the causal call bit for bit.
+// log-sum-exp, took 182; with one workgroup a CU or less this one, unsplit, takes 25 us
+// where they, split, take 30 (8 and 16 heads of 2048 rows, a window of 512).  They remain
+// for a window over everything, which is the causal call bit for bit.
 constexpr float SLACK_W = 8.0f;
 template <int NW, bool TOK>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(3))) void attn_window_fwd_kernel(AttnArgs a) {
@@ -978,10 +967,15 @@ static void set_tok(AttnArgs& a, const AttnLaunch& q) {
 // Whether a window, or the first positions, are everything: the causal attention, with its results bit for bit.
 static bool whole(const AttnLaunch& q) { return q.window <= 0 || std::max(q.window, q.sinks) >= q.L; }
 
-// Whether a call's walks are split, split_walk's rule for windows: all rows but the sinks' walk alike.
-static bool splits(const AttnLaunch& q, int nblk) {
-  if (whole(q)) return split_walk(nblk, q.batch, q.L);
-  return nblk * q.batch <= 256 && std::min(q.L, std::min(q.window, q.L) + NW * NB) >= 512;
+// Whether the walks of a window's backward are split: where workgroups of four waves give one a CU at most, and the
+// longest walk is 384 rows or more: of all rows where the first keys are in sight, else of the window and a block.
+// Both directions' calls without and with the split, us: no first positions, 256 workgroups (L = 2048), windows of 1 /
+// 64 / 128 / 256 / 1024: 39 / 49 / 58 / 71 / 152 against 42 / 50 / 56 / 67 / 132; 288 workgroups 52 / 63 / 73 / 91 / 191
+// against 70 / 84 / 94 / 113 / 214.  First positions in sight, 256 workgroups, window 64: L = 512 70 against 65, 2048
+// 171 against 128; L = 256 (128 workgroups) 52 against 51, 384 (48) 58 against 54.
+static bool split_window_bwd(const AttnLaunch& q, int nblk) {
+  const int walk = q.sinks > 0 ? q.L : std::min(q.L, q.window + NW * NB);
+  return nblk * q.batch <= 256 && walk >= 384;
 }
 
 hipError_t launch_attn_fwd(const AttnLaunch& q, hipStream_t st) {
@@ -990,11 +984,11 @@ hipError_t launch_attn_fwd(const AttnLaunch& q, hipStream_t st) {
   a.Q = q.Q; a.K = q.K; a.V = q.V; a.O_out = q.O_out; a.lse = q.lse;
   set_tok(a, q);
   const int nblk = (q.L + NW * NB - 1) / (NW * NB);
-  const bool split = splits(q, nblk);
-  if (!whole(q) && !split) {
+  if (!whole(q)) {
     launch(q.tok_seqs > 0 ? attn_window_fwd_kernel<NW, true> : attn_window_fwd_kernel<NW, false>, nblk * q.batch, 1, a, st);
     return hipGetLastError();
   }
+  const bool split = split_walk(nblk, q.batch, q.L);
   launch(UQ_ATTN_FORM(attn_fwd_kernel)(q.tok_seqs > 0, split, q.window > 0), nblk * q.batch, split ? 2 : 1, a, st);
   return hipGetLastError();
 }
@@ -1008,7 +1002,7 @@ hipError_t launch_attn_bwd(const AttnLaunch& q, hipStream_t st) {
   const bool tok = q.tok_seqs > 0, win = q.window > 0;
   const int nblk = (q.L + NW * NB - 1) / (NW * NB);
   const int64_t blocks = nblk * q.batch;
-  const bool split = splits(q, nblk);
+  const bool split = whole(q) ? split_walk(nblk, q.batch, q.L) : split_window_bwd(q, nblk);
   const int ks = split ? 2 : 1;
   if (win) {
     const auto kern = tok ? attn_window_delta_kernel<NW, S, true> : attn_window_delta_kernel<NW, S, false>;

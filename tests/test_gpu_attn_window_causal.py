@@ -29,3 +29,12 @@ def test_equal_to_the_causal_call(L, n, H, Hkv, tok):
                                                     (1000, 20, 1001, 1, 40, 8)])
 def test_gradients_of_a_window_over_everything(L, window, sinks, n, H, Hkv, tok):
     check(Case(L, window, sinks, n, H, Hkv), tok)
+
+
+@pytest.mark.parametrize("tok", [False, True])
+@pytest.mark.parametrize("L,window,sinks,n,H,Hkv", [(383, 100, 2, 1, 2, 2), (384, 100, 2, 2, 2, 1), (385, 384, 1, 1, 3, 3),
+                                                    (600, 255, 0, 1, 2, 2), (600, 256, 0, 1, 4, 2), (1024, 300, 0, 2, 16, 16),
+                                                    (1024, 300, 5, 3, 11, 11), (700, 1, 1, 1, 2, 1)])
+def test_windows_where_the_backward_begins_to_split(L, window, sinks, n, H, Hkv, tok):
+    """Longest walks of 383 to 385 rows, with and without first positions, and 256 workgroups and more."""
+    check(Case(L, window, sinks, n, H, Hkv), tok)
