@@ -8,7 +8,8 @@
 // its rows see, or a share of them.  Where the tiles are fewer than the GPU holds
 // workgroups, and where some are much longer than others, they are cut into shares
 // of about equal length, and attn_extend_join_kernel joins those; workgroups find
-// their place by adding up all sequences' tiles and steps of 32 positions.
+// their place by adding up all sequences' tiles and steps of 32 positions, or, where
+// nothing is cut, by a search among the sequences' first rows.
 //
 // Few columns (attn_extend_kernel: 16 or 32).  One step is that of the single-token
 // attention (attn_decode.hip): S^T = K Q^T and O^T += V^T P^T with the heads as
@@ -99,29 +100,58 @@ struct Unit {
   }
 };
 
+// Unit x where no tile is cut.  Sequence s has the numbers from floor(row_start[s] G / COLS) + s on, as many as tiles
+// or one more (floor(a + b) - floor(a) + 1 is ceil(b) at least), so that a search finds it.  Adding up all sequences'
+// tiles in every workgroup takes time with their square: 4096 of one row, 8 heads and 128 positions 2.4 ms (so 0.56),
+// 16384 of one head 4.0 (0.28).  Where only sequences of up to to_cols columns are taken, each has as many numbers as
+// such a one has tiles.
+template <int COLS>
+__device__ __forceinline__ bool find_whole(const AttnExtendLaunch& p, int G, int64_t x, Unit& u) {
+  const int lane = threadIdx.x & 63, n = int(p.c.n_seq);
+  int s = 0;
+  int64_t at;
+  if (p.to_cols < INT64_MAX) {
+    const int64_t per = (p.to_cols + COLS - 1) / COLS;
+    if (x >= per * n) return false;
+    s = int(x / per);
+    at = x % per;
+  } else {
+    auto first = [&](int j) { return std::min<int64_t>(std::max(p.row_start[j], 0), p.T) * G / COLS + j; };
+    for (int size = n; size > 1;) {  // it is one of the `size` from s on
+      const int step = (size + 63) / 64;
+      const uint64_t past = __ballot(lane * step < size && first(s + lane * step) <= x);
+      if (!past) return false;
+      const int k = 63 - __builtin_clzll(past);
+      s += k * step;
+      size = std::min(step, size - k * step);
+    }
+    at = x - first(s);
+  }
+  u = Unit{uniform(s), int(at), 0, 0, 0.0, 0};
+  const Seq seq = seq_of(p, p.row_start[u.s], p.row_start[u.s + 1], 0);
+  return at >= 0 && at < Work<COLS>{p, G}.tiles(seq);
+}
+
 // Unit x: a share of a tile, or with TILES a tile that is cut; false: there are fewer.
 // target: shares that are wanted (0: no tile is cut).
 template <int COLS, bool TILES>
 __device__ __forceinline__ bool find(const AttnExtendLaunch& p, int G, int64_t x, int target, Unit& u) {
+  if (target == 0) return find_whole<COLS>(p, G, x, u);
   const Work<COLS> w{p, G};
   const int lane = threadIdx.x & 63;
   const int n = int(p.c.n_seq), run = (n + 63) / 64;
   auto seq = [&](int j) { return seq_of(p, p.row_start[j], p.row_start[j + 1], p.lens[j]); };
-  u.rate = 0.0;
-  u.total = 0;
-  u.target = target;
-  if (target > 0) {
-    int64_t total = 0;
-    for (int j = lane * run; j < lane * run + run && j < n; ++j) {
-      const Seq s = seq(j);
-      total += int64_t(w.tiles(s)) * w.steps(s);
-    }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1)
-      total += int64_t(uint64_t(uint32_t(__shfl_xor(int(total >> 32), d))) << 32 | uint32_t(__shfl_xor(int(total), d)));
-    u.total = int64_t(uint64_t(uint32_t(uniform(int(total >> 32)))) << 32 | uint32_t(uniform(int(total))));
-    u.rate = double(target) / double(u.total > 0 ? u.total : 1);
+  int64_t total = 0;
+  for (int j = lane * run; j < lane * run + run && j < n; ++j) {
+    const Seq s = seq(j);
+    total += int64_t(w.tiles(s)) * w.steps(s);
   }
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1)
+    total += int64_t(uint64_t(uint32_t(__shfl_xor(int(total >> 32), d))) << 32 | uint32_t(__shfl_xor(int(total), d)));
+  u.total = int64_t(uint64_t(uint32_t(uniform(int(total >> 32)))) << 32 | uint32_t(uniform(int(total))));
+  u.rate = double(target) / double(u.total > 0 ? u.total : 1);
+  u.target = target;
   auto count = [&](int j, int& un, int& sp) {
     un = sp = 0;
     if (j >= n) return;
@@ -1119,8 +1149,11 @@ int columns_of(int64_t T, int64_t n_seq, int H, int H_kv, int d, Kind f) {
   if (d != 128 || f == ONE_GROUP) return 32;
   return cols > 64 ? WIDE : f == PLAIN ? 32 : 16;
 }
-// Tiles of one key/value head, if no row is padding.
+// Tiles of one key/value head, if no row is padding; workgroups for them and as many shares (or numbers, find_whole).
 int64_t tiles_of(int64_t T, int H, int H_kv, int cols) { return T * (H / H_kv) / cols; }
+int64_t units_of(const AttnExtendLaunch& p, int cols, int target) {
+  return tiles_of(p.T, p.H, p.c.H_kv, cols) + (target ? std::min(p.T, p.c.n_seq) + target : p.c.n_seq);
+}
 // Whether a tile can be cut at all: two shares of a key/value head have to have a place, and steps enough.
 bool cuttable(int H_kv, int64_t max_pages, int page_len) {
   return 2 * CUS / H_kv >= 2 && max_pages * page_len > MIN_STEPS * STEP;
@@ -1142,8 +1175,12 @@ int target_of(int64_t T, int64_t n_seq, int H, int H_kv, int cols, int64_t max_p
 // 632 -> 367; 7 tokens 198 -> 165 and 325 -> 222.  Sequences alike pay the empty launches (8 x 128 rows 225 -> 230 us,
 // 359 -> 370), so that fewer than four go without.
 int few_of(Kind f) { return f == PLAIN ? 16 : 64; }
+// (Not cut where there are more sequences than a workgroup adds up in passing.)
+bool few_apart(int64_t n_seq, int H_kv, int64_t max_pages, int page_len) {
+  return n_seq >= 4 && cuttable(H_kv, max_pages, page_len);
+}
 int target_of_few(int64_t n_seq, int H_kv, int64_t max_pages, int page_len) {
-  return n_seq < 4 || !cuttable(H_kv, max_pages, page_len) ? 0 : 2 * CUS / H_kv;
+  return few_apart(n_seq, H_kv, max_pages, page_len) && n_seq <= 1024 ? 2 * CUS / H_kv : 0;
 }
 
 template <int D, int COLS>
@@ -1162,22 +1199,24 @@ hipError_t launch_form(const AttnExtendLaunch& p, hipStream_t st) {
   constexpr Kind KIND = kind_of(FMT, NG);
   const int H_kv = p.c.H_kv, cols = columns_of(p.T, p.c.n_seq, p.H, H_kv, D, KIND);
   const int target = target_of(p.T, p.c.n_seq, p.H, H_kv, cols, p.c.max_pages, p.c.page_len);
-  const int64_t tiles = tiles_of(p.T, p.H, H_kv, cols) + std::min(p.T, p.c.n_seq);
-  const dim3 grid = grid_of((tiles + target) * H_kv);
+  const dim3 grid = grid_of(units_of(p, cols, target) * H_kv);
   const float back = FMT == KV_BF16 ? BF16_BACK : 1.0f;
   if constexpr (D == 128 && KIND != ONE_GROUP) {
     if (cols == WIDE) {
       AttnExtendLaunch many = p, few = p;
-      const int few_target = target_of_few(p.c.n_seq, H_kv, p.c.max_pages, p.c.page_len);
-      if (few_target) many.from_cols = (few.to_cols = few_of(KIND)) + 1;
+      const bool apart = few_apart(p.c.n_seq, H_kv, p.c.max_pages, p.c.page_len);
+      if (apart) many.from_cols = (few.to_cols = few_of(KIND)) + 1;
       attn_extend_wide_kernel<FMT, NG><<<grid, 256, 0, st>>>(many, target);
       if (hipError_t e = hipGetLastError()) return e;
-      if (few_target) {
-        const int64_t n = std::min(p.T, p.c.n_seq) * (few_of(KIND) / 16);
+      if (apart) {
+        const int few_target = target_of_few(p.c.n_seq, H_kv, p.c.max_pages, p.c.page_len);
+        const int64_t n = (few_target ? std::min(p.T, p.c.n_seq) : p.c.n_seq) * (few_of(KIND) / 16) + few_target;
         few.ws = p.ws + size_t(target) * size_t(H_kv) * WIDE * (D + 4);
-        attn_extend_kernel<FMT, D, NG, 1><<<grid_of((n + few_target) * H_kv), 256, 0, st>>>(few, few_target);
+        attn_extend_kernel<FMT, D, NG, 1><<<grid_of(n * H_kv), 256, 0, st>>>(few, few_target);
         if (hipError_t e = hipGetLastError()) return e;
-        if (hipError_t e = launch_join<D, 16>(few, few_target, back, st)) return e;
+        if (few_target) {
+          if (hipError_t e = launch_join<D, 16>(few, few_target, back, st)) return e;
+        }
       }
       return target ? launch_join<D, WIDE>(many, target, 1.0f, st) : hipSuccess;
     }
