@@ -146,7 +146,7 @@ class DecoderBlock:
     backpropagation reads and writes both in one product each; with
     grouped-query attention, the W_hat and G arrays of k and v likewise.
     With window > 0 the attention is that of a sliding window (token i sees
-    j <= i with i - j < window or j < sinks; any L then).
+    j <= i with i - j < window or j < sinks; any L then, T a multiple of 32).
 
     ``prepare(X)`` computes the full-precision block's output on the
     full-precision input X (the target); ``set_input(Xhat)`` gives the
