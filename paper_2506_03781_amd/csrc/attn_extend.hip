@@ -30,7 +30,7 @@
 // are 0, not NaN).  All other steps, nearly all of a long history, have no masks.
 //
 // Precision.  With 16 columns as in attn_decode.hip.  With more a weight enters the
-// second product as one bf16 value, rounded to nearest (2^-9 of it at most, either
+// second product as one bf16 value, rounded to nearest (2^-8 of it at most, either
 // way), as in the block's causal attention: a second term would double that product,
 // which bounds such calls.
 #include <hip/hip_runtime.h>
@@ -224,12 +224,9 @@ __device__ __forceinline__ bool wild(uint32_t w) {
   return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
 }
 
-// Workgroups a CU holds (their registers are bounded to that): the most for which nothing is spilled in the loop.
+// (Two workgroups a CU are the most for which nothing is spilled in the loop.)
 template <int FMT, int D, int NG, int NT>
-constexpr int kHeld = NT == 2 && NG == 4 ? 1 : 2;
-
-template <int FMT, int D, int NG, int NT>
-__global__ __launch_bounds__(256, (kHeld<FMT, D, NG, NT>)) void attn_extend_kernel(AttnExtendLaunch p, int target) {
+__global__ __launch_bounds__(256, 2) void attn_extend_kernel(AttnExtendLaunch p, int target) {
   using F = Form<FMT, D>;
   constexpr int COLS = 16 * NT;
   constexpr bool CODES = FMT != KV_BF16, TWO = NT == 1;  // two terms a weight
@@ -1140,6 +1137,11 @@ __global__ __launch_bounds__(256) void attn_extend_join_kernel(AttnExtendLaunch 
 //   32 columns:  bf16 185 | 171 | 225,  u8 113 | 103 | -,    u8 in groups of 32 144 | 361 | 296
 //   64 columns:  bf16 264 | 185 | 212,  u8 178 | 124 | -,    u8 in groups of 32 235 | 552 | 315
 //   128 columns: bf16 474 | 275 | 229,  u8 317 | 202 | 276,  u8 in groups of 32 423 | 957 | 338
+// and of heads of 64 channels, with 16 | 32:
+//   32 columns:  bf16 94 | 87,    u8 55 | 57,    u8 in groups of 32 65 | 65
+//   128 columns: bf16 274 | 155,  u8 174 | 147,  u8 in groups of 32 213 | 178
+// One sequence of 32768 positions goes alike; batches too small to fill the GPU lose up to 17 us by the larger tiles
+// (4 sequences of 4096 positions, 2 heads, 128 columns: bf16 26 | 28 | 34, u8 22 | 26 | -, in groups of 32 25 | - | 42).
 // Two column tiles and the statistics of four groups do not fit into the registers.
 enum Kind { PLAIN, ONE_GROUP, GROUPS };
 constexpr Kind kind_of(int fmt, int ng) { return fmt == KV_BF16 ? PLAIN : ng == 1 ? ONE_GROUP : GROUPS; }
