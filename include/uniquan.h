@@ -650,9 +650,10 @@ uq_status uniquan_attn_bwd(int64_t batch, int64_t kv_batch, int L, int d,
  * may be rounded to bf16 as 2^(c S - m), m a running maximum, and O divided by their
  * unrounded sum; that P enters dS before it is rounded: dS = bf16(2^(c S - row_lse)
  * (dP - delta)); and that delta is sum_j P_ij dP_ij (fp32; O is not read).
- * window >= 1, sinks >= 0 (window or sinks >= L: the causal attention); any L >= 1
- * (up to 2^22, batch ceil(L / 128) at most 2^22); scale positive and finite.  Q, K, V, dO have to be finite: a key outside
- * a query's sight has weight 0, not no part.
+ * window >= 1, sinks >= 0 (window or sinks >= L: the causal attention, the forward
+ * uniquan_attn_fwd's bit for bit); any L >= 1 (up to 2^22, batch ceil(L / 128) at most
+ * 2^22); scale positive and finite.  Q, K, V, dO have to be finite: a key outside a
+ * query's sight has weight 0, not no part.
  */
 uq_status uniquan_attn_window_fwd(int64_t batch, int64_t kv_batch, int L, int d,
                                   const uint16_t* Q, const uint16_t* K, const uint16_t* V,

@@ -19,7 +19,7 @@
 // Many columns (attn_extend_wide_kernel: 128).  Tiles of keys and values in LDS, read
 // by four wavefronts with 32 columns each.  A wavefront's products wait for its weights
 // and the other way round, and 64 KB of tiles and 256 registers leave two wavefronts a
-// SIMD to cover that: 2 x 2048 rows behind 6144 positions, 32 heads over 8, in 606 us,
+// SIMD to cover that: 2 x 2048 rows behind 6144 positions, 32 heads over 8, in 605 us,
 // 795 TFLOP/s.  columns_of says which is taken where; with four sequences or more, those
 // of few columns among many have the first kernel's tiles beside the second's.
 //

@@ -517,7 +517,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(3))) vo
 // and with keys whose mean is not 0 (channels of outliers) it was the largest error
 // of dQ by far (4 x 2048 rows, 32 heads, window 512, one channel of the keys ten
 // times the others: dQ off by 4.0e-3 of its norm and by up to 0.66 of an element's
-// size, now 3.2e-3 and 0.25; the walk takes 124 of 725 us).
+// size, now 3.2e-3 and 0.25; the walk takes 124 of the 640 us of both directions).
 template <int NW, int S, bool TOK>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(3))) void attn_window_delta_kernel(AttnArgs a) {
   constexpr int QB = NW * NB;
