@@ -6,7 +6,7 @@ import torch
 
 from oracle.sample import shift, weights
 from paper_2506_03781_amd import uniquan as uq
-from test_gpu_sample import check, dev
+from test_gpu_sample import call, check, dev
 
 pytestmark = pytest.mark.gpu
 
@@ -125,3 +125,38 @@ def test_more_rows_than_a_dimension_of_the_grid_takes():
     assert (token[T:] == -7).all() and (prob[T:] == -7.0).all()
     assert torch.equal(token[:T], t2) and torch.equal(prob[:T], p2)
     assert torch.equal(token[:T][::3].long(), x[::3].argmax(1))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [1 << 22, (1 << 22) - 3, 1 << 20])
+def test_the_largest_rows(V, dtype):
+    """The plain reference's steps on whole arrays: its integers fit 64 bits (V 2^sh is 2^62 at most)."""
+    g = torch.Generator(device="cuda").manual_seed(V % 100)
+    x = (2 * torch.randn(V, generator=g, device="cuda")).to(dtype)
+    row = x.float().cpu().numpy()
+    sh = shift(V)
+    w = np.rint(np.exp(row.astype(np.longdouble) - np.longdouble(row.max())) * np.longdouble(2.0) ** sh).astype(np.int64)
+    order = np.lexsort((np.arange(V), -row))
+    before = np.cumsum(w[order]) - w[order]
+    total = int(w.sum())
+    k = [0, 0, 1000, 600000, 0, V - 1]
+    p = np.array([1.0, 0.9, 0.8, 0.95, 0.999, 1.0], np.float32)
+    lo = np.array([0, 0, 0, 0, 1e-3, 1e-5], np.float32)
+    u = np.array([0.3, 0.8, 0.999, 0.5, 1.0, 0.7], np.float32)
+    token, prob = call(x[None].repeat(6, 1), u, top_k=k, top_p=p, min_p=lo)
+    for r in range(6):
+        first = order[:k[r]] if k[r] else order
+        if p[r] < 1:
+            mass = int(w[first].sum())
+            border = -(-int(np.float64(p[r]) * 2.0 ** 64) * mass >> 64)  # ceil
+            first = first[before[:len(first)] < border]
+        if lo[r] > 0:
+            first = first[w[first] >= np.ceil(np.float64(lo[r]) * 2.0 ** sh)]
+        kept = np.sort(first)
+        upto = np.cumsum(w[kept])
+        mass = int(upto[-1])
+        at = mass - 1 if u[r] >= 1 else int(np.float64(u[r]) * 2.0 ** 64) * mass >> 64
+        want = kept[np.searchsorted(upto, at, side="right")]
+        assert token[r] == want, f"row {r}: {token[r]}, expected {want}"
+        assert abs(prob[r] - w[want] / mass) <= 2.0 ** -22 * w[want] / mass
+    assert total <= 1 << 62
