@@ -1177,10 +1177,11 @@ int target_of(int64_t T, int64_t n_seq, int H, int H_kv, int cols, int64_t max_p
 // 632 -> 367; 7 tokens 198 -> 165 and 325 -> 222.  Sequences alike pay the empty launches (8 x 128 rows 225 -> 230 us,
 // 359 -> 370), so that fewer than four go without.
 int few_of(Kind f) { return f == PLAIN ? 16 : 64; }
-// (Not cut where there are more sequences than a workgroup adds up in passing.)
 bool few_apart(int64_t n_seq, int H_kv, int64_t max_pages, int page_len) {
   return n_seq >= 4 && cuttable(H_kv, max_pages, page_len);
 }
+// (Not cut above 1024 sequences, which every workgroup would add up: 1024 x 70 rows over 400 positions of 8 heads 880
+// us, 1025 so 635; 128 prompts of 700 rows beside 896 single tokens over 2000 positions 2530, one more so 2467.)
 int target_of_few(int64_t n_seq, int H_kv, int64_t max_pages, int page_len) {
   return few_apart(n_seq, H_kv, max_pages, page_len) && n_seq <= 1024 ? 2 * CUS / H_kv : 0;
 }

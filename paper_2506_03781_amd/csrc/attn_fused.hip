@@ -969,7 +969,7 @@ static bool whole(const AttnLaunch& q) { return q.window <= 0 || std::max(q.wind
 
 // Whether the walks of a window's backward are split: where workgroups of four waves give one a CU at most, and the
 // longest walk is 384 rows or more: of all rows where the first keys are in sight, else of the window and a block.
-// Both directions' calls without and with the split, us: no first positions, 256 workgroups (L = 2048), windows of 1 /
+// Its call's time without and with the split, us: no first positions, 256 workgroups (L = 2048), windows of 1 /
 // 64 / 128 / 256 / 1024: 39 / 49 / 58 / 71 / 152 against 42 / 50 / 56 / 67 / 132; 288 workgroups 52 / 63 / 73 / 91 / 191
 // against 70 / 84 / 94 / 113 / 214.  First positions in sight, 256 workgroups, window 64: L = 512 70 against 65, 2048
 // 171 against 128; L = 256 (128 workgroups) 52 against 51, 384 (48) 58 against 54.
